@@ -375,6 +375,99 @@ int32_t ftc_agnn_layer_backward_fused(const ftc_csr *g, const ftc_windows *w, co
                                       void *stream);
 
 /*
+ * ---- Graph transformer -------------------------------------------------------------------------
+ * Layers of models that learn features per node id and attend between all nodes of a graph: the rows of a
+ * table by id, the dense layer with its epilogue, and attention over a batch of graphs, each with its
+ * gradients.  Matrices are row-major with a leading dimension at any alignment of an element (16-byte aligned
+ * rows are fastest), sums and softmax statistics fp32, results the same in every run.
+ */
+
+/*
+ * Rows of a table: out[i, :] = scale * E[ids[i], :], E vocab x D (dtype), out n x D (out_dtype).  An id outside
+ * [0, vocab) (a padded place, -1) gives a row of zeros.
+ * Gradient: dE[v, :] = scale * sum over {i : ids[i] = v} of dOut[i, :], all vocab rows written (zeros without
+ * an id), added up in fp32 by ascending i and rounded once; ids outside the table are left out.
+ */
+int32_t ftc_embedding(int32_t n, const int32_t *ids, int32_t vocab, const void *E, int32_t lde, int32_t dtype,
+                      int32_t D, float scale, void *out, int32_t ldo, int32_t out_dtype, void *stream);
+size_t ftc_embedding_backward_workspace_bytes(int32_t n, int32_t vocab, int32_t D);
+int32_t ftc_embedding_backward(int32_t n, const int32_t *ids, int32_t vocab, const void *dOut, int32_t lddo,
+                               int32_t dtype, int32_t D, float scale, void *dE, int32_t ldde, int32_t de_dtype,
+                               void *ws, size_t ws_bytes, void *stream);
+
+typedef enum {
+    FTC_ACT_NONE = 0,
+    FTC_ACT_RELU = 1,
+    FTC_ACT_GELU = 2, /* p Phi(p), the exact form */
+    FTC_ACT_SILU = 3  /* p / (1 + exp(-p)) */
+} ftc_act;
+
+/*
+ * Dense layer: Z = act(X * W + bias) + residual, X n x d_in and W d_in x d_out (contiguous) of `dtype`,
+ * bias (d_out numbers, may be NULL) and residual (n x d_out, may be NULL) of the same, Z n x d_out of z_dtype
+ * (fp32 or `dtype`); sums, activation and residual in fp32, one rounding at the end.  Z may be the residual itself
+ * (in place: same pointer, leading dimension and type).
+ * slope (n x d_out, may be NULL) receives act'(X * W + bias), which is all the backward pass needs of the
+ * activation: float for fp32 inputs, int16 for 16-bit ones (fixed point, 2^14 is 1; -2^15 is NaN).
+ * ftc_linear differs from ftc_update_gemm in the epilogue, and in its kernels, which are for layers of any
+ * width; narrow outputs of many rows with a row scale or ReLU alone are ftc_update_gemm's.
+ */
+size_t ftc_linear_workspace_bytes(int32_t n, int32_t d_in, int32_t d_out);
+int32_t ftc_linear(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W,
+                   int32_t d_out, const void *bias, int32_t act, const void *residual, int32_t ldr, void *slope,
+                   int32_t lds, void *Z, int32_t ldz, int32_t z_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Backward of ftc_linear for dL/dZ = dZ (n x d_out, `dtype`): dP = dZ * slope (slope NULL: no activation),
+ *   dX = dP * W^T (n x d_in, dx_dtype),  dW = X^T * dP (d_in x d_out, contiguous),  db = column sums of dP;
+ * dX, dW, db may each be NULL (not computed); dW and db are of dw_dtype; dx_dtype and dw_dtype are fp32 or `dtype`.
+ * The gradient of the residual is dZ.  dP is rounded to `dtype` for the products, db sums it unrounded.
+ */
+size_t ftc_linear_backward_workspace_bytes(int32_t n, int32_t d_in, int32_t d_out);
+int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W,
+                            int32_t d_out, const void *slope, int32_t lds, const void *dZ, int32_t lddz, void *dX,
+                            int32_t lddx, int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/*
+ * Attention inside every graph of a packed batch.  Graph g has the query rows q_ptr[g] .. q_ptr[g+1] of Q and out,
+ * and the rows kv_ptr[g] .. kv_ptr[g+1] of K and V (device int32, n_graphs + 1 entries, non-decreasing; the same
+ * array where every node attends to every node; one query a graph: a readout).  Head h has columns h D .. of Q and
+ * out, and columns (h / (heads / kv_heads)) D .. of K and V: kv_heads divides heads.  Q, K, V may be column ranges of one matrix.
+ *   s_ij = scale <q_i, k_j>,  p = softmax over the keys j of the graph with kv_mask[j] != 0,  out_i = sum_j p_ij v_j.
+ * kv_mask (n_kv bytes) may be NULL: all keys; K and V of masked keys are not read.  A query without a key gives
+ * zeros.  Rows in front of the first and behind the last graph are neither read nor written.  lse (n_q x heads floats, may be NULL)
+ * receives log sum_j exp(s_ij) (-inf without a key), what the backward pass needs.  All matrices are of `dtype`; D <= 128,
+ * n_q * heads and n_kv * kv_heads at most 2^30.  Offsets outside [0, n_q] ([0, n_kv]) are taken as the nearest end.
+ * In 16 bits the probabilities are rounded to `dtype` before they multiply V.
+ */
+size_t ftc_graph_attention_workspace_bytes(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads,
+                                           int32_t kv_heads, int32_t D);
+int32_t ftc_graph_attention(int32_t n_q, const int32_t *q_ptr, int32_t n_kv, const int32_t *kv_ptr,
+                            int32_t n_graphs, int32_t heads, int32_t kv_heads, int32_t D, int32_t dtype,
+                            const void *Q, int32_t ldq, const void *K, int32_t ldk, const void *V, int32_t ldv,
+                            const uint8_t *kv_mask, float scale, void *out, int32_t ldo, float *lse, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/*
+ * Gradients of ftc_graph_attention for dL/d(out) = dOut; out and lse as the forward call wrote them, the other
+ * arguments as it was given them.  The probabilities are computed again from lse, nothing of the size queries x keys is kept:
+ *   dV_j = sum_i p_ij dOut_i,  ds_ij = p_ij (<dOut_i, v_j> - <dOut_i, out_i>),
+ *   dQ_i = scale sum_j ds_ij k_j,  dK_j = scale sum_i ds_ij q_i   (sums over the heads that share a K/V head).
+ * All matrices are of `dtype`; rows of dK and dV of masked keys are zeros.  dQ, dK, dV must not overlap an input.  In 16 bits
+ * p and ds are rounded to `dtype` for their products.
+ */
+size_t ftc_graph_attention_backward_workspace_bytes(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads,
+                                                    int32_t kv_heads, int32_t D);
+int32_t ftc_graph_attention_backward(int32_t n_q, const int32_t *q_ptr, int32_t n_kv, const int32_t *kv_ptr,
+                                     int32_t n_graphs, int32_t heads, int32_t kv_heads, int32_t D, int32_t dtype,
+                                     const void *Q, int32_t ldq, const void *K, int32_t ldk, const void *V,
+                                     int32_t ldv, const uint8_t *kv_mask, float scale, const void *out, int32_t ldo,
+                                     const float *lse, const void *dOut, int32_t lddo, void *dQ, int32_t lddq,
+                                     void *dK, int32_t lddk, void *dV, int32_t lddv, void *ws, size_t ws_bytes,
+                                     void *stream);
+
+/*
  * ---- Locality reordering (preprocessing) ------------------------------------------------------
  * The sparse graph transformation (Section IV.A) condenses the columns that the rows of a window
  * share; how many they share, and how often a gathered feature row is still in cache, depends on

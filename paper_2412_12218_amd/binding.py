@@ -58,6 +58,18 @@ _SIGNATURES = {
     "ftc_agnn_layer_backward": (_I, [_P, _P, _P, _P, _I, _I, _I, _F, _P, _P, _I, _P, _I, _I, _P, _I, _P, _Z, _P]),
     "ftc_agnn_layer_backward_fused_workspace_bytes": (_Z, [_I, _I, _I]),
     "ftc_agnn_layer_backward_fused": (_I, [_P, _P, _P, _I, _I, _I, _F, _P, _P, _I, _I, _P, _I, _P, _I, _I, _P, _P, _P, _Z, _P]),
+    "ftc_embedding": (_I, [_I, _P, _I, _P, _I, _I, _I, _F, _P, _I, _I, _P]),
+    "ftc_embedding_backward_workspace_bytes": (_Z, [_I, _I, _I]),
+    "ftc_embedding_backward": (_I, [_I, _P, _I, _P, _I, _I, _I, _F, _P, _I, _I, _P, _Z, _P]),
+    "ftc_linear_workspace_bytes": (_Z, [_I, _I, _I]),
+    "ftc_linear": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _Z, _P]),
+    "ftc_linear_backward_workspace_bytes": (_Z, [_I, _I, _I]),
+    "ftc_linear_backward": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _P, _Z, _P]),
+    "ftc_graph_attention_workspace_bytes": (_Z, [_I, _I, _I, _I, _I, _I]),
+    "ftc_graph_attention": (_I, [_I, _P, _I, _P, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _F, _P, _I, _P, _P, _Z, _P]),
+    "ftc_graph_attention_backward_workspace_bytes": (_Z, [_I, _I, _I, _I, _I, _I]),
+    "ftc_graph_attention_backward": (_I, [_I, _P, _I, _P, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _F, _P, _I, _P, _P, _I,
+                                          _P, _I, _P, _I, _P, _I, _P, _Z, _P]),
     "ftc_reorder_workspace_bytes": (_Z, [_I, _I]),
     "ftc_degree_order": (_I, [_P, _I, _P, _P, _P, _Z, _P]),
     "ftc_order_by_key": (_I, [_I, _P, _P, _P, _P, _P, _Z, _P]),
@@ -434,6 +446,168 @@ def ftc_agnn_layer_backward_fused(g, w, H, row_z, Y, dY, beta=1.0, dH=None, dh_d
         dH.stride(0), _dt(dH), _ptr(dbeta), _ptr(pattern_flag), _ptr(ws), ws.numel(),
         _stream()))
     return dH, dbeta
+
+
+# ---- graph transformer ----------------------------------------------------------------------------------
+FTC_ACT_NONE, FTC_ACT_RELU, FTC_ACT_GELU, FTC_ACT_SILU = 0, 1, 2, 3
+
+
+def _check_tensors(*tensors):
+    """All on the current device, on whose stream the call is made."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _ld(t, rows, cols, dtype=None):
+    """Leading dimension of a rows x cols matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"expected {rows} x {cols}" + (f" of {dtype}" if dtype is not None else "") + f", got {tuple(t.shape)} of {t.dtype}")
+    st, sc = t.stride()
+    if cols > 1 and sc != 1:
+        raise ValueError("rows must be contiguous")
+    return st if rows > 1 else max(st, cols)
+
+
+def _vector(t, numel, dtypes):
+    if t.dim() != 1 or (numel is not None and t.numel() != numel) or t.dtype not in dtypes or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous vector of {numel} {dtypes}, got {tuple(t.shape)} of {t.dtype}")
+
+
+def ftc_embedding(ids, E, scale=1.0, out=None, out_dtype=None):
+    """scale * E[ids], zeros for ids outside the table; out in E's type unless given."""
+    n, (vocab, D) = ids.numel(), E.shape
+    if out is None:
+        out = torch.empty((n, D), dtype=out_dtype or E.dtype, device=E.device)
+    _vector(ids, n, (torch.int32,))
+    _check_tensors(ids, E, out)
+    _check(lib().ftc_embedding(n, _ptr(ids), vocab, _ptr(E), _ld(E, vocab, D), _dt(E), D, scale, _ptr(out), _ld(out, n, D), _dt(out),
+                               _stream()))
+    return out
+
+
+def ftc_embedding_backward(ids, dOut, vocab, scale=1.0, dE=None, de_dtype=torch.float32, ws=None):
+    n, D = dOut.shape
+    if dE is None:
+        dE = torch.empty((vocab, D), dtype=de_dtype, device=dOut.device)
+    if ws is None:
+        ws = _workspace(lib().ftc_embedding_backward_workspace_bytes(n, vocab, D), dOut.device)
+    _vector(ids, n, (torch.int32,))
+    _check_tensors(ids, dOut, dE, ws)
+    _check(lib().ftc_embedding_backward(n, _ptr(ids), vocab, _ptr(dOut), _ld(dOut, n, D), _dt(dOut), D, scale, _ptr(dE),
+                                        _ld(dE, vocab, D), _dt(dE), _ptr(ws), ws.numel(), _stream()))
+    return dE
+
+
+def slope_like(t):
+    """A tensor of t's shape for the activation slopes that ftc_linear keeps for inputs of t's type."""
+    return torch.empty(t.shape, dtype=torch.float32 if t.dtype == torch.float32 else torch.int16, device=t.device)
+
+
+def ftc_linear(X, W, bias=None, act=FTC_ACT_NONE, residual=None, out=None, out_dtype=None, slope=None, ws=None):
+    """act(X W + bias) + residual; out in X's type unless given.  slope: see slope_like."""
+    n, d_in = X.shape
+    d_out = W.shape[1]
+    if out is None:
+        out = torch.empty((n, d_out), dtype=out_dtype or X.dtype, device=X.device)
+    if ws is None:
+        ws = _workspace(lib().ftc_linear_workspace_bytes(n, d_in, d_out), X.device)
+    _check_tensors(X, W, bias, residual, out, slope, ws)
+    _ld(W, d_in, d_out, X.dtype)
+    if not W.is_contiguous():
+        raise ValueError("W must be contiguous")
+    if bias is not None:
+        _vector(bias, d_out, (X.dtype,))
+    sdt = torch.float32 if X.dtype == torch.float32 else torch.int16
+    _check(lib().ftc_linear(n, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(bias), act, _ptr(residual),
+                            _ld(residual, n, d_out, X.dtype) if residual is not None else 0, _ptr(slope),
+                            _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(out), _ld(out, n, d_out), _dt(out), _ptr(ws),
+                            ws.numel(), _stream()))
+    return out
+
+
+def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_db=True, dX=None, dx_dtype=None, dW=None, db=None,
+                        dw_dtype=torch.float32, ws=None):
+    """(dX, dW, db); dX in X's type unless given; dW and db share a type (dw_dtype where they are not given)."""
+    n, d_in = X.shape
+    d_out = W.shape[1]
+    if dX is None and want_dX:
+        dX = torch.empty((n, d_in), dtype=dx_dtype or X.dtype, device=X.device)
+    wdt = dW.dtype if dW is not None else db.dtype if db is not None else dw_dtype
+    if dW is None and want_dW:
+        dW = torch.empty((d_in, d_out), dtype=wdt, device=X.device)
+    if db is None and want_db:
+        db = torch.empty(d_out, dtype=wdt, device=X.device)
+    if ws is None:
+        ws = _workspace(lib().ftc_linear_backward_workspace_bytes(n, d_in, d_out), X.device)
+    _check_tensors(X, W, dZ, slope, dX, dW, db, ws)
+    _ld(W, d_in, d_out, X.dtype)
+    if not W.is_contiguous() or (dW is not None and not dW.is_contiguous()):
+        raise ValueError("W and dW must be contiguous")
+    if dW is not None:
+        _ld(dW, d_in, d_out, wdt)
+    if db is not None:
+        _vector(db, d_out, (wdt,))
+    sdt = torch.float32 if X.dtype == torch.float32 else torch.int16
+    _check(lib().ftc_linear_backward(n, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(slope),
+                                     _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(dZ), _ld(dZ, n, d_out, X.dtype),
+                                     _ptr(dX), _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
+                                     _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), _stream()))
+    return dX, dW, db
+
+
+def _attention_sizes(Q, K, V, q_ptr, kv_ptr, heads, kv_heads, kv_mask):
+    if heads < 1 or Q.dim() != 2 or Q.shape[1] % heads:
+        raise ValueError("Q has heads * D columns")
+    n_q, D, n_kv, graphs = Q.shape[0], Q.shape[1] // heads, K.shape[0], q_ptr.numel() - 1
+    _vector(q_ptr, graphs + 1, (torch.int32,))
+    _vector(kv_ptr, graphs + 1, (torch.int32,))
+    if kv_mask is not None:
+        _vector(kv_mask, n_kv, (torch.uint8, torch.bool))
+    return n_q, n_kv, graphs, heads, kv_heads, D
+
+
+def ftc_graph_attention(Q, K, V, q_ptr, kv_ptr, heads, kv_heads=None, scale=None, kv_mask=None, out=None, lse=None, ws=None):
+    """Attention inside every graph of a packed batch; Q n_q x (heads D), K and V n_kv x (kv_heads D).  scale: 1 / sqrt(D) unless
+    given.  lse: n_q x heads fp32, for the backward pass."""
+    kv_heads = heads if kv_heads is None else kv_heads
+    sizes = n_q, n_kv, graphs, _, _, D = _attention_sizes(Q, K, V, q_ptr, kv_ptr, heads, kv_heads, kv_mask)
+    if out is None:
+        out = torch.empty((n_q, heads * D), dtype=Q.dtype, device=Q.device)
+    if ws is None:
+        ws = _workspace(lib().ftc_graph_attention_workspace_bytes(*sizes), Q.device)
+    _check_tensors(Q, K, V, q_ptr, kv_ptr, kv_mask, out, lse, ws)
+    dt = Q.dtype
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_q, heads) or not lse.is_contiguous()):
+        raise ValueError("lse is a contiguous n_q x heads fp32 tensor")
+    _check(lib().ftc_graph_attention(n_q, _ptr(q_ptr), n_kv, _ptr(kv_ptr), graphs, heads, kv_heads, D, _DTYPES[dt],
+                                     _ptr(Q), _ld(Q, n_q, heads * D), _ptr(K), _ld(K, n_kv, kv_heads * D, dt), _ptr(V),
+                                     _ld(V, n_kv, kv_heads * D, dt), _ptr(kv_mask), D ** -0.5 if scale is None else scale, _ptr(out),
+                                     _ld(out, n_q, heads * D, dt), _ptr(lse), _ptr(ws), ws.numel(), _stream()))
+    return out
+
+
+def ftc_graph_attention_backward(Q, K, V, q_ptr, kv_ptr, out, lse, dOut, heads, kv_heads=None, scale=None, kv_mask=None, dQ=None,
+                                 dK=None, dV=None, ws=None):
+    """(dQ, dK, dV) in Q's type."""
+    kv_heads = heads if kv_heads is None else kv_heads
+    sizes = n_q, n_kv, graphs, _, _, D = _attention_sizes(Q, K, V, q_ptr, kv_ptr, heads, kv_heads, kv_mask)
+    dt = Q.dtype
+    new = lambda t: torch.empty(t.shape, dtype=dt, device=Q.device)
+    dQ, dK, dV = dQ if dQ is not None else new(Q), dK if dK is not None else new(K), dV if dV is not None else new(V)
+    if ws is None:
+        ws = _workspace(lib().ftc_graph_attention_backward_workspace_bytes(*sizes), Q.device)
+    _check_tensors(Q, K, V, q_ptr, kv_ptr, kv_mask, out, lse, dOut, dQ, dK, dV, ws)
+    if lse.dtype != torch.float32 or lse.shape != (n_q, heads) or not lse.is_contiguous():
+        raise ValueError("lse is a contiguous n_q x heads fp32 tensor")
+    hd, kd = heads * D, kv_heads * D
+    _check(lib().ftc_graph_attention_backward(
+        n_q, _ptr(q_ptr), n_kv, _ptr(kv_ptr), graphs, heads, kv_heads, D, _DTYPES[dt], _ptr(Q), _ld(Q, n_q, hd), _ptr(K), _ld(K, n_kv, kd, dt),
+        _ptr(V), _ld(V, n_kv, kd, dt), _ptr(kv_mask), D ** -0.5 if scale is None else scale, _ptr(out), _ld(out, n_q, hd, dt), _ptr(lse),
+        _ptr(dOut), _ld(dOut, n_q, hd, dt), _ptr(dQ), _ld(dQ, n_q, hd, dt), _ptr(dK), _ld(dK, n_kv, kd, dt), _ptr(dV),
+        _ld(dV, n_kv, kd, dt), _ptr(ws), ws.numel(), _stream()))
+    return dQ, dK, dV
 
 
 # ---- locality reordering ------------------------------------------------------------------------------

@@ -787,6 +787,226 @@ int32_t ftc_agnn_layer_backward_fused(const ftc_csr *g, const ftc_windows *w, co
                                       pattern_flag, ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
+// ---- graph transformer ---------------------------------------------------------------------------
+static int32_t check_ws(const char *who, size_t need, const void *ws, size_t ws_bytes)
+{
+    if (need == 0) return FTC_OK;
+    if (!ws || ws_bytes < need)
+        return fail(FTC_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, ws ? ws_bytes : static_cast<size_t>(0));
+    if (reinterpret_cast<uintptr_t>(ws) % 256 != 0) return fail(FTC_EALIGN, "%s: workspace must be 256-byte aligned", who);
+    return FTC_OK;
+}
+
+static int32_t check_out_type(const char *who, const char *name, int32_t dtype, int32_t out_dtype)
+{
+    if (out_dtype != FTC_F32 && out_dtype != dtype)
+        return fail(FTC_EUNSUPPORTED, "%s: %s is fp32 or of the type of the inputs", who, name);
+    return FTC_OK;
+}
+
+int32_t ftc_embedding(int32_t n, const int32_t *ids, int32_t vocab, const void *E, int32_t lde, int32_t dtype, int32_t D,
+                      float scale, void *out, int32_t ldo, int32_t out_dtype, void *stream)
+{
+    const char *who = "ftc_embedding";
+    if (n < 0 || vocab < 0) return fail(FTC_EINVAL, "%s: negative n or vocab", who);
+    if (n == 0) return FTC_OK;
+    if (!ids) return fail(FTC_EINVAL, "%s: ids is NULL", who);
+    if (vocab > 0) FTC_TRY(check_dense(E, lde, dtype, D, who, "E"));
+    if (!valid_dtype(dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for E", who);
+    FTC_TRY(check_dense(out, ldo, out_dtype, D, who, "out"));
+    if (out == E) return fail(FTC_EINVAL, "%s: out aliases E", who);
+    return launch_embedding(n, ids, vocab, E, lde, dtype, D, scale, out, ldo, out_dtype, static_cast<hipStream_t>(stream));
+}
+
+size_t ftc_embedding_backward_workspace_bytes(int32_t n, int32_t vocab, int32_t D)
+{
+    if (n < 0 || vocab < 0 || D < 1) return 0;
+    return embedding_backward_ws(n, vocab, D);
+}
+
+int32_t ftc_embedding_backward(int32_t n, const int32_t *ids, int32_t vocab, const void *dOut, int32_t lddo, int32_t dtype,
+                               int32_t D, float scale, void *dE, int32_t ldde, int32_t de_dtype, void *ws, size_t ws_bytes,
+                               void *stream)
+{
+    const char *who = "ftc_embedding_backward";
+    if (n < 0 || vocab < 0) return fail(FTC_EINVAL, "%s: negative n or vocab", who);
+    if (vocab == 0) return FTC_OK;
+    if (n > 0) {
+        if (!ids) return fail(FTC_EINVAL, "%s: ids is NULL", who);
+        FTC_TRY(check_dense(dOut, lddo, dtype, D, who, "dOut"));
+    }
+    if (!valid_dtype(dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for dOut", who);
+    FTC_TRY(check_dense(dE, ldde, de_dtype, D, who, "dE"));
+    if (dE == dOut) return fail(FTC_EINVAL, "%s: dE aliases dOut", who);
+    FTC_TRY(check_ws(who, embedding_backward_ws(n, vocab, D), ws, ws_bytes));
+    return launch_embedding_backward(n, ids, vocab, dOut, lddo, dtype, D, scale, dE, ldde, de_dtype, ws,
+                                     static_cast<hipStream_t>(stream));
+}
+
+size_t ftc_linear_workspace_bytes(int32_t n, int32_t d_in, int32_t d_out)
+{
+    if (n < 0 || d_in < 1 || d_out < 1) return 0;
+    return linear_ws(n, d_in, d_out);
+}
+
+int32_t ftc_linear(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W, int32_t d_out,
+                   const void *bias, int32_t act, const void *residual, int32_t ldr, void *slope, int32_t lds, void *Z,
+                   int32_t ldz, int32_t z_dtype, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_linear";
+    if (n < 0) return fail(FTC_EINVAL, "%s: negative n", who);
+    if (act < FTC_ACT_NONE || act > FTC_ACT_SILU) return fail(FTC_EINVAL, "%s: unknown activation %d", who, act);
+    if (n == 0) return FTC_OK;
+    FTC_TRY(check_dense(X, ldx, dtype, d_in, who, "X"));
+    FTC_TRY(check_dense(W, d_out, dtype, d_out, who, "W"));
+    FTC_TRY(check_dense(Z, ldz, z_dtype, d_out, who, "Z"));
+    FTC_TRY(check_out_type(who, "Z", dtype, z_dtype));
+    if (bias) FTC_TRY(check_dense(bias, d_out, dtype, d_out, who, "bias"));
+    if (residual) FTC_TRY(check_dense(residual, ldr, dtype, d_out, who, "residual"));
+    if (slope) {
+        if (lds < d_out) return fail(FTC_EINVAL, "%s: need ld >= D for slope", who);
+        if (reinterpret_cast<uintptr_t>(slope) % elem_size(dtype) != 0)
+            return fail(FTC_EALIGN, "%s: slope is not aligned to its element size", who);
+    }
+    if (Z == X || Z == W || Z == bias || Z == slope || (slope && (slope == X || slope == W || slope == bias || slope == residual)))
+        return fail(FTC_EINVAL, "%s: an output aliases an input or the other output", who);
+    if (Z == residual && (ldz != ldr || z_dtype != dtype))
+        return fail(FTC_EINVAL, "%s: Z on top of the residual needs its leading dimension and type", who);
+    FTC_TRY(check_ws(who, linear_ws(n, d_in, d_out), ws, ws_bytes));
+    const LinearShape p = {n, d_in, d_out, dtype, X, W, bias, residual, slope, Z, ldx, ldr, lds, ldz, act, z_dtype};
+    return launch_linear(p, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t ftc_linear_backward_workspace_bytes(int32_t n, int32_t d_in, int32_t d_out)
+{
+    if (n < 0 || d_in < 1 || d_out < 1) return 0;
+    return linear_backward_ws(n, d_in, d_out);
+}
+
+int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W, int32_t d_out,
+                            const void *slope, int32_t lds, const void *dZ, int32_t lddz, void *dX, int32_t lddx,
+                            int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_linear_backward";
+    if (n < 0 || d_in < 1 || d_out < 1) return fail(FTC_EINVAL, "%s: negative n, or a width below 1", who);
+    if (!valid_dtype(dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for X", who);
+    if (n > 0) {
+        if (dW) FTC_TRY(check_dense(X, ldx, dtype, d_in, who, "X"));
+        if (dX) FTC_TRY(check_dense(W, d_out, dtype, d_out, who, "W"));
+        FTC_TRY(check_dense(dZ, lddz, dtype, d_out, who, "dZ"));
+        if (slope && lds < d_out) return fail(FTC_EINVAL, "%s: need ld >= D for slope", who);
+        if (reinterpret_cast<uintptr_t>(slope) % elem_size(dtype) != 0)
+            return fail(FTC_EALIGN, "%s: slope is not aligned to its element size", who);
+        if (dX) {
+            FTC_TRY(check_dense(dX, lddx, dx_dtype, d_in, who, "dX"));
+            FTC_TRY(check_out_type(who, "dX", dtype, dx_dtype));
+        }
+    }
+    if (dW) FTC_TRY(check_dense(dW, d_out, dw_dtype, d_out, who, "dW"));
+    if (db) FTC_TRY(check_dense(db, d_out, dw_dtype, d_out, who, "db"));
+    if (dW || db) FTC_TRY(check_out_type(who, "dW", dtype, dw_dtype));
+    const void *outs[3] = {dX, dW, db}, *ins[4] = {X, W, slope, dZ};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 4; ++j)
+            if (outs[i] && outs[i] == ins[j]) return fail(FTC_EINVAL, "%s: an output aliases an input", who);
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return fail(FTC_EINVAL, "%s: two outputs are the same", who);
+    }
+    FTC_TRY(check_ws(who, linear_backward_ws(n, d_in, d_out), ws, ws_bytes));
+    const LinearShape p = {n, d_in, d_out, dtype, X, W, nullptr, nullptr, const_cast<void *>(slope), nullptr, ldx, 0, lds, 0, FTC_ACT_NONE, dtype};
+    const LinearGrads g = {dZ, dX, dW, db, lddz, lddx, dx_dtype, dw_dtype};
+    return launch_linear_backward(p, g, ws, static_cast<hipStream_t>(stream));
+}
+
+static constexpr int64_t ATTENTION_MOST_ROWS = 1 << 30;  // rows and heads of a matrix together, counted in int32
+static constexpr int32_t ATTENTION_MOST_HEADS = 65535;   // K/V heads are a dimension of the grid
+
+static bool attention_sizes_ok(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads, int32_t kv_heads, int32_t D)
+{
+    return n_q >= 0 && n_kv >= 0 && n_graphs >= 0 && n_graphs <= ATTENTION_MOST_ROWS && heads >= 1 && kv_heads >= 1 &&
+           kv_heads <= ATTENTION_MOST_HEADS && heads % kv_heads == 0 && D >= 1 && D <= 128 &&
+           static_cast<int64_t>(n_q) * heads <= ATTENTION_MOST_ROWS && static_cast<int64_t>(n_kv) * kv_heads <= ATTENTION_MOST_ROWS;
+}
+
+static int32_t check_attention(const char *who, const AttnShape &p)
+{
+    if (p.n_q < 0 || p.n_kv < 0 || p.graphs < 0) return fail(FTC_EINVAL, "%s: negative n_q, n_kv or n_graphs", who);
+    if (p.heads < 1 || p.kv_heads < 1 || p.heads % p.kv_heads != 0)
+        return fail(FTC_EINVAL, "%s: heads must be a multiple of kv_heads, both at least 1", who);
+    if (p.D < 1) return fail(FTC_EINVAL, "%s: need D >= 1", who);
+    if (!attention_sizes_ok(p.n_q, p.n_kv, p.graphs, p.heads, p.kv_heads, p.D))
+        return fail(FTC_EUNSUPPORTED, "%s: D is at most 128, kv_heads 65535, n_q * heads and n_kv * kv_heads 2^30", who);
+    if (!valid_dtype(p.dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype", who);
+    if (p.graphs > 0 && (!p.q_ptr || !p.kv_ptr)) return fail(FTC_EINVAL, "%s: q_ptr or kv_ptr is NULL", who);
+    if (static_cast<int64_t>(p.heads) * p.D > INT32_MAX) return fail(FTC_EUNSUPPORTED, "%s: heads * D does not fit 32 bits", who);
+    if (p.n_q > 0) FTC_TRY(check_dense(p.Q, p.ldq, p.dtype, p.heads * p.D, who, "Q"));
+    if (p.n_kv > 0) {
+        FTC_TRY(check_dense(p.K, p.ldk, p.dtype, p.kv_heads * p.D, who, "K"));
+        FTC_TRY(check_dense(p.V, p.ldv, p.dtype, p.kv_heads * p.D, who, "V"));
+    }
+    return FTC_OK;
+}
+
+size_t ftc_graph_attention_workspace_bytes(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads, int32_t kv_heads, int32_t D)
+{
+    if (!attention_sizes_ok(n_q, n_kv, n_graphs, heads, kv_heads, D)) return 0;
+    return attention_ws(n_q, n_kv, n_graphs, heads, kv_heads, D);
+}
+
+int32_t ftc_graph_attention(int32_t n_q, const int32_t *q_ptr, int32_t n_kv, const int32_t *kv_ptr, int32_t n_graphs,
+                            int32_t heads, int32_t kv_heads, int32_t D, int32_t dtype, const void *Q, int32_t ldq, const void *K,
+                            int32_t ldk, const void *V, int32_t ldv, const uint8_t *kv_mask, float scale, void *out, int32_t ldo,
+                            float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_graph_attention";
+    const AttnShape p = {n_q, n_kv, n_graphs, heads, kv_heads, D, dtype, Q, K, V, ldq, ldk, ldv, q_ptr, kv_ptr, kv_mask, scale};
+    FTC_TRY(check_attention(who, p));
+    if (n_q == 0 || n_graphs == 0) return FTC_OK;
+    FTC_TRY(check_dense(out, ldo, dtype, heads * D, who, "out"));
+    if (out == Q || out == K || out == V) return fail(FTC_EINVAL, "%s: out aliases an input", who);
+    FTC_TRY(check_ws(who, attention_ws(n_q, n_kv, n_graphs, heads, kv_heads, D), ws, ws_bytes));
+    return launch_attention(p, out, ldo, lse, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t ftc_graph_attention_backward_workspace_bytes(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads, int32_t kv_heads,
+                                                    int32_t D)
+{
+    if (!attention_sizes_ok(n_q, n_kv, n_graphs, heads, kv_heads, D)) return 0;
+    return attention_backward_ws(n_q, n_kv, n_graphs, heads, kv_heads, D);
+}
+
+int32_t ftc_graph_attention_backward(int32_t n_q, const int32_t *q_ptr, int32_t n_kv, const int32_t *kv_ptr, int32_t n_graphs,
+                                     int32_t heads, int32_t kv_heads, int32_t D, int32_t dtype, const void *Q, int32_t ldq,
+                                     const void *K, int32_t ldk, const void *V, int32_t ldv, const uint8_t *kv_mask, float scale,
+                                     const void *out, int32_t ldo, const float *lse, const void *dOut, int32_t lddo, void *dQ,
+                                     int32_t lddq, void *dK, int32_t lddk, void *dV, int32_t lddv, void *ws, size_t ws_bytes,
+                                     void *stream)
+{
+    const char *who = "ftc_graph_attention_backward";
+    const AttnShape p = {n_q, n_kv, n_graphs, heads, kv_heads, D, dtype, Q, K, V, ldq, ldk, ldv, q_ptr, kv_ptr, kv_mask, scale};
+    FTC_TRY(check_attention(who, p));
+    if (n_graphs == 0 || (n_q == 0 && n_kv == 0)) return FTC_OK;
+    if (n_q > 0) {
+        FTC_TRY(check_dense(out, ldo, dtype, heads * D, who, "out"));
+        FTC_TRY(check_dense(dOut, lddo, dtype, heads * D, who, "dOut"));
+        FTC_TRY(check_dense(dQ, lddq, dtype, heads * D, who, "dQ"));
+        if (!lse) return fail(FTC_EINVAL, "%s: lse is NULL", who);
+    }
+    if (n_kv > 0) {
+        FTC_TRY(check_dense(dK, lddk, dtype, kv_heads * D, who, "dK"));
+        FTC_TRY(check_dense(dV, lddv, dtype, kv_heads * D, who, "dV"));
+    }
+    const void *outs[3] = {n_q > 0 ? dQ : nullptr, n_kv > 0 ? dK : nullptr, n_kv > 0 ? dV : nullptr}, *ins[6] = {Q, K, V, out, dOut, lse};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 6; ++j)
+            if (outs[i] && outs[i] == ins[j]) return fail(FTC_EINVAL, "%s: an output aliases an input", who);
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return fail(FTC_EINVAL, "%s: two outputs are the same", who);
+    }
+    FTC_TRY(check_ws(who, attention_backward_ws(n_q, n_kv, n_graphs, heads, kv_heads, D), ws, ws_bytes));
+    return launch_attention_backward(p, out, ldo, lse, dOut, lddo, dQ, lddq, dK, lddk, dV, lddv, ws, static_cast<hipStream_t>(stream));
+}
+
 // ---- locality reordering (preprocessing) ---------------------------------------------------------
 size_t ftc_reorder_workspace_bytes(int32_t n, int32_t nnz)
 {

@@ -176,6 +176,47 @@ size_t build_windows_ws(int n, int nnz, int blk_h, int blk_w);
 int32_t launch_build_windows(const ftc_csr &g, ftc_windows &w, void *ws, size_t ws_bytes, const ftc_side_streams *side,
                              hipStream_t s);
 
+// reorder.hip: positions 0 .. n - 1 by ascending id, ties by position; an id outside [0, vocab) comes last, as vocab.  keys and order
+// are in `ws`, which stays theirs until they are read.
+size_t id_sort_ws(int n);
+int32_t launch_sort_ids(int n, const int *ids, int vocab, const uint32_t **keys, const uint32_t **order, void *ws, hipStream_t s);
+// embedding.hip
+int32_t launch_embedding(int n, const int *ids, int vocab, const void *E, int lde, int dt, int D, float scale, void *out, int ldo, int odt,
+                         hipStream_t s);
+size_t embedding_backward_ws(int n, int vocab, int D);
+int32_t launch_embedding_backward(int n, const int *ids, int vocab, const void *G, int ldg, int dt, int D, float scale, void *dE, int lde,
+                                  int de_dt, void *ws, hipStream_t s);
+// linear.hip
+struct LinearShape {
+    int n, d_in, d_out, dtype;
+    const void *X, *W, *bias, *residual;
+    void *slope, *Z;
+    int ldx, ldr, lds, ldz, act, z_dtype;
+};
+struct LinearGrads {
+    const void *dZ;
+    void *dX, *dW, *db;
+    int lddz, lddx, dx_dtype, dw_dtype;
+};
+size_t linear_ws(int n, int d_in, int d_out);
+int32_t launch_linear(const LinearShape &p, void *ws, hipStream_t s);
+size_t linear_backward_ws(int n, int d_in, int d_out);
+int32_t launch_linear_backward(const LinearShape &p, const LinearGrads &g, void *ws, hipStream_t s);
+// graph_attention.hip
+struct AttnShape {
+    int n_q, n_kv, graphs, heads, kv_heads, D, dtype;
+    const void *Q, *K, *V;
+    int ldq, ldk, ldv;
+    const int *q_ptr, *kv_ptr;
+    const uint8_t *kv_mask;
+    float scale;
+};
+size_t attention_ws(int n_q, int n_kv, int graphs, int heads, int kv_heads, int D);
+int32_t launch_attention(const AttnShape &p, void *out, int ldo, float *lse, void *ws, hipStream_t s);
+size_t attention_backward_ws(int n_q, int n_kv, int graphs, int heads, int kv_heads, int D);
+int32_t launch_attention_backward(const AttnShape &p, const void *out, int ldo, const float *lse, const void *dO, int lddo, void *dQ, int lddq,
+                                  void *dK, int lddk, void *dV, int lddv, void *ws, hipStream_t s);
+
 // ---- device side -----------------------------------------------------------------------------
 #if defined(__HIPCC__)
 

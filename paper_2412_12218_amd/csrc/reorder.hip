@@ -387,6 +387,39 @@ int32_t launch_order_by_key(int n, const int *keys_in, int *perm, int *inv, int 
     return launch_status("order by key");
 }
 
+// ---- positions by id -------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void id_pairs_kernel(int n, const int *__restrict__ ids, int vocab, uint32_t *__restrict__ keys,
+                                                       uint32_t *__restrict__ vals)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int id = ids[i];
+    keys[i] = static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab);
+    vals[i] = static_cast<uint32_t>(i);
+}
+
+static size_t id_table_bytes(int n)
+{
+    const int64_t table = 256 * radix_tiles(n, radix_rounds(n));
+    return align_up(static_cast<size_t>(table) * sizeof(int), 256) + scan_ws(table);
+}
+
+size_t id_sort_ws(int n) { return 4 * align_up(static_cast<size_t>(n) * sizeof(uint32_t), 256) + id_table_bytes(n); }
+
+int32_t launch_sort_ids(int n, const int *ids, int vocab, const uint32_t **keys, const uint32_t **order, void *ws, hipStream_t s)
+{
+    const size_t arr = align_up(static_cast<size_t>(n) * sizeof(uint32_t), 256);
+    char *p = static_cast<char *>(ws);
+    uint32_t *k0 = reinterpret_cast<uint32_t *>(p), *v0 = reinterpret_cast<uint32_t *>(p + arr);
+    uint32_t *k1 = reinterpret_cast<uint32_t *>(p + 2 * arr), *v1 = reinterpret_cast<uint32_t *>(p + 3 * arr);
+    if (n > 0) hipLaunchKernelGGL(id_pairs_kernel, dim3(ceil_div(n, 256)), dim3(256), 0, s, n, ids, vocab, k0, v0);
+    uint32_t *kr, *vr;
+    const int32_t st = radix_sort_pairs(k0, v0, k1, v1, n, bit_length(static_cast<uint32_t>(vocab)), nullptr, &kr, &vr, p + 4 * arr, s, true);
+    *keys = kr;
+    *order = vr;
+    return st;
+}
+
 // ---- label propagation ---------------------------------------------------------------------------
 // Graphs of at most ROW_SORT_NODES nodes are handled row by row (reorder_rows.hip).  Above, every round: pairs (label of the
 // entry's column, row) sorted by label and then, stably, by row put equal labels of a row side by side; a run of equal

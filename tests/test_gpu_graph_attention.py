@@ -1,0 +1,229 @@
+"""Attention inside the graphs of a packed batch, and its gradients, against their formulas in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2412_12218_amd import binding as B
+from transformer_reference import attention, check
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+def offsets(lens, first=0):
+    return torch.tensor(np.concatenate([[first], first + np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+
+
+class Batch:
+    """Inputs of a batch: Q, K, V column ranges of one matrix where every node attends to every node (odd leading dimensions)."""
+
+    def __init__(self, lens, heads, kv_heads, D, dtype, qlens=None, masked=0.0, seed=0, before=0, behind=0, spread=1.0):
+        gen = torch.Generator().manual_seed(seed)
+        new = lambda n, c: torch.randn((n, c), generator=gen).mul_(spread).to(dtype).cuda()
+        self.heads, self.kv_heads, self.D = heads, kv_heads, D
+        n_kv = before + sum(lens) + behind
+        self.kv_ptr = offsets(lens, before)
+        hd, kd = heads * D, kv_heads * D
+        if qlens is None:
+            self.q_ptr, n_q = self.kv_ptr, n_kv
+            whole = new(n_kv, hd + 2 * kd + 1)
+            self.Q, self.K, self.V = whole[:, :hd], whole[:, hd:hd + kd], whole[:, hd + kd:hd + 2 * kd]
+        else:
+            self.q_ptr, n_q = offsets(qlens, before), before + sum(qlens) + behind
+            self.Q, self.K, self.V = new(n_q, hd + 3)[:, :hd], new(n_kv, kd), new(n_kv, kd + 2)[:, :kd]
+        self.dO = new(n_q, hd)
+        self.n_q, self.n_kv, self.scale = n_q, n_kv, D ** -0.5
+        self.mask = None
+        if masked:
+            self.mask = (torch.rand(n_kv, generator=gen) >= masked).to(torch.uint8).cuda()
+
+    def args(self):
+        return self.Q, self.K, self.V, self.q_ptr, self.kv_ptr
+
+    def kw(self):
+        return dict(heads=self.heads, kv_heads=self.kv_heads, scale=self.scale, kv_mask=self.mask)
+
+    def run(self, backward=True):
+        dt = self.Q.dtype
+        full = lambda n, c, t=dt: torch.full((n, c + 1), float("nan"), dtype=t, device="cuda")[:, :c]
+        out, lse = full(self.n_q, self.heads * self.D), torch.full((self.n_q, self.heads), float("nan"), device="cuda")
+        B.ftc_graph_attention(*self.args(), out=out, lse=lse, **self.kw())
+        got = dict(out=out, lse=lse)
+        if backward:
+            g = [full(self.n_q, self.heads * self.D), full(self.n_kv, self.kv_heads * self.D), full(self.n_kv, self.kv_heads * self.D)]
+            B.ftc_graph_attention_backward(*self.args(), out, lse, self.dO, dQ=g[0], dK=g[1], dV=g[2], **self.kw())
+            got.update(dQ=g[0], dK=g[1], dV=g[2])
+        return got
+
+    def check(self, name, backward=True):
+        got = self.run(backward)
+        want = attention(*self.args(), self.heads, self.kv_heads, self.scale, self.mask, self.dO if backward else None)
+        for key, (value, bound) in want.items():
+            check(f"{name} {key}", got[key], value, bound)
+        again = self.run(backward)
+        assert all(torch.equal(got[k].view(torch.int32 if got[k].dtype == torch.float32 else torch.int16),
+                               again[k].view(torch.int32 if got[k].dtype == torch.float32 else torch.int16))
+                   if got[k].is_contiguous() else torch.equal(got[k].nan_to_num(9.0), again[k].nan_to_num(9.0)) for k in got)
+        return got
+
+
+LENS = [[1], [33], [128], [129], [5, 0, 64, 1, 32, 65], [300, 7], [23, 40, 1, 0, 50, 31, 32, 33, 2, 17] * 3]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [1, 20, 32, 37, 64, 65, 96, 128])
+@pytest.mark.parametrize("lens", LENS, ids=lambda v: f"{len(v)}x{max(v)}")
+def test_every_node_to_every_node(dtype, D, lens):
+    Batch(lens, 2, 2, D, dtype, seed=D).check(f"{dtype} D={D} {lens[:6]}")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (6, 2), (4, 1), (9, 3), (5, 5)])
+def test_shared_heads(dtype, heads, kv_heads):
+    Batch([70, 1, 150, 0, 31], heads, kv_heads, 40, dtype, masked=0.3, seed=heads).check(f"{dtype} {heads} over {kv_heads}")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("qlens,lens", [([1], [1]), ([1, 1, 1], [2000, 1, 900]), ([3, 0, 1, 2], [700, 50, 0, 64]), ([1000], [5]), ([2000, 3], [40, 0]),
+                                        ([1] * 40, [60, 3] * 20), ([600, 20], [20, 600])], ids=lambda v: f"{len(v)}x{max(v)}")
+def test_queries_of_their_own(dtype, qlens, lens):
+    """Readouts and the like: few queries over many keys and many over few, split over workgroups where one side is short."""
+    for heads, kv_heads in ((2, 2), (4, 1)):
+        Batch(lens, heads, kv_heads, 64, dtype, qlens=qlens, masked=0.1, seed=len(qlens)).check(f"{dtype} {qlens[:4]} over {lens[:4]}")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_single_tokens(dtype):
+    """One key: p = 1, so out = v and ds = 0 exactly, and dV = dO.  The backward pass takes p = exp(s - lse) from an lse that is rounded
+    to fp32: with |lse| below 8 and three roundings on the way (lse, its factor log2 e, the difference) p is off by at most 8 * 3 * 2^-24 < 2^-19,
+    which a rounding of p to 16 bits (half a step: 2^-11, 2^-8) takes back to 1, and which stays in dV in fp32."""
+    b = Batch([1] * 70, 3, 3, 48, dtype, seed=4)
+    got = b.check(f"{dtype} single")
+    assert torch.equal(got["out"], b.V) and float(got["lse"].abs().max()) < 8
+    if dtype == torch.float32:
+        assert bool(((got["dV"] - b.dO).abs() <= 2.0 ** -19 * b.dO.abs()).all())
+    else:
+        assert torch.equal(got["dV"], b.dO)
+    assert bool((got["dQ"] == 0).all()) and bool((got["dK"] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_of_no_graph_stay(dtype):
+    for qlens in (None, [2, 1, 0]):
+        Batch([40, 0, 70], 2, 1, 32, dtype, qlens=qlens, before=3, behind=9, seed=1).check(f"{dtype} rows outside")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_masks_that_leave_nothing_and_what_they_hide(dtype):
+    """Masked keys may hold NaN and infinities; graphs without a key give zeros, lse -inf and no gradients."""
+    b = Batch([50, 64, 3, 200], 2, 1, 64, dtype, masked=0.5, seed=2)
+    b.mask[:50] = 0
+    b.mask[50:114] = 0
+    b.mask[113] = 1
+    hidden = b.mask == 0
+    got = b.check(f"{dtype} masks")
+    for t, bad in ((b.K, float("nan")), (b.V, float("inf"))):
+        t[hidden] = torch.where(torch.arange(t.shape[1], device="cuda") % 3 == 0, bad, -1e4).to(dtype)
+    again = b.run()
+    for key in got:
+        assert torch.equal(got[key], again[key]), key
+    assert bool((got["out"][:50] == 0).all()) and bool((got["dQ"][:50] == 0).all()) and bool((got["dK"][hidden] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_scores(dtype):
+    """Scores of hundreds: one key has all the weight, no exponential overflows."""
+    Batch([90, 33], 2, 2, 64, dtype, seed=3, spread=6.0).check(f"{dtype} large scores")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_nan_stays_in_its_graph(dtype):
+    b = Batch([40, 130, 9], 2, 2, 32, dtype, seed=5)
+    clean = b.run()
+    b.K[60, 3] = float("nan")
+    got = b.run()
+    other = torch.ones(179, dtype=torch.bool, device="cuda")
+    other[40:170] = False
+    for key in got:
+        assert torch.equal(got[key][other], clean[key][other]), key
+    assert bool(got["out"][40:170, :32].isnan().all()) and bool(got["dV"][40:170, :32].isnan().all())
+
+
+def test_gradient_against_differences():
+    """Central differences of <out, dO> in fp32 along random directions.  h = 2^-8: off by the third derivative (a softmax of scores up to
+    about 4 in 24 dimensions: below 60 times the direction's length cubed) times h^2 / 6, and by the rounding of out over h."""
+    b = Batch([40, 9], 2, 1, 24, torch.float32, masked=0.2, seed=6)
+    got = b.run()
+    f = lambda: float((B.ftc_graph_attention(*b.args(), **b.kw()).double() * b.dO.double()).sum())
+    h = 2.0 ** -8
+    for t, name in ((b.Q, "dQ"), (b.K, "dK"), (b.V, "dV")):
+        gen = torch.Generator().manual_seed(1)
+        d = torch.randn(t.shape, generator=gen).cuda()
+        d /= d.norm()
+        keep = t.clone()
+        t.copy_(keep + h * d)
+        up = f()
+        t.copy_(keep - h * d)
+        down = f()
+        t.copy_(keep)
+        want = float((got[name].double() * d.double()).sum())
+        size = float(b.dO.double().norm())
+        assert abs((up - down) / (2 * h) - want) <= size * (60 * h * h / 6 + 64 * 2.0 ** -24 * 4 / h), name
+
+
+def test_longer_graphs_than_a_part():
+    """Split over the keys (one query) and over the queries (one key): more keys than 64 parts hold in one tile each."""
+    for dtype in DTYPES:
+        Batch([9000], 1, 1, 16, dtype, qlens=[2], masked=0.05, seed=8).check(f"{dtype} 9000 keys")
+        Batch([2], 1, 1, 16, dtype, qlens=[9000], seed=9).check(f"{dtype} 9000 queries")
+
+
+def test_offsets_beyond_32_bits():
+    """Rows that begin behind 2^31 elements."""
+    ld, D = (1 << 30) + 8, 32
+    whole = torch.empty(3 * ld + D, dtype=torch.float16, device="cuda")
+    gen = torch.Generator().manual_seed(0)
+    t = [whole[i * 64:].as_strided((3, D), (ld, 1)) for i in range(3)]
+    small = [torch.randn((3, D), generator=gen).half().cuda() for _ in range(3)]
+    for a, b in zip(t, small):
+        a.copy_(b)
+    ptr = offsets([3])
+    out = whole[256:].as_strided((3, D), (ld, 1))
+    B.ftc_graph_attention(*t, ptr, ptr, heads=1, out=out)
+    assert torch.equal(out, B.ftc_graph_attention(*small, ptr, ptr, heads=1))
+
+
+def test_captured_and_on_another_stream():
+    b = Batch([200, 0, 90, 33], 4, 2, 64, torch.float16, masked=0.1, seed=7)
+    L = B.lib()
+    sizes = (b.n_q, b.n_kv, 4, 4, 2, 64)
+    ws = B._workspace(max(L.ftc_graph_attention_workspace_bytes(*sizes), L.ftc_graph_attention_backward_workspace_bytes(*sizes)), "cuda")
+    new = lambda t: torch.empty_like(t, memory_format=torch.contiguous_format)
+    out, lse, dQ, dK, dV = new(b.Q), torch.empty((b.n_q, 4), device="cuda"), new(b.Q), new(b.K), new(b.V)
+
+    def both():
+        B.ftc_graph_attention(*b.args(), out=out, lse=lse, ws=ws, **b.kw())
+        B.ftc_graph_attention_backward(*b.args(), out, lse, b.dO, dQ=dQ, dK=dK, dV=dV, ws=ws, **b.kw())
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    side.synchronize()
+    want = [t.clone() for t in (out, lse, dQ, dK, dV)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        for t in (out, lse, dQ, dK, dV):
+            t.fill_(float("nan"))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((out, lse, dQ, dK, dV), want))
+        b.Q.float().sum().item()
+    b.mask.fill_(1)      # new inputs in place
+    graph.replay()
+    torch.cuda.synchronize()
+    got = b.run()
+    assert torch.equal(out, got["out"]) and torch.equal(dK, got["dK"])
