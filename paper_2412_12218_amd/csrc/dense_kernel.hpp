@@ -1,0 +1,367 @@
+// The product kernel of the dense layer and its gradients (linear.hip): C = A B with an epilogue, in tiles of the result.
+//
+// A workgroup has a tile; its waves, RW x CW of them, WM x WN blocks of 32 x 32 each (matrix_frag.hpp).  An operand whose memory rows run along the
+// contraction is a tile of rows read along rows, one whose memory rows run across it (AX, BX) is read along columns, so nothing is
+// transposed in memory.  Steps of 128 bytes of the contraction go from memory to one of two LDS buffers while the other is
+// multiplied.
+//   whole pieces (FAST)  rows and widths of whole 16-byte pieces at 16-byte alignment: global_load_lds, no registers on the way.  An instruction
+//                        fills 64 consecutive pieces of LDS, so the lanes fetch the pieces that the swizzle puts there.  Rows and columns behind the
+//                        result's ends are those at the end once more: what they give is not stored.
+//   else                 through registers, element by element at the ends.
+// The indices that a last step lacks are zeros in both operands.
+//
+// Results go through LDS once more, so that neighbouring lanes have neighbouring columns: bias, activation, residual and the store work on
+// eight numbers of a row.
+#pragma once
+#include "matrix_frag.hpp"
+
+namespace ftc {
+
+struct DenseArgs {
+    const void *A, *B;  // M x K, K x N
+    int64_t lda, ldb;
+    int M, N, K, splits, k_each;
+    float *part;  // splits x M x N
+    const void *bias, *residual;
+    void *slope, *out;
+    int64_t ldr, lds, ldo;
+    int act, out_dtype;
+};
+
+// Tiles of the result.
+enum { DENSE_64 = 0, DENSE_128 = 1, DENSE_256 = 2 };
+constexpr int dense_side(int tile) { return 64 << tile; }
+
+// One launch for each place of the operands' rows: Z (A along, B across), dX (both along), dW (both across).
+template <bool AX, bool BX>
+void launch_dense(const DenseArgs &a, int dtype, int tile, hipStream_t s);
+
+// Rows of whole 16-byte pieces at 16-byte alignment, 256 of them within 2^32 bytes.
+inline bool dense_whole_pieces(const void *p, int64_t ld, int width, int dtype)
+{
+    const int e = elem_size(dtype);
+    return aligned16(p) && ld * e % 16 == 0 && static_cast<int64_t>(width) * e % 16 == 0 && ld * e < (1 << 24);
+}
+
+#if defined(__HIPCC__)
+constexpr int SLOPE_BITS = 14;
+
+// act(p) and act'(p).  Infinite p: the limits.  For fp32 from the functions of the device library; for 16-bit results, which have 11 bits, from
+// one exponential and one reciprocal: Phi(-|p|) = exp(-p^2 / 2) (a1 t + .. + a5 t^5) / 2 with t = 1 / (1 + 0.3275911 |p| / sqrt 2), off by at most
+// 0.75e-7 (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26), and sigma(p) = 1 / (1 + exp(-p)).
+template <class T>
+__device__ __forceinline__ float activation(float p, int act, float &slope)
+{
+    slope = 1.f;
+    if (act == FTC_ACT_RELU) {
+        slope = p > 0.f ? 1.f : p != p ? p : 0.f;
+        return p > 0.f ? p : p != p ? p : 0.f;
+    }
+    if (act == FTC_ACT_GELU) {
+        const float q = p < -40.f ? -40.f : p > 40.f ? 40.f : p;
+        float cdf, density;
+        if constexpr (T::BYTES == 4) {
+            cdf = 0.5f * (1.f + erff(q * 0.70710678118654752f));
+            density = 0.39894228040143268f * expf(-0.5f * q * q);
+        } else {
+            const float e = __builtin_amdgcn_exp2f(q * q * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(fmaf(fabsf(q), 0.23164188f, 1.f));
+            const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+            cdf = q < 0.f ? tail : 1.f - tail;
+            density = 0.39894228040143268f * e;
+        }
+        slope = fmaf(q, density, cdf);
+        return p > 40.f ? p : q * cdf;
+    }
+    if (act == FTC_ACT_SILU) {
+        const float q = p < -80.f ? -80.f : p > 80.f ? 80.f : p;
+        float g;
+        if constexpr (T::BYTES == 4) g = 1.f / (1.f + expf(-q));
+        else g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(q * -1.4426950408889634f));
+        slope = g * fmaf(q, 1.f - g, 1.f);
+        return p > 80.f ? p : p < -80.f ? 0.f : q * g;
+    }
+    return p;
+}
+
+__device__ __forceinline__ int16_t slope_code(float s)
+{
+    return s != s ? INT16_MIN : static_cast<int16_t>(rintf(s * (1 << SLOPE_BITS)));
+}
+__device__ __forceinline__ float slope_value(int16_t c)
+{
+    return c == INT16_MIN ? __builtin_nanf("") : c * (1.f / (1 << SLOPE_BITS));
+}
+
+// Eight neighbouring numbers of a row of the result, `left` of them inside it; bias: theirs.
+template <class T>
+__device__ __forceinline__ void epilogue(const DenseArgs &a, int row, int col, int left, const float (&bias)[8], float (&x)[8])
+{
+    float slope[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] += bias[j];
+    if (a.act != FTC_ACT_NONE || a.slope) {  // uniform
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = activation<T>(x[j], a.act, slope[j]);
+    }
+    if (a.residual) {
+        float add[8];
+        load_eight_numbers<T>(a.residual, row * a.ldr + col, left, add);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] += add[j];
+    }
+    if (a.slope) {
+        if constexpr (T::BYTES == 4) {
+            store_eight_numbers(a.slope, row * a.lds + col, FTC_F32, left, slope);
+        } else {
+            int16_t *to = static_cast<int16_t *>(a.slope) + row * a.lds + col;
+            typedef int16_t s8 __attribute__((ext_vector_type(8), aligned(2)));
+            s8 code;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) code[j] = slope_code(slope[j]);
+            if (left >= 8) {
+                *reinterpret_cast<s8 *>(to) = code;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
+                    if (j < left) to[j] = code[j];
+            }
+        }
+    }
+    store_eight_numbers(a.out, row * a.ldo + col, a.out_dtype, left, x);
+}
+
+// One operand's tile: SIDE rows of the result's side and STEP of the contraction, staged by WAVES waves.
+template <class T, int SIDE, int STEP, bool ACROSS, int WAVES>
+struct Operand {
+    static constexpr int ROWS = ACROSS ? STEP : SIDE, COLS = ACROSS ? SIDE : STEP;
+    typedef LdsTile<T, COLS> L;
+    static constexpr int BYTES = ROWS * L::ROW, EACH = BYTES / (WAVES * 64 * 16);
+    static_assert(BYTES % (WAVES * 64 * 16) == 0, "whole pieces a thread");
+
+    // ---- straight to LDS: piece number e * threads + thread of the tile, as it lies there
+    const char *base;    // the step's first number
+    uint32_t off[EACH];  // this lane's pieces from there, in bytes (dense_whole_pieces: below 2^32)
+    __device__ __forceinline__ void aim(const void *p, int64_t ld, int side0, int side, int k0)
+    {
+        base = static_cast<const char *>(p) + (ACROSS ? k0 * ld + side0 : side0 * ld + k0) * T::BYTES;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x), r = id / L::PIECES, c = ((id % L::PIECES) ^ L::swizzle(r)) * T::VEC;
+            const uint32_t row = ACROSS ? r : min(r, side - 1 - side0), col = ACROSS ? min(c, side - T::VEC - side0) : c;
+            off[e] = (row * static_cast<uint32_t>(ld) + col) * T::BYTES;
+        }
+    }
+    // `step`: bytes to the next step
+    __device__ __forceinline__ void fetch(char *tile, int64_t step)
+    {
+        typedef __attribute__((address_space(3))) void *lds_ptr;
+        typedef const __attribute__((address_space(1))) void *global_ptr;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            __builtin_amdgcn_global_load_lds((global_ptr)(base + off[e]), (lds_ptr)(tile + (e * WAVES + wave) * 1024), 16, 0, 0);
+        base += step;
+    }
+    // the same where indices from `left` on are to be zeros
+    __device__ __forceinline__ void fetch_last(char *tile, int left) const
+    {
+        ftc_u32x4 w[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x), r = id / L::PIECES, c = ((id % L::PIECES) ^ L::swizzle(r)) * T::VEC;
+            w[e] = ftc_u32x4{0u, 0u, 0u, 0u};
+            if ((ACROSS ? r : c) < left) w[e] = *reinterpret_cast<const ftc_u32x4 *>(base + off[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) *reinterpret_cast<ftc_u32x4 *>(tile + (e * WAVES * 64 + static_cast<int>(threadIdx.x)) * 16) = w[e];
+    }
+
+    // ---- through registers; `side`, `k_end`: where zeros begin
+    ftc_u32x4 v[EACH];
+    __device__ __forceinline__ void load(const void *base, int64_t ld, int side0, int side, int k0, int k_end)
+    {
+        const int row0 = ACROSS ? k0 : side0, rows = ACROSS ? k_end : side, col0 = ACROSS ? side0 : k0, cols = ACROSS ? side : k_end;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x), r = row0 + id / L::PIECES, c = col0 + id % L::PIECES * T::VEC;
+            v[e] = load_piece<T>(base, r * ld + c, r < rows ? cols - c : 0);
+        }
+    }
+    __device__ __forceinline__ void store(char *tile) const
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x);
+            L::store(tile, id / L::PIECES, id % L::PIECES, v[e]);
+        }
+    }
+
+    // the 32 from side0 on, indices 16 s .. of the step
+    static __device__ __forceinline__ Frag<T> frag(const char *tile, int side0, int s, int lane)
+    {
+        const int half = lane >> 5;
+        if constexpr (ACROSS) return L::along_column(tile + 16 * s * L::ROW, 8 * half, 8 * half + 4, side0);
+        else return L::along_row(tile + side0 * L::ROW, lane & 31, 2 * s + half);
+    }
+};
+
+// Which tile a workgroup has.  Workgroups go round the eight XCDs, each of which has an L2: every XCD gets a range of consecutive
+// tiles (the rest keep their place), in the order of bands of eight tile rows, column by column inside a band, so that the tiles at
+// work in an XCD share rows of A and columns of B.
+__device__ __forceinline__ void dense_tile(int id, int tiles_m, int tiles_n, int &m, int &n)
+{
+    const int each = tiles_m * tiles_n / 8;
+    if (id < each * 8) id = (id % 8) * each + id / 8;
+    constexpr int BAND = 8;
+    const int band = id / (BAND * tiles_n), in = id % (BAND * tiles_n), rows = min(BAND, tiles_m - band * BAND);
+    m = band * BAND + in % rows;
+    n = in / rows;
+}
+
+template <class T, bool AX, bool BX, bool FAST, int RW, int CW, int WM, int WN>
+__global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
+{
+    constexpr int WAVES = RW * CW, TM = 32 * WM * RW, TN = 32 * WN * CW, STEP = 128 / T::BYTES, KS = STEP / 16;
+    typedef Operand<T, TM, STEP, AX, WAVES> OA;
+    typedef Operand<T, TN, STEP, BX, WAVES> OB;
+    // arrays of their own: the compiler sees that reads of one buffer need not wait for the loads into the other
+    __shared__ __align__(16) char A0[OA::BYTES], B0[OB::BYTES], A1[OA::BYTES], B1[OB::BYTES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int tm, tn;
+    dense_tile(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
+    const int m0 = tm * TM, n0 = tn * TN, wm = wave / CW * 32 * WM, wn = wave % CW * 32 * WN;
+    const int k_begin = static_cast<int>(blockIdx.y) * a.k_each, k_end = min(a.K, k_begin + a.k_each);
+    f32x16 c[WM][WN];
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int j = 0; j < WN; ++j) c[i][j] = zero16();
+    // operands of the next 16 indices are read while these are multiplied, and not earlier: registers
+    auto multiply = [&](const char *A, const char *B) {
+        Frag<T> fa[2][WM], fb[2][WN];
+        auto read = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < WM; ++i) fa[s & 1][i] = OA::frag(A, wm + 32 * i, s, lane);
+#pragma unroll
+            for (int j = 0; j < WN; ++j) fb[s & 1][j] = OB::frag(B, wn + 32 * j, s, lane);
+        };
+        read(0);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if (s + 1 < KS) read(s + 1);
+#pragma unroll
+            for (int i = 0; i < WM; ++i)
+#pragma unroll
+                for (int j = 0; j < WN; ++j) mma<T>(c[i][j], fb[s & 1][j], fa[s & 1][i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    OA oa;
+    OB ob;
+    if constexpr (FAST) {
+        const int64_t da = (AX ? STEP * a.lda : STEP) * T::BYTES, db = (BX ? STEP * a.ldb : STEP) * T::BYTES;
+        const int whole = (k_end - k_begin) / STEP, left = (k_end - k_begin) % STEP;
+        oa.aim(a.A, a.lda, m0, a.M, k_begin);
+        ob.aim(a.B, a.ldb, n0, a.N, k_begin);
+        if (whole > 0) {
+            oa.fetch(A0, da);
+            ob.fetch(B0, db);
+        }
+        __syncthreads();
+        for (int k = 1; k < whole; k += 2) {
+            oa.fetch(A1, da);
+            ob.fetch(B1, db);
+            multiply(A0, B0);
+            __syncthreads();
+            if (k + 1 < whole) {
+                oa.fetch(A0, da);
+                ob.fetch(B0, db);
+            }
+            multiply(A1, B1);
+            __syncthreads();
+        }
+        if (left > 0) {
+            oa.fetch_last(A1, left);
+            ob.fetch_last(B1, left);
+        }
+        if (whole & 1) multiply(A0, B0);
+        __syncthreads();
+        if (left > 0) {
+            multiply(A1, B1);
+            __syncthreads();
+        }
+    } else {
+        auto load = [&](int k) {
+            oa.load(a.A, a.lda, m0, a.M, k, k_end);
+            ob.load(a.B, a.ldb, n0, a.N, k, k_end);
+        };
+        load(k_begin);
+        for (int k = k_begin; k < k_end; k += STEP) {
+            oa.store(A0);
+            ob.store(B0);
+            __syncthreads();
+            if (k + STEP < k_end) load(k + STEP);
+            multiply(A0, B0);
+            __syncthreads();
+        }
+    }
+    // A wave's 32 rows through LDS, where no other wave looks any more: neighbouring lanes then have neighbouring columns.
+    constexpr int WIDTH = 32 * WN, PITCH = WIDTH * 4 + 16, EIGHTS = WIDTH / 8;
+    static_assert((WAVES / 4) * 32 * PITCH <= OA::BYTES && (WAVES / 4) * 32 * PITCH <= OB::BYTES, "a place for every wave");
+    char *area = ((wave & 3) == 0 ? A0 : (wave & 3) == 1 ? B0 : (wave & 3) == 2 ? A1 : B1) + (wave >> 2) * 32 * PITCH;
+    const int q = lane % EIGHTS, col = n0 + wn + 8 * q, left = a.N - col;
+    float bias[8];
+    load_eight_numbers<T>(a.bias, col, a.bias && a.splits == 1 ? left : 0, bias);
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int j = 0; j < WN; ++j)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<ftc_f32x4 *>(area + (lane & 31) * PITCH + (32 * j + 8 * b + 4 * (lane >> 5)) * 4) =
+                    ftc_f32x4{c[i][j][4 * b], c[i][j][4 * b + 1], c[i][j][4 * b + 2], c[i][j][4 * b + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 2
+        for (int r = lane / EIGHTS; r < 32; r += 64 / EIGHTS) {
+            const int row = m0 + wm + 32 * i + r;
+            if (row >= a.M || left <= 0) break;
+            const ftc_f32x4 u = *reinterpret_cast<const ftc_f32x4 *>(area + r * PITCH + 32 * q), v = *reinterpret_cast<const ftc_f32x4 *>(area + r * PITCH + 32 * q + 16);
+            float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+            if (a.splits > 1) store_eight_numbers(a.part, (static_cast<int64_t>(blockIdx.y) * a.M + row) * a.N + col, FTC_F32, left, x);
+            else epilogue<T>(a, row, col, left, bias, x);
+        }
+    }
+}
+
+template <class T, bool AX, bool BX, bool FAST>
+void launch_dense_t(const DenseArgs &a, int tile, hipStream_t s)
+{
+    const int side = dense_side(tile);
+    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(ceil_div(a.M, side)) * ceil_div(a.N, side)), a.splits);
+    if (tile == DENSE_64) {
+        hipLaunchKernelGGL((dense_kernel<T, AX, BX, FAST, 2, 2, 1, 1>), grid, dim3(256), 0, s, a);
+    } else if (tile == DENSE_128) {
+        hipLaunchKernelGGL((dense_kernel<T, AX, BX, FAST, 2, 2, 2, 2>), grid, dim3(256), 0, s, a);
+    } else if constexpr (FAST && T::BYTES == 2) {
+        hipLaunchKernelGGL((dense_kernel<T, AX, BX, FAST, 2, 4, 4, 2>), grid, dim3(512), 0, s, a);
+    }
+}
+
+template <bool AX, bool BX>
+void launch_dense(const DenseArgs &a, int dtype, int tile, hipStream_t s)
+{
+    const bool fast = dense_whole_pieces(a.A, a.lda, AX ? a.M : a.K, dtype) && dense_whole_pieces(a.B, a.ldb, BX ? a.N : a.K, dtype);
+#define FTC_DENSE(T)                                                  \
+    do {                                                             \
+        if (fast) launch_dense_t<T, AX, BX, true>(a, tile, s);        \
+        else launch_dense_t<T, AX, BX, false>(a, tile, s);            \
+    } while (0)
+    if (dtype == FTC_F32) FTC_DENSE(F32);
+    else if (dtype == FTC_F16) FTC_DENSE(F16);
+    else FTC_DENSE(BF16);
+#undef FTC_DENSE
+}
+
+#endif  // __HIPCC__
+}  // namespace ftc

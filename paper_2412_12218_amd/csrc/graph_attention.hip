@@ -174,7 +174,7 @@ __global__ __launch_bounds__(64 * NW, (attn_occupancy<T, DP, NW>())) void attent
         for (int u = 0; u < SUB; ++u) {
             s[u] = zero16();
 #pragma unroll
-            for (int k = 0; k < KS; ++k) mma<T>(s[u], L::along_row(Ks, 32 * u + col, 2 * k + half), q[k]);
+            for (int k = 0; k < KS; ++k) mma<T>(s[u], L::along_row(Ks + 32 * u * L::ROW, col, 2 * k + half), q[k]);
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const ftc_f32x4 w = *reinterpret_cast<const ftc_f32x4 *>(&bias[32 * u + 8 * b + 4 * half]);
@@ -203,9 +203,9 @@ __global__ __launch_bounds__(64 * NW, (attn_occupancy<T, DP, NW>())) void attent
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const Frag<T> p = operand_of<T>(s[u], k);
-                const int r0 = 32 * u + 16 * k + 4 * half;
+                const int r0 = (32 * u + 16 * k) * L::ROW;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) mma<T>(o[d], L::along_column(Vs, r0, r0 + 8, 32 * d), p);
+                for (int d = 0; d < DT; ++d) mma<T>(o[d], L::along_column(Vs + r0, 4 * half, 4 * half + 8, 32 * d), p);
             }
         }
     }
@@ -361,8 +361,8 @@ __global__ __launch_bounds__(64 * NW, (attn_occupancy<T, DP, NW>())) void attent
             dp[u] = zero16();
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                mma<T>(p[u], L::along_row(Ks, 32 * u + col, 2 * k + half), q[k]);
-                mma<T>(dp[u], L::along_row(Vs, 32 * u + col, 2 * k + half), g[k]);
+                mma<T>(p[u], L::along_row(Ks + 32 * u * L::ROW, col, 2 * k + half), q[k]);
+                mma<T>(dp[u], L::along_row(Vs + 32 * u * L::ROW, col, 2 * k + half), g[k]);
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -394,9 +394,9 @@ __global__ __launch_bounds__(64 * NW, (attn_occupancy<T, DP, NW>())) void attent
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const Frag<T> ds = operand_of<T>(p[u], k);
-                const int r0 = 32 * u + 16 * k + 4 * half;
+                const int r0 = (32 * u + 16 * k) * L::ROW;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) mma<T>(dq[d], L::along_column(Ks, r0, r0 + 8, 32 * d), ds);
+                for (int d = 0; d < DT; ++d) mma<T>(dq[d], L::along_column(Ks + r0, 4 * half, 4 * half + 8, 32 * d), ds);
             }
         }
     }
@@ -484,8 +484,8 @@ __global__ __launch_bounds__(64 * NW, (attn_occupancy<T, DP, NW>())) void attent
             f32x16 p = zero16(), ds = zero16();
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                mma<T>(p, L::along_row(Qs, 32 * u + col, 2 * s + half), k[s]);
-                mma<T>(ds, L::along_row(Gs, 32 * u + col, 2 * s + half), v[s]);
+                mma<T>(p, L::along_row(Qs + 32 * u * L::ROW, col, 2 * s + half), k[s]);
+                mma<T>(ds, L::along_row(Gs + 32 * u * L::ROW, col, 2 * s + half), v[s]);
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -500,11 +500,11 @@ __global__ __launch_bounds__(64 * NW, (attn_occupancy<T, DP, NW>())) void attent
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const Frag<T> pf = operand_of<T>(p, s), df = operand_of<T>(ds, s);
-                const int r0 = 32 * u + 16 * s + 4 * half;
+                const int r0 = (32 * u + 16 * s) * L::ROW;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    mma<T>(dv[d], L::along_column(Gs, r0, r0 + 8, 32 * d), pf);
-                    mma<T>(dk[d], L::along_column(Qs, r0, r0 + 8, 32 * d), df);
+                    mma<T>(dv[d], L::along_column(Gs + r0, 4 * half, 4 * half + 8, 32 * d), pf);
+                    mma<T>(dk[d], L::along_column(Qs + r0, 4 * half, 4 * half + 8, 32 * d), df);
                 }
             }
         }

@@ -110,6 +110,36 @@ __device__ __forceinline__ Frag<T> load_frag(const void *base, int64_t idx, int 
     return a;
 }
 
+// Eight consecutive numbers at element `idx`, aligned to an element; those from `left` on are zero and not read.
+template <class T>
+__device__ __forceinline__ void load_eight_numbers(const void *base, int64_t idx, int left, float (&x)[8])
+{
+    const Frag<T> a = load_frag<T>(base, idx, left);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (T::BYTES == 4) x[j] = a.f[j];
+        else if constexpr (std::is_same<T, F16>::value) x[j] = f16_bits_to_f32((a.w[j / 2] >> (16 * (j & 1))) & 0xffffu);
+        else x[j] = bf16_bits_to_f32((a.w[j / 2] >> (16 * (j & 1))) & 0xffffu);
+    }
+}
+// ... in a run-time type; those from `left` on are not written
+__device__ __forceinline__ void store_eight_numbers(void *base, int64_t idx, int dtype, int left, const float (&x)[8])
+{
+    if (left >= 8) {
+        if (dtype == FTC_F32) {
+            store_vec_any<8>(base, idx, dtype, x);
+        } else {
+            typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+            const ftc_u32x4 w = dtype == FTC_F16 ? frag_of<F16>(x).w : frag_of<BF16>(x).w;
+            *reinterpret_cast<u4 *>(static_cast<uint16_t *>(base) + idx) = u4{w[0], w[1], w[2], w[3]};
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < left) store_elem(base, idx + j, dtype, x[j]);
+    }
+}
+
 // Four consecutive numbers at element `idx`, aligned to an element; those from `left` on are not written.
 template <class T>
 __device__ __forceinline__ void store_four(void *base, int64_t idx, int left, const float (&x)[4])
@@ -126,7 +156,9 @@ __device__ __forceinline__ void store_four(void *base, int64_t idx, int left, co
 
 // ---- tiles in LDS -------------------------------------------------------------------------------------------
 // Rows of COLS elements, 16-byte pieces permuted inside a row by its number: the 16 rows that a read along rows touches at
-// once, and the four rows by 64 bytes of a read along columns, each fall on the 64 banks without conflict.
+// once, and the four rows by 64 bytes of a read along columns, each fall on the 64 banks without conflict.  The permutation repeats
+// every 16 rows, so reads take the place of such a row as `tile` and rows from there: what remains of an address is the lane's, and the
+// same for all of them.
 template <class T, int COLS>
 struct LdsTile {
     static constexpr int ROW = COLS * T::BYTES, PIECES = ROW / 16;
