@@ -121,33 +121,58 @@ struct DensePlan {
 
 static int64_t dense_tiles(int M, int N, int tile) { return static_cast<int64_t>(ceil_div(M, dense_side(tile))) * ceil_div(N, dense_side(tile)); }
 
-// The largest tile that gives every compute unit one; else the small one, and parts of the contraction of 128 indices at least
-// until there are two workgroups a compute unit.  large: the 256 x 256 tile can be taken.
-static DensePlan dense_plan(int M, int N, int K, bool large)
+// Tile and parts of the contraction by an estimate of the time.  A step (128 bytes of the contraction) of a workgroup takes `alone` where it
+// has a compute unit to itself and `shared` for each of the workgroups of one that is full, `most` of them; parts cost the second kernel, and
+// writing and reading them once.  us, from products of 8192^3 (1780 with tiles of 64 / 1080 of 128 / 900 of 256), 4096 x 1024 x 1024 (16 / 15 / 31
+// for Z, 22 / 25 / 30 for dW at the best number of parts), 20 000 x 768 x 768 (40 / 34 / 30, 52 / 49 / 50) and 65 536 x 1024 x 4096
+// (852 / 652 / 582, 1000 / 596 / 485), the last two with parts of up to 16 tried: more lose (4096 x 1024 x 1024, dW of 2 / 4 / 8 / 16 parts: 28 / 25 / 27 / 39).
+struct DenseCost {
+    float alone, shared;
+    int most;
+};
+static DensePlan dense_plan(int M, int N, int K, bool f32, bool large)
 {
-    DensePlan p = {DENSE_64, 1, 64};
-    if (M < 1 || N < 1) return p;
-    p.tile = large && dense_tiles(M, N, DENSE_256) >= 256 ? DENSE_256 : dense_tiles(M, N, DENSE_128) >= 256 ? DENSE_128 : DENSE_64;
-    const int64_t tiles = dense_tiles(M, N, p.tile);
-    int64_t s = tiles >= 512 || p.tile != DENSE_64 ? 1 : (512 + tiles - 1) / tiles;
-    const int most = K > 128 ? ceil_div(K, 128) : 1;
-    if (s > most) s = most;
-    if (s > 64) s = 64;
-    p.k_each = static_cast<int>(align_up(K > 0 ? ceil_div(K, static_cast<int>(s)) : 1, 64));
-    p.splits = K > 0 ? ceil_div(K, p.k_each) : 1;
-    return p;
+    static constexpr DenseCost cost[2][3] = {{{0.45f, 0.22f, 5}, {0.79f, 0.53f, 2}, {1.74f, 1.74f, 1}}, {{0.55f, 0.44f, 4}, {1.75f, 1.75f, 2}, {0.f, 0.f, 0}}};
+    constexpr float JOIN_US = 5.f, PART_BYTES_US = 4e6f;
+    DensePlan best = {DENSE_64, 1, 64};
+    if (M < 1 || N < 1 || K < 1) return best;
+    float least = INFINITY;
+    const int step = f32 ? 32 : 64;
+    for (int tile = DENSE_64; tile <= (large && !f32 ? DENSE_256 : DENSE_128); ++tile) {
+        const DenseCost &c = cost[f32][tile];
+        const int64_t tiles = dense_tiles(M, N, tile);
+        for (int want = 1; want <= 64; want = want < 8 ? want + 1 : want + want / 4) {
+            DensePlan p = {tile, 1, static_cast<int>(align_up(ceil_div(K, want), 64))};
+            p.splits = ceil_div(K, p.k_each);
+            if (p.splits != want) continue;
+            const int64_t groups = tiles * p.splits, room = 256ll * c.most, full = groups / room, rest = groups % room;
+            const auto each = [&](int64_t n) { return n * c.shared > c.alone ? n * c.shared : c.alone; };
+            float us = ceil_div(p.k_each, step) * (full * each(c.most) + (rest ? each((rest + 255) / 256) : 0.f));
+            if (p.splits > 1) us += JOIN_US + 8.f * p.splits * M * N / PART_BYTES_US;
+            if (us < least) {
+                least = us;
+                best = p;
+            }
+            if (tiles * want >= 2048) break;  // more workgroups than the chip holds
+        }
+    }
+    return best;
 }
 static size_t dense_ws(int M, int N, int K)
 {
-    const DensePlan p = dense_plan(M, N, K, false);
-    return p.splits > 1 ? align_up(static_cast<size_t>(p.splits) * M * N * sizeof(float), 256) : 0;
+    int most = 1;
+    for (int v = 0; v < 3; ++v) {
+        const DensePlan p = dense_plan(M, N, K, v == 0, v == 2);
+        if (p.splits > most) most = p.splits;
+    }
+    return most > 1 ? align_up(static_cast<size_t>(most) * M * N * sizeof(float), 256) : 0;
 }
 
 template <bool AX, bool BX>
 static void dense(DenseArgs a, int dtype, void *ws, hipStream_t s)
 {
     const bool fast = dense_whole_pieces(a.A, a.lda, AX ? a.M : a.K, dtype) && dense_whole_pieces(a.B, a.ldb, BX ? a.N : a.K, dtype);
-    const DensePlan p = dense_plan(a.M, a.N, a.K, fast && dtype != FTC_F32);
+    const DensePlan p = dense_plan(a.M, a.N, a.K, dtype == FTC_F32, fast);
     a.splits = p.splits;
     a.k_each = p.k_each;
     a.part = static_cast<float *>(ws);
