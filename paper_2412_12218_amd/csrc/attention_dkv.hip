@@ -1,0 +1,188 @@
+// Attention between all nodes of a graph: the kernel of dK and dV.  See attention_common.hpp.
+//
+// A wave has 32 keys, their K and V in registers, and walks over the virtual rows of their graph's queries.
+#include "attention_common.hpp"
+
+namespace ftc {
+
+template <class T, int DP>
+constexpr int query_rows() { return T::BYTES == 2 ? 64 : 32; }
+
+template <class T, int DP, int NW, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
+{
+    constexpr int TK = 32 * NW, TQ = query_rows<T, DP>(), SUB = TQ / 32, KS = DP / 16, DT = DP / 32;
+    typedef LdsTile<T, DP> L;
+    typedef Rows<T, DP, TQ, 64 * NW, WHOLE> R;
+    __shared__ __align__(16) char Qs[2][R::BYTES], Gs[2][R::BYTES];
+    __shared__ __align__(16) float lses[2][TQ], deltas[2][TQ];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const Place here = place_of(a);
+    const Tile tile = find_tile(a.kv_ptr, a.graphs, a.n_kv, 1, TK, here.tile);
+    if (tile.graph < 0) return;
+    const int k0 = clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
+    if (k1 <= k0 || static_cast<int64_t>(tile.index) * TK >= k1 - k0) return;
+    const int q0 = clamped(a.q_ptr, tile.graph, a.n_q), q1 = clamped(a.q_ptr, tile.graph + 1, a.n_q);
+    const int rows = max(q1 - q0, 0) * a.group, tiles = (rows + TQ - 1) / TQ;
+    const int each = (tiles + a.splits - 1) / a.splits, first = here.part * each, last = min(tiles, first + each);
+
+    const int key = k0 + tile.index * TK + wave * 32 + col;
+    const bool there = key < k1, seen = there && (!a.mask || a.mask[key]);
+    R qs, gs;
+    float my_lse, my_delta;
+    auto get = [&](int t, char *Q, char *G) {
+        if (t >= last) return;
+        // rows from the query of the tile's first virtual row on
+        int q_first, h_first;
+        split_row(a, t * TQ, q_first, h_first);
+        q_first = __builtin_amdgcn_readfirstlane(q_first);
+        const char *qp = head_of<T>(a.Q, q0 + q_first, a.ldq, here.share * a.group * a.D), *gp = head_of<T>(a.dO, q0 + q_first, a.lddo, here.share * a.group * a.D);
+        const typename R::Offset ldq = a.ldq, ldg = a.lddo;
+        const bool full = (t + 1) * TQ <= rows;
+#pragma unroll
+        for (int e = 0; e < R::EACH; ++e) {
+            uint32_t q = R::row(e), c = R::col(e);
+            if (a.group > 1) {
+                int query, head;
+                split_row(a, t * TQ + R::row(e), query, head);
+                q = query - q_first;
+                c += head * a.D;
+            }
+            if (full || t * TQ + R::row(e) < rows) {
+                qs.get(Q, e, qp, q * ldq + c, a.D);
+                gs.get(G, e, gp, q * ldg + c, a.D);
+            } else {
+                qs.get_zeros(Q, e);
+                gs.get_zeros(G, e);
+            }
+        }
+        if (static_cast<int>(threadIdx.x) < TQ) {
+            const int r = t * TQ + threadIdx.x;
+            my_lse = -INFINITY;  // no probabilities behind the last row
+            my_delta = 0.f;
+            if (r < rows) {
+                int query, head;
+                split_row(a, r, query, head);
+                const int64_t at = static_cast<int64_t>(q0 + query) * a.heads + here.share * a.group + head;
+                const float lse = a.lse[at];
+                my_lse = lse == -INFINITY ? -INFINITY : -lse * LOG2E;
+                my_delta = a.delta[at];
+            }
+        }
+    };
+    auto put = [&](int t, char *Q, char *G, float *row_lse, float *row_delta) {
+        if (t < last) {
+            qs.put(Q);
+            gs.put(G);
+            if (static_cast<int>(threadIdx.x) < TQ) {
+                row_lse[threadIdx.x] = my_lse;
+                row_delta[threadIdx.x] = my_delta;
+            }
+        }
+        __syncthreads();
+    };
+    for (int b = 0; b < 2; ++b) {
+        R::clear(Qs[b], a.D);
+        R::clear(Gs[b], a.D);
+    }
+    if (WHOLE && a.D < DP) __syncthreads();
+    get(first, Qs[0], Gs[0]);
+    const char *k_row = head_of<T>(a.K, seen ? key : k0, a.ldk, here.share * a.D), *v_row = head_of<T>(a.V, seen ? key : k0, a.ldv, here.share * a.D);
+    Frag<T> k[KS], v[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        const int c = 16 * s + 8 * half;
+        k[s] = operand_at<T, WHOLE>(k_row, c, a.D, seen);
+        v[s] = operand_at<T, WHOLE>(v_row, c, a.D, seen);
+    }
+    const float scale2 = a.scale * LOG2E, bias = seen ? 0.f : -INFINITY;
+    f32x16 dk[DT], dv[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) { dk[d] = zero16(); dv[d] = zero16(); }
+
+    // products of 32 rows with the keys: <q, k> and <dO, v>
+    auto scores = [&](const char *Q, const char *G, int u, f32x16 &p, f32x16 &ds) {
+        p = zero16();
+        ds = zero16();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            mma<T>(p, L::along_row(Q + 32 * u * L::ROW, col, 2 * s + half), k[s]);
+            mma<T>(ds, L::along_row(G + 32 * u * L::ROW, col, 2 * s + half), v[s]);
+        }
+    };
+    // p and ds from them
+    auto weights = [&](const float *row_lse, const float *row_delta, int u, f32x16 &p, f32x16 &ds) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const ftc_f32x4 w = *reinterpret_cast<const ftc_f32x4 *>(&row_lse[32 * u + 8 * b + 4 * half]);
+            const ftc_f32x4 x = *reinterpret_cast<const ftc_f32x4 *>(&row_delta[32 * u + 8 * b + 4 * half]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(p[4 * b + i], scale2, w[i] + bias));
+                ds[4 * b + i] = p[4 * b + i] * (ds[4 * b + i] - x[i]);
+            }
+        }
+    };
+    auto gather = [&](const char *Q, const char *G, int u, const f32x16 &p, const f32x16 &ds) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const Frag<T> pf = operand_of<T>(p, s), df = operand_of<T>(ds, s);
+            const int r0 = (32 * u + 16 * s) * L::ROW;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                mma<T>(dv[d], L::along_column(G + r0, 4 * half, 4 * half + 8, 32 * d), pf);
+                mma<T>(dk[d], L::along_column(Q + r0, 4 * half, 4 * half + 8, 32 * d), df);
+            }
+        }
+    };
+    // The products of one 32 rows run beside the exponentials of the other (a wave's matrix instructions take 32 cycles, 4 to issue).
+    auto attend = [&](const char *Q, const char *G, const float *row_lse, const float *row_delta) {
+        f32x16 p0, ds0, p1, ds1;
+        scores(Q, G, 0, p0, ds0);
+        if constexpr (SUB == 2) {
+            __builtin_amdgcn_sched_barrier(0);
+            scores(Q, G, 1, p1, ds1);
+            weights(row_lse, row_delta, 0, p0, ds0);
+            __builtin_amdgcn_sched_barrier(0);
+            gather(Q, G, 0, p0, ds0);
+            weights(row_lse, row_delta, 1, p1, ds1);
+            __builtin_amdgcn_sched_barrier(0);
+            gather(Q, G, 1, p1, ds1);
+        } else {
+            weights(row_lse, row_delta, 0, p0, ds0);
+            gather(Q, G, 0, p0, ds0);
+        }
+    };
+    // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
+    auto turn = [&](int t, const char *__restrict__ Q, const char *__restrict__ G, const float *__restrict__ row_lse,
+                    const float *__restrict__ row_delta, char *__restrict__ Qn, char *__restrict__ Gn, float *__restrict__ lse_n,
+                    float *__restrict__ delta_n) {
+        get(t + 1, Qn, Gn);
+        attend(Q, G, row_lse, row_delta);
+        put(t + 1, Qn, Gn, lse_n, delta_n);
+    };
+    put(first, Qs[0], Gs[0], lses[0], deltas[0]);
+    for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Qs[b], Gs[b], lses[b], deltas[b], Qs[b ^ 1], Gs[b ^ 1], lses[b ^ 1], deltas[b ^ 1]);
+    if (!there) return;
+    const int64_t all = static_cast<int64_t>(a.n_kv) * a.kv_heads;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int c = 32 * d + 8 * b + 4 * half;
+            const float x[4] = {dk[d][4 * b] * a.scale, dk[d][4 * b + 1] * a.scale, dk[d][4 * b + 2] * a.scale, dk[d][4 * b + 3] * a.scale};
+            const float y[4] = {dv[d][4 * b], dv[d][4 * b + 1], dv[d][4 * b + 2], dv[d][4 * b + 3]};
+            if (a.splits > 1) {
+                const int64_t row = (static_cast<int64_t>(here.part) * 2 * a.n_kv + key) * a.kv_heads + here.share;
+                store_four<F32>(a.part, row * a.D + c, a.D - c, x);
+                store_four<F32>(a.part, (row + all) * a.D + c, a.D - c, y);
+            } else {
+                store_four<T>(a.dK, key * a.lddk + here.share * a.D + c, a.D - c, x);
+                store_four<T>(a.dV, key * a.lddv + here.share * a.D + c, a.D - c, y);
+            }
+        }
+}
+
+void launch_attention_dkv(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s) { FTC_ATTN_TYPES(attention_dkv_kernel); }
+
+}  // namespace ftc

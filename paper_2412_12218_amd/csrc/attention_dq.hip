@@ -1,0 +1,139 @@
+// Attention between all nodes of a graph: the kernel of dQ.  See attention_common.hpp.
+//
+// delta = <dO, out> carries the rounding of out.  Where one tile holds all keys of a graph it is the sum of p <dO, v> instead, in fp32,
+// which the dK / dV kernel then finds in its place: one key gives ds = 0 exactly, and few keys, whose ds is small against delta, lose nothing.
+#include "attention_common.hpp"
+
+namespace ftc {
+
+template <class T, int DP, int NW, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void attention_dq_kernel(AttnArgs a)
+{
+    constexpr int TQ = 32 * NW, TK = key_rows<T, NW>(), SUB = TK / 32, KS = DP / 16, DT = DP / 32;
+    typedef LdsTile<T, DP> L;
+    typedef Keys<T, DP, TK, 64 * NW, WHOLE> Tiles;
+    __shared__ __align__(16) char Ks[2][Tiles::BYTES], Vs[2][Tiles::BYTES];
+    __shared__ __align__(16) float biases[2][TK];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const Place here = place_of(a);
+    const Tile tile = find_tile(a.q_ptr, a.graphs, a.n_q, a.group, TQ, here.tile);
+    if (tile.graph < 0) return;
+    const int q0 = clamped(a.q_ptr, tile.graph, a.n_q), q1 = clamped(a.q_ptr, tile.graph + 1, a.n_q);
+    const int rows = (q1 - q0) * a.group;
+    if (q1 <= q0 || static_cast<int64_t>(tile.index) * TQ >= rows) return;
+    const int k0 = clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
+    const int keys = max(k1 - k0, 0), tiles = (keys + TK - 1) / TK;
+    const int each = (tiles + a.splits - 1) / a.splits, first = here.part * each, last = min(tiles, first + each);
+
+    Tiles next;
+    next.look(a, k0 + first * TK, first < last ? k1 : 0);
+    const int r = tile.index * TQ + wave * 32 + col;
+    const bool there = r < rows;
+    int query, head;
+    split_row(a, there ? r : 0, query, head);
+    query += q0;
+    head += here.share * a.group;
+    const char *q_row = head_of<T>(a.Q, query, a.ldq, head * a.D), *g_row = head_of<T>(a.dO, query, a.lddo, head * a.D);
+    Frag<T> q[KS], g[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        const int c = 16 * s + 8 * half;
+        q[s] = operand_at<T, WHOLE>(q_row, c, a.D, there);
+        g[s] = operand_at<T, WHOLE>(g_row, c, a.D, there);
+    }
+    const float scale2 = a.scale * LOG2E;
+    const int64_t at = static_cast<int64_t>(query) * a.heads + head;
+    const float lse = there ? a.lse[at] : -INFINITY;
+    const float minus_lse2 = lse == -INFINITY ? -INFINITY : -lse * LOG2E;  // a row without keys has no probabilities
+    float delta = there && tiles > 1 ? a.delta[at] : 0.f;
+    f32x16 dq[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dq[d] = zero16();
+
+    // p and <dO, v> of 32 keys
+    auto scores = [&](const char *K, const char *V, const float *bias, int u, f32x16 &p, f32x16 &dp) {
+        p = zero16();
+        dp = zero16();
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            mma<T>(p, L::along_row(K + 32 * u * L::ROW, col, 2 * k + half), q[k]);
+            mma<T>(dp, L::along_row(V + 32 * u * L::ROW, col, 2 * k + half), g[k]);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const ftc_f32x4 w = *reinterpret_cast<const ftc_f32x4 *>(&bias[32 * u + 8 * b + 4 * half]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(p[4 * b + i], scale2, w[i] + minus_lse2));
+        }
+    };
+    auto attend = [&](const char *K, const char *V, const float *bias) {
+        if (tiles == 1) {
+            float sum = 0.f, d = 0.f;
+#pragma unroll 1
+            for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+                for (int u = 0; u < SUB; ++u) {
+                    f32x16 p, dp;
+                    scores(K, V, bias, u, p, dp);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        if (pass == 0) sum += p[e];
+                        else d = p[e] != 0.f ? fmaf(p[e] / sum, dp[e], d) : d;
+                    }
+                }
+                if (pass == 0) sum = both_halves_sum(sum);
+            }
+            delta = both_halves_sum(d);
+            if (there && half == 0) a.delta[at] = delta;
+        }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            f32x16 p, dp;
+            scores(K, V, bias, u, p, dp);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] *= dp[e] - delta;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const Frag<T> ds = operand_of<T>(p, k);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) mma<T>(dq[d], L::along_column(K + (32 * u + 16 * k) * L::ROW, 4 * half, 4 * half + 8, 32 * d), ds);
+            }
+        }
+    };
+    auto get = [&](int t, char *K, char *V, float *bias) {
+        if (t >= last) return;
+        next.get(a, K, V, bias, k0 + t * TK, keys - t * TK, here.share);
+        next.look(a, k0 + (t + 1) * TK, k1);
+    };
+    auto put = [&](int t, char *K, char *V, float *bias) {
+        if (t < last) next.put(K, V, bias);
+        __syncthreads();
+    };
+    // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
+    auto turn = [&](int t, const char *__restrict__ K, const char *__restrict__ V, const float *__restrict__ bias, char *__restrict__ Kn,
+                    char *__restrict__ Vn, float *__restrict__ bias_n) {
+        get(t + 1, Kn, Vn, bias_n);
+        attend(K, V, bias);
+        put(t + 1, Kn, Vn, bias_n);
+    };
+    Tiles::clear(a, Ks[0], Vs[0]);
+    Tiles::clear(a, Ks[1], Vs[1]);
+    if (WHOLE && a.D < DP) __syncthreads();
+    get(first, Ks[0], Vs[0], biases[0]);
+    put(first, Ks[0], Vs[0], biases[0]);
+    for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
+    if (!there) return;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int c = 32 * d + 8 * b + 4 * half;
+            const float x[4] = {dq[d][4 * b] * a.scale, dq[d][4 * b + 1] * a.scale, dq[d][4 * b + 2] * a.scale, dq[d][4 * b + 3] * a.scale};
+            if (a.splits > 1) store_four<F32>(a.part, (static_cast<int64_t>(here.part) * a.n_q * a.heads + at) * a.D + c, a.D - c, x);
+            else store_four<T>(a.dQ, query * a.lddq + head * a.D + c, a.D - c, x);
+        }
+}
+
+void launch_attention_dq(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s) { FTC_ATTN_TYPES(attention_dq_kernel); }
+
+}  // namespace ftc

@@ -1,0 +1,148 @@
+// Attention between all nodes of a graph: the forward kernel.  See attention_common.hpp.
+//
+// A workgroup has 32 queries a wave and walks over the keys of their graph in tiles, the next one on its way to LDS while
+// this one is multiplied.
+#include "attention_common.hpp"
+
+namespace ftc {
+
+template <class T, int DP, int NW, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void attention_forward_kernel(AttnArgs a)
+{
+    constexpr int TQ = 32 * NW, TK = key_rows<T, NW>(), SUB = TK / 32, KS = DP / 16, DT = DP / 32;
+    typedef LdsTile<T, DP> L;
+    typedef Keys<T, DP, TK, 64 * NW, WHOLE> Tiles;
+    __shared__ __align__(16) char Ks[2][Tiles::BYTES], Vs[2][Tiles::BYTES];
+    __shared__ __align__(16) float biases[2][TK];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const Place here = place_of(a);
+    const Tile tile = find_tile(a.q_ptr, a.graphs, a.n_q, a.group, TQ, here.tile);
+    if (tile.graph < 0) return;
+    const int q0 = clamped(a.q_ptr, tile.graph, a.n_q), q1 = clamped(a.q_ptr, tile.graph + 1, a.n_q);
+    const int rows = (q1 - q0) * a.group;  // virtual rows of the graph
+    if (q1 <= q0 || static_cast<int64_t>(tile.index) * TQ >= rows) return;
+    const int k0 = clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
+    const int keys = max(k1 - k0, 0), tiles = (keys + TK - 1) / TK;
+    const int each = (tiles + a.splits - 1) / a.splits, first = here.part * each, last = min(tiles, first + each);
+
+    Tiles next;
+    next.look(a, k0 + first * TK, first < last ? k1 : 0);
+    const int r = tile.index * TQ + wave * 32 + col;
+    const bool there = r < rows;
+    int query, head;
+    split_row(a, there ? r : 0, query, head);
+    query += q0;
+    head += here.share * a.group;
+    // scale has the sign of +: the maximum of the products is then that of the scores
+    const float scale2 = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);
+    const char *q_row = head_of<T>(a.Q, query, a.ldq, head * a.D);
+    Frag<T> q[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        const int c = 16 * s + 8 * half;
+        q[s] = operand_at<T, WHOLE>(q_row, c, a.D, there);
+        if (a.scale < 0.f) frag_negate<T>(q[s]);
+    }
+    float m = -INFINITY, l = 0.f;  // maximum of the products, sum of the exponentials (a half's keys)
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = zero16();
+
+    auto attend = [&](const char *K, const char *V, const float *bias, bool ragged) {
+        f32x16 s[SUB];
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            s[u] = zero16();
+#pragma unroll
+            for (int k = 0; k < KS; ++k) mma<T>(s[u], L::along_row(K + 32 * u * L::ROW, col, 2 * k + half), q[k]);
+            if (ragged) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const ftc_f32x4 w = *reinterpret_cast<const ftc_f32x4 *>(&bias[32 * u + 8 * b + 4 * half]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[u][4 * b + i] += w[i];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+        }
+        const float m_new = fmaxf(m, both_halves_max(top)), shift = m_new == -INFINITY ? 0.f : m_new * scale2;
+        if (__builtin_amdgcn_ballot_w64(m_new != m)) {
+            const float fade = __builtin_amdgcn_exp2f(fmaf(m, scale2, -shift));
+            l *= fade;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= fade;
+            m = m_new;
+        }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], scale2, -shift));
+                l += s[u][e];
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const Frag<T> p = operand_of<T>(s[u], k);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) mma<T>(o[d], L::along_column(V + (32 * u + 16 * k) * L::ROW, 4 * half, 4 * half + 8, 32 * d), p);
+            }
+        }
+    };
+    auto get = [&](int t, char *K, char *V, float *bias) {
+        if (t >= last) return;
+        next.get(a, K, V, bias, k0 + t * TK, keys - t * TK, here.share);
+        next.look(a, k0 + (t + 1) * TK, k1);
+    };
+    auto put = [&](int t, char *K, char *V, float *bias) {
+        if (t < last) next.put(K, V, bias);
+        __syncthreads();
+    };
+    // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
+    auto turn = [&](int t, const char *__restrict__ K, const char *__restrict__ V, const float *__restrict__ bias, char *__restrict__ Kn,
+                    char *__restrict__ Vn, float *__restrict__ bias_n) {
+        get(t + 1, Kn, Vn, bias_n);
+        attend(K, V, bias, a.mask || (t + 1) * TK > keys);
+        put(t + 1, Kn, Vn, bias_n);
+    };
+    Tiles::clear(a, Ks[0], Vs[0]);
+    Tiles::clear(a, Ks[1], Vs[1]);
+    if (WHOLE && a.D < DP) __syncthreads();
+    get(first, Ks[0], Vs[0], biases[0]);
+    put(first, Ks[0], Vs[0], biases[0]);
+    for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
+    l = both_halves_sum(l);
+    m *= scale2;
+    if (!there) return;
+    if (a.splits > 1) {
+        const int64_t row = (static_cast<int64_t>(here.part) * a.n_q + query) * a.heads + head;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int c = 32 * d + 8 * b + 4 * half;
+                const float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+                store_four<F32>(a.part, row * a.D + c, a.D - c, x);
+            }
+        if (half == 0) {
+            a.part_ml[2 * row] = m;
+            a.part_ml[2 * row + 1] = l;
+        }
+        return;
+    }
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int c = 32 * d + 8 * b + 4 * half;
+            const float x[4] = {o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv};
+            store_four<T>(a.out, query * a.ldo + head * a.D + c, a.D - c, x);
+        }
+    if (a.lse && half == 0) a.lse[static_cast<int64_t>(query) * a.heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+void launch_attention_forward(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s) { FTC_ATTN_TYPES(attention_forward_kernel); }
+
+}  // namespace ftc

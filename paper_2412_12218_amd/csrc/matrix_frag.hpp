@@ -41,6 +41,18 @@ __device__ __forceinline__ void frag_zero(Frag<T> &a)
     }
 }
 
+template <class T>
+__device__ __forceinline__ void frag_negate(Frag<T> &a)
+{
+    if constexpr (T::BYTES == 4) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) a.f[j] = -a.f[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a.w[j] ^= 0x80008000u;
+    }
+}
+
 // Eight fp32 numbers as an operand, rounded to nearest even where it has 16 bits.
 template <class T>
 __device__ __forceinline__ Frag<T> frag_of(const float (&x)[8])
