@@ -278,9 +278,9 @@ inline bool attn_whole(const void *p, int64_t ld, int D, int dtype)
 // dtype, width and waves of a workgroup to template arguments.
 #define FTC_ATTN_WIDTHS(KERNEL, T, NW, WHOLE)                                                                              \
     do {                                                                                                                  \
-        if (a.D <= 32) hipLaunchKernelGGL((KERNEL<T, 32, NW, WHOLE>), dim3(grid), dim3(64 * NW), 0, s, a);                 \
-        else if (a.D <= 64) hipLaunchKernelGGL((KERNEL<T, 64, NW, WHOLE>), dim3(grid), dim3(64 * NW), 0, s, a);            \
-        else hipLaunchKernelGGL((KERNEL<T, 128, NW, WHOLE>), dim3(grid), dim3(64 * NW), 0, s, a);                          \
+        if (a.D <= 32) hipLaunchKernelGGL((KERNEL<T, 32, NW, WHOLE>), dim3(grid), dim3((KERNEL##_threads<T, 32, NW>())), 0, s, a); \
+        else if (a.D <= 64) hipLaunchKernelGGL((KERNEL<T, 64, NW, WHOLE>), dim3(grid), dim3((KERNEL##_threads<T, 64, NW>())), 0, s, a); \
+        else hipLaunchKernelGGL((KERNEL<T, 128, NW, WHOLE>), dim3(grid), dim3((KERNEL##_threads<T, 128, NW>())), 0, s, a);  \
     } while (0)
 #define FTC_ATTN_LAUNCH(KERNEL, T)                                                                                        \
     do {                                                                                                                  \
@@ -296,7 +296,7 @@ inline bool attn_whole(const void *p, int64_t ld, int D, int dtype)
         else FTC_ATTN_LAUNCH(KERNEL, BF16);                                                                                \
     } while (0)
 
-// nw: waves of a workgroup, 1 or 4; grid: a.tiles * a.kv_heads * a.splits workgroups
+// nw: waves of a workgroup that have rows of their own, 1 or 4; grid: a.tiles * a.kv_heads * a.splits workgroups
 void launch_attention_forward(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s);
 void launch_attention_dq(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s);
 void launch_attention_dkv(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s);

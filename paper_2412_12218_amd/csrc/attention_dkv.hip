@@ -1,6 +1,8 @@
 // Attention between all nodes of a graph: the kernel of dK and dV.  See attention_common.hpp.
 //
-// A wave has 32 keys, their K and V in registers, and walks over the virtual rows of their graph's queries.
+// A wave has 32 keys and walks over the virtual rows of their graph's queries, its K and V in registers.  Where these, dK and dV
+// would leave a SIMD one wave (16 bits, D above 64), K and V of the workgroup's keys are in LDS instead and a second set of waves has the
+// same keys and every second 32 rows; the two sums are added at the end.
 #include "attention_common.hpp"
 
 namespace ftc {
@@ -8,15 +10,21 @@ namespace ftc {
 template <class T, int DP>
 constexpr int query_rows() { return T::BYTES == 2 ? 64 : 32; }
 
+// Sets of waves that share the keys.
+template <class T, int DP, int NW>
+constexpr int wave_sets() { return T::BYTES == 2 && DP == 128 && NW == 4 ? 2 : 1; }
+
 template <class T, int DP, int NW, bool WHOLE>
-__global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
+__global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (wave_sets<T, DP, NW>()) == 1 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
 {
-    constexpr int TK = 32 * NW, TQ = query_rows<T, DP>(), SUB = TQ / 32, KS = DP / 16, DT = DP / 32;
+    constexpr int SETS = wave_sets<T, DP, NW>(), THREADS = 64 * NW * SETS;
+    constexpr int TK = 32 * NW, TQ = query_rows<T, DP>(), SUB = TQ / 32 / SETS, KS = DP / 16, DT = DP / 32;
     typedef LdsTile<T, DP> L;
-    typedef Rows<T, DP, TQ, 64 * NW, WHOLE> R;
-    __shared__ __align__(16) char Qs[2][R::BYTES], Gs[2][R::BYTES];
+    typedef Rows<T, DP, TQ, THREADS, WHOLE> R;
+    typedef Rows<T, DP, TK, THREADS, WHOLE> KeyRows;
+    __shared__ __align__(16) char Qs[2][R::BYTES], Gs[2][R::BYTES], Ks[SETS == 2 ? KeyRows::BYTES : 16], Vs[SETS == 2 ? KeyRows::BYTES : 16];
     __shared__ __align__(16) float lses[2][TQ], deltas[2][TQ];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % NW, set = (threadIdx.x >> 6) / NW, col = lane & 31, half = lane >> 5;
     const Place here = place_of(a);
     const Tile tile = find_tile(a.kv_ptr, a.graphs, a.n_kv, 1, TK, here.tile);
     if (tile.graph < 0) return;
@@ -87,14 +95,45 @@ __global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kern
     }
     if (WHOLE && a.D < DP) __syncthreads();
     get(first, Qs[0], Gs[0]);
-    const char *k_row = head_of<T>(a.K, seen ? key : k0, a.ldk, here.share * a.D), *v_row = head_of<T>(a.V, seen ? key : k0, a.ldv, here.share * a.D);
-    Frag<T> k[KS], v[KS];
+    Frag<T> k[SETS == 2 ? 1 : KS], v[SETS == 2 ? 1 : KS];
+    if constexpr (SETS == 2) {
+        const int first_key = k0 + tile.index * TK;
+        const char *kp = head_of<T>(a.K, first_key, a.ldk, here.share * a.D), *vp = head_of<T>(a.V, first_key, a.ldv, here.share * a.D);
+        const typename R::Offset ldk = a.ldk, ldv = a.ldv;
+        KeyRows kr, vr;
+        KeyRows::clear(Ks, a.D);
+        KeyRows::clear(Vs, a.D);
+        if (WHOLE && a.D < DP) __syncthreads();
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        const int c = 16 * s + 8 * half;
-        k[s] = operand_at<T, WHOLE>(k_row, c, a.D, seen);
-        v[s] = operand_at<T, WHOLE>(v_row, c, a.D, seen);
+        for (int e = 0; e < KeyRows::EACH; ++e) {
+            const int j = first_key + KeyRows::row(e);
+            if (j < k1 && (!a.mask || a.mask[j])) {
+                kr.get(Ks, e, kp, KeyRows::row(e) * ldk + KeyRows::col(e), a.D);
+                vr.get(Vs, e, vp, KeyRows::row(e) * ldv + KeyRows::col(e), a.D);
+            } else {
+                kr.get_zeros(Ks, e);
+                vr.get_zeros(Vs, e);
+            }
+        }
+        kr.put(Ks);
+        vr.put(Vs);
+    } else {
+        const char *k_row = head_of<T>(a.K, seen ? key : k0, a.ldk, here.share * a.D), *v_row = head_of<T>(a.V, seen ? key : k0, a.ldv, here.share * a.D);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int c = 16 * s + 8 * half;
+            k[s] = operand_at<T, WHOLE>(k_row, c, a.D, seen);
+            v[s] = operand_at<T, WHOLE>(v_row, c, a.D, seen);
+        }
     }
+    auto key_operand = [&](int s) {
+        if constexpr (SETS == 2) return L::along_row(Ks + 32 * wave * L::ROW, col, 2 * s + half);
+        else return k[s];
+    };
+    auto value_operand = [&](int s) {
+        if constexpr (SETS == 2) return L::along_row(Vs + 32 * wave * L::ROW, col, 2 * s + half);
+        else return v[s];
+    };
     const float scale2 = a.scale * LOG2E, bias = seen ? 0.f : -INFINITY;
     f32x16 dk[DT], dv[DT];
 #pragma unroll
@@ -106,8 +145,8 @@ __global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kern
         ds = zero16();
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            mma<T>(p, L::along_row(Q + 32 * u * L::ROW, col, 2 * s + half), k[s]);
-            mma<T>(ds, L::along_row(G + 32 * u * L::ROW, col, 2 * s + half), v[s]);
+            mma<T>(p, L::along_row(Q + 32 * u * L::ROW, col, 2 * s + half), key_operand(s));
+            mma<T>(ds, L::along_row(G + 32 * u * L::ROW, col, 2 * s + half), value_operand(s));
         }
     };
     // p and ds from them
@@ -138,7 +177,8 @@ __global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kern
     // The products of one 32 rows run beside the exponentials of the other (a wave's matrix instructions take 32 cycles, 4 to issue).
     auto attend = [&](const char *Q, const char *G, const float *row_lse, const float *row_delta) {
         f32x16 p0, ds0, p1, ds1;
-        scores(Q, G, 0, p0, ds0);
+        const int u0 = SETS == 2 ? set : 0;
+        scores(Q, G, u0, p0, ds0);
         if constexpr (SUB == 2) {
             __builtin_amdgcn_sched_barrier(0);
             scores(Q, G, 1, p1, ds1);
@@ -149,8 +189,8 @@ __global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kern
             __builtin_amdgcn_sched_barrier(0);
             gather(Q, G, 1, p1, ds1);
         } else {
-            weights(row_lse, row_delta, 0, p0, ds0);
-            gather(Q, G, 0, p0, ds0);
+            weights(row_lse, row_delta, u0, p0, ds0);
+            gather(Q, G, u0, p0, ds0);
         }
     };
     // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
@@ -163,6 +203,37 @@ __global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kern
     };
     put(first, Qs[0], Gs[0], lses[0], deltas[0]);
     for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Qs[b], Gs[b], lses[b], deltas[b], Qs[b ^ 1], Gs[b ^ 1], lses[b ^ 1], deltas[b ^ 1]);
+    if constexpr (SETS == 2) {  // dK, then dV of the second set, where the queries were
+        static_assert(sizeof(Qs) + sizeof(Gs) >= NW * DT * 4 * 1024, "room for a sum of every wave");
+        auto add = [&](f32x16(&sum)[DT]) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int at = (wave * DT + d) * 4 + b;
+                    ftc_f32x4 *to = reinterpret_cast<ftc_f32x4 *>(at < static_cast<int>(sizeof(Qs) / 1024) ? &Qs[0][0] + at * 1024 : &Gs[0][0] + at * 1024 - sizeof(Qs)) + lane;
+                    if (set == 1) {
+                        *to = ftc_f32x4{sum[d][4 * b], sum[d][4 * b + 1], sum[d][4 * b + 2], sum[d][4 * b + 3]};
+                    }
+                }
+            __syncthreads();
+            if (set == 0) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const int at = (wave * DT + d) * 4 + b;
+                        const ftc_f32x4 x = reinterpret_cast<const ftc_f32x4 *>(at < static_cast<int>(sizeof(Qs) / 1024) ? &Qs[0][0] + at * 1024 : &Gs[0][0] + at * 1024 - sizeof(Qs))[lane];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[d][4 * b + i] += x[i];
+                    }
+            }
+            __syncthreads();
+        };
+        add(dk);
+        add(dv);
+        if (set == 1) return;
+    }
     if (!there) return;
     const int64_t all = static_cast<int64_t>(a.n_kv) * a.kv_heads;
 #pragma unroll
@@ -182,6 +253,9 @@ __global__ __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) void attention_dkv_kern
             }
         }
 }
+
+template <class T, int DP, int NW>
+constexpr int attention_dkv_kernel_threads() { return 64 * NW * wave_sets<T, DP, NW>(); }
 
 void launch_attention_dkv(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s) { FTC_ATTN_TYPES(attention_dkv_kernel); }
 

@@ -134,6 +134,9 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         }
 }
 
+template <class T, int DP, int NW>
+constexpr int attention_dq_kernel_threads() { return 64 * NW; }
+
 void launch_attention_dq(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s) { FTC_ATTN_TYPES(attention_dq_kernel); }
 
 }  // namespace ftc

@@ -143,6 +143,9 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
     if (a.lse && half == 0) a.lse[static_cast<int64_t>(query) * a.heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
+template <class T, int DP, int NW>
+constexpr int attention_forward_kernel_threads() { return 64 * NW; }
+
 void launch_attention_forward(const AttnArgs &a, int dtype, int nw, bool whole, unsigned grid, hipStream_t s) { FTC_ATTN_TYPES(attention_forward_kernel); }
 
 }  // namespace ftc
