@@ -133,6 +133,10 @@ def _ptr(t):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+# torch.cuda.current_device() without its check that CUDA is initialised, which a tensor on the GPU implies
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream():
     """Handle of torch's current stream on the current device."""
     if _raw_stream is None:
@@ -452,12 +456,13 @@ def ftc_agnn_layer_backward_fused(g, w, H, row_z, Y, dY, beta=1.0, dH=None, dh_d
 FTC_ACT_NONE, FTC_ACT_RELU, FTC_ACT_GELU, FTC_ACT_SILU = 0, 1, 2, 3
 
 
-def _check_tensors(*tensors):
-    """All on the current device, on whose stream the call is made."""
-    dev = torch.cuda.current_device()
+def _here(*tensors):
+    """Handle of the current stream; the tensors are on its device."""
+    dev = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
 
 def _ld(t, rows, cols, dtype=None):
@@ -481,9 +486,9 @@ def ftc_embedding(ids, E, scale=1.0, out=None, out_dtype=None):
     if out is None:
         out = torch.empty((n, D), dtype=out_dtype or E.dtype, device=E.device)
     _vector(ids, n, (torch.int32,))
-    _check_tensors(ids, E, out)
+    stream = _here(ids, E, out)
     _check(lib().ftc_embedding(n, _ptr(ids), vocab, _ptr(E), _ld(E, vocab, D), _dt(E), D, scale, _ptr(out), _ld(out, n, D), _dt(out),
-                               _stream()))
+                               stream))
     return out
 
 
@@ -494,9 +499,9 @@ def ftc_embedding_backward(ids, dOut, vocab, scale=1.0, dE=None, de_dtype=torch.
     if ws is None:
         ws = _workspace(lib().ftc_embedding_backward_workspace_bytes(n, vocab, D), dOut.device)
     _vector(ids, n, (torch.int32,))
-    _check_tensors(ids, dOut, dE, ws)
+    stream = _here(ids, dOut, dE, ws)
     _check(lib().ftc_embedding_backward(n, _ptr(ids), vocab, _ptr(dOut), _ld(dOut, n, D), _dt(dOut), D, scale, _ptr(dE),
-                                        _ld(dE, vocab, D), _dt(dE), _ptr(ws), ws.numel(), _stream()))
+                                        _ld(dE, vocab, D), _dt(dE), _ptr(ws), ws.numel(), stream))
     return dE
 
 
@@ -513,7 +518,7 @@ def ftc_linear(X, W, bias=None, act=FTC_ACT_NONE, residual=None, out=None, out_d
         out = torch.empty((n, d_out), dtype=out_dtype or X.dtype, device=X.device)
     if ws is None:
         ws = _workspace(lib().ftc_linear_workspace_bytes(n, d_in, d_out), X.device)
-    _check_tensors(X, W, bias, residual, out, slope, ws)
+    stream = _here(X, W, bias, residual, out, slope, ws)
     _ld(W, d_in, d_out, X.dtype)
     if not W.is_contiguous():
         raise ValueError("W must be contiguous")
@@ -523,7 +528,7 @@ def ftc_linear(X, W, bias=None, act=FTC_ACT_NONE, residual=None, out=None, out_d
     _check(lib().ftc_linear(n, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(bias), act, _ptr(residual),
                             _ld(residual, n, d_out, X.dtype) if residual is not None else 0, _ptr(slope),
                             _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(out), _ld(out, n, d_out), _dt(out), _ptr(ws),
-                            ws.numel(), _stream()))
+                            ws.numel(), stream))
     return out
 
 
@@ -541,7 +546,7 @@ def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_d
         db = torch.empty(d_out, dtype=wdt, device=X.device)
     if ws is None:
         ws = _workspace(lib().ftc_linear_backward_workspace_bytes(n, d_in, d_out), X.device)
-    _check_tensors(X, W, dZ, slope, dX, dW, db, ws)
+    stream = _here(X, W, dZ, slope, dX, dW, db, ws)
     _ld(W, d_in, d_out, X.dtype)
     if not W.is_contiguous() or (dW is not None and not dW.is_contiguous()):
         raise ValueError("W and dW must be contiguous")
@@ -553,7 +558,7 @@ def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_d
     _check(lib().ftc_linear_backward(n, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(slope),
                                      _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(dZ), _ld(dZ, n, d_out, X.dtype),
                                      _ptr(dX), _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
-                                     _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), _stream()))
+                                     _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), stream))
     return dX, dW, db
 
 
@@ -577,14 +582,14 @@ def ftc_graph_attention(Q, K, V, q_ptr, kv_ptr, heads, kv_heads=None, scale=None
         out = torch.empty((n_q, heads * D), dtype=Q.dtype, device=Q.device)
     if ws is None:
         ws = _workspace(lib().ftc_graph_attention_workspace_bytes(*sizes), Q.device)
-    _check_tensors(Q, K, V, q_ptr, kv_ptr, kv_mask, out, lse, ws)
+    stream = _here(Q, K, V, q_ptr, kv_ptr, kv_mask, out, lse, ws)
     dt = Q.dtype
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_q, heads) or not lse.is_contiguous()):
         raise ValueError("lse is a contiguous n_q x heads fp32 tensor")
     _check(lib().ftc_graph_attention(n_q, _ptr(q_ptr), n_kv, _ptr(kv_ptr), graphs, heads, kv_heads, D, _DTYPES[dt],
                                      _ptr(Q), _ld(Q, n_q, heads * D), _ptr(K), _ld(K, n_kv, kv_heads * D, dt), _ptr(V),
                                      _ld(V, n_kv, kv_heads * D, dt), _ptr(kv_mask), D ** -0.5 if scale is None else scale, _ptr(out),
-                                     _ld(out, n_q, heads * D, dt), _ptr(lse), _ptr(ws), ws.numel(), _stream()))
+                                     _ld(out, n_q, heads * D, dt), _ptr(lse), _ptr(ws), ws.numel(), stream))
     return out
 
 
@@ -598,7 +603,7 @@ def ftc_graph_attention_backward(Q, K, V, q_ptr, kv_ptr, out, lse, dOut, heads, 
     dQ, dK, dV = dQ if dQ is not None else new(Q), dK if dK is not None else new(K), dV if dV is not None else new(V)
     if ws is None:
         ws = _workspace(lib().ftc_graph_attention_backward_workspace_bytes(*sizes), Q.device)
-    _check_tensors(Q, K, V, q_ptr, kv_ptr, kv_mask, out, lse, dOut, dQ, dK, dV, ws)
+    stream = _here(Q, K, V, q_ptr, kv_ptr, kv_mask, out, lse, dOut, dQ, dK, dV, ws)
     if lse.dtype != torch.float32 or lse.shape != (n_q, heads) or not lse.is_contiguous():
         raise ValueError("lse is a contiguous n_q x heads fp32 tensor")
     hd, kd = heads * D, kv_heads * D
@@ -606,7 +611,7 @@ def ftc_graph_attention_backward(Q, K, V, q_ptr, kv_ptr, out, lse, dOut, heads, 
         n_q, _ptr(q_ptr), n_kv, _ptr(kv_ptr), graphs, heads, kv_heads, D, _DTYPES[dt], _ptr(Q), _ld(Q, n_q, hd), _ptr(K), _ld(K, n_kv, kd, dt),
         _ptr(V), _ld(V, n_kv, kd, dt), _ptr(kv_mask), D ** -0.5 if scale is None else scale, _ptr(out), _ld(out, n_q, hd, dt), _ptr(lse),
         _ptr(dOut), _ld(dOut, n_q, hd, dt), _ptr(dQ), _ld(dQ, n_q, hd, dt), _ptr(dK), _ld(dK, n_kv, kd, dt), _ptr(dV),
-        _ld(dV, n_kv, kd, dt), _ptr(ws), ws.numel(), _stream()))
+        _ld(dV, n_kv, kd, dt), _ptr(ws), ws.numel(), stream))
     return dQ, dK, dV
 
 

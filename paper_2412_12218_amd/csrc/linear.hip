@@ -171,6 +171,10 @@ static size_t dense_ws(int M, int N, int K)
 template <bool AX, bool BX>
 static void dense(DenseArgs a, int dtype, void *ws, hipStream_t s)
 {
+    if (!AX && a.M <= dense_few_rows(BX)) {
+        launch_dense_rows(a, dtype, BX, s);
+        return;
+    }
     const bool fast = dense_whole_pieces(a.A, a.lda, AX ? a.M : a.K, dtype) && dense_whole_pieces(a.B, a.ldb, BX ? a.N : a.K, dtype);
     const DensePlan p = dense_plan(a.M, a.N, a.K, dtype == FTC_F32, fast);
     a.splits = p.splits;

@@ -122,17 +122,22 @@ __device__ __forceinline__ Frag<T> load_frag(const void *base, int64_t idx, int 
     return a;
 }
 
-// Eight consecutive numbers at element `idx`, aligned to an element; those from `left` on are zero and not read.
+// The eight numbers of an operand in fp32.
 template <class T>
-__device__ __forceinline__ void load_eight_numbers(const void *base, int64_t idx, int left, float (&x)[8])
+__device__ __forceinline__ void frag_numbers(const Frag<T> &a, float (&x)[8])
 {
-    const Frag<T> a = load_frag<T>(base, idx, left);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if constexpr (T::BYTES == 4) x[j] = a.f[j];
         else if constexpr (std::is_same<T, F16>::value) x[j] = f16_bits_to_f32((a.w[j / 2] >> (16 * (j & 1))) & 0xffffu);
         else x[j] = bf16_bits_to_f32((a.w[j / 2] >> (16 * (j & 1))) & 0xffffu);
     }
+}
+// Eight consecutive numbers at element `idx`, aligned to an element; those from `left` on are zero and not read.
+template <class T>
+__device__ __forceinline__ void load_eight_numbers(const void *base, int64_t idx, int left, float (&x)[8])
+{
+    frag_numbers<T>(load_frag<T>(base, idx, left), x);
 }
 // ... in a run-time type; those from `left` on are not written
 __device__ __forceinline__ void store_eight_numbers(void *base, int64_t idx, int dtype, int left, const float (&x)[8])

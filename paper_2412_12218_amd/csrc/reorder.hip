@@ -388,36 +388,212 @@ int32_t launch_order_by_key(int n, const int *keys_in, int *perm, int *inv, int 
 }
 
 // ---- positions by id -------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void id_pairs_kernel(int n, const int *__restrict__ ids, int vocab, uint32_t *__restrict__ keys,
-                                                       uint32_t *__restrict__ vals)
+// The radix sort above with what ids allow: the first pass takes them where they are (an id outside the table as `vocab`, the last key), a workgroup
+// scans the tiles of one digit, and the scatter kernel adds up the digits before its own itself: three launches a pass instead of four and one before all.
+// Up to ID_RANK ids one launch does: a place is the number of ids that are smaller, or equal and before, which eight threads count
+// for each of the 32 ids of a workgroup.
+constexpr int ID_RANK = 4096, ID_RANK_EACH = 32;
+
+__device__ __forceinline__ uint32_t id_key(int id, int vocab) { return static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab); }
+
+__global__ __launch_bounds__(256) void id_rank_kernel(int n, const int *__restrict__ ids, int vocab, uint32_t *__restrict__ keys,
+                                                      uint32_t *__restrict__ order)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const int id = ids[i];
-    keys[i] = static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab);
-    vals[i] = static_cast<uint32_t>(i);
+    __shared__ __align__(16) uint32_t all[ID_RANK];
+    const int quads = (n + 3) / 4;
+    for (int i = threadIdx.x; i < quads * 4; i += 256) all[i] = i < n ? id_key(ids[i], vocab) : 0xffffffffu;
+    __syncthreads();
+    const int mine = blockIdx.x * ID_RANK_EACH + threadIdx.x / 8, slice = threadIdx.x % 8;
+    const uint32_t key = mine < n ? all[mine] : 0u;
+    int rank = 0;
+#pragma unroll 4
+    for (int q = slice; q < quads; q += 8) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(&all[4 * q]);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) rank += w[k] < key || (w[k] == key && 4 * q + k < mine) ? 1 : 0;
+    }
+#pragma unroll
+    for (int m = 4; m >= 1; m >>= 1) rank += __shfl_xor(rank, m, 64);
+    if (slice == 0 && mine < n) {
+        keys[rank] = key;
+        order[rank] = static_cast<uint32_t>(mine);
+    }
 }
 
-static size_t id_table_bytes(int n)
+template <int BITS, int ROUNDS, bool FIRST>
+__global__ __launch_bounds__(256) void id_hist_kernel(const uint32_t *__restrict__ keys, int vocab, int64_t count, int shift, int64_t n_tiles,
+                                                      int *__restrict__ hist)
 {
-    const int64_t table = 256 * radix_tiles(n, radix_rounds(n));
-    return align_up(static_cast<size_t>(table) * sizeof(int), 256) + scan_ws(table);
+    constexpr int DIGITS = 1 << BITS;
+    __shared__ int cnt_all[4][DIGITS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t tile = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    if (tile >= n_tiles) return;  // no workgroup barrier below
+    int *cnt = cnt_all[wave];
+#pragma unroll
+    for (int k = 0; k < DIGITS / 64; ++k) cnt[lane + 64 * k] = 0;
+    const int64_t base = tile * (64 * ROUNDS);
+    uint32_t key[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int64_t i = base + r * 64 + lane;
+        key[r] = i < count ? keys[i] : 0u;
+        if (FIRST) key[r] = id_key(static_cast<int>(key[r]), vocab);
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+        if (base + r * 64 + lane < count) atomicAdd(&cnt[(key[r] >> shift) & (DIGITS - 1u)], 1);
+    wave_lds_fence();
+#pragma unroll
+    for (int k = 0; k < DIGITS / 64; ++k) hist[(lane + 64 * k) * n_tiles + tile] = cnt[lane + 64 * k];
 }
 
-size_t id_sort_ws(int n) { return 4 * align_up(static_cast<size_t>(n) * sizeof(uint32_t), 256) + id_table_bytes(n); }
+// Tiles of digit blockIdx.x: hist[tile] <- the digit's elements in the tiles before; totals[digit] <- in all of them.
+__global__ __launch_bounds__(256) void id_scan_kernel(int64_t n_tiles, int *__restrict__ hist, int *__restrict__ totals)
+{
+    int *row = hist + blockIdx.x * n_tiles;
+    int carry = 0;
+    for (int64_t base = 0; base < n_tiles; base += 1024) {
+        int v[4], sum = 0, total;
+        const int64_t i = base + threadIdx.x * 4;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = i + k < n_tiles ? row[i + k] : 0;
+            sum += v[k];
+        }
+        int run = carry + block_exclusive_scan(sum, &total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i + k < n_tiles) row[i + k] = run;
+            run += v[k];
+        }
+        carry += total;
+    }
+    if (threadIdx.x == 0) totals[blockIdx.x] = carry;
+}
+
+template <int BITS, int ROUNDS, bool FIRST>
+__global__ __launch_bounds__(256) void id_scatter_kernel(const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals, int vocab, int64_t count,
+                                                         int shift, int64_t n_tiles, const int *__restrict__ pos, const int *__restrict__ totals,
+                                                         uint32_t *__restrict__ keys_out, uint32_t *__restrict__ vals_out)
+{
+    constexpr int DIGITS = 1 << BITS;
+    __shared__ int digits[DIGITS], next_all[4][DIGITS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int mine[DIGITS / 256], sum = 0, all;
+#pragma unroll
+    for (int k = 0; k < DIGITS / 256; ++k) {
+        mine[k] = totals[threadIdx.x * (DIGITS / 256) + k];
+        sum += mine[k];
+    }
+    int before = block_exclusive_scan(sum, &all);
+#pragma unroll
+    for (int k = 0; k < DIGITS / 256; ++k) {
+        digits[threadIdx.x * (DIGITS / 256) + k] = before;
+        before += mine[k];
+    }
+    const int64_t tile = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    const int64_t base = tile * (64 * ROUNDS);
+    uint32_t key[ROUNDS], val[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int64_t i = base + r * 64 + lane;
+        key[r] = i < count ? keys[i] : 0u;
+        if (FIRST) {
+            key[r] = id_key(static_cast<int>(key[r]), vocab);
+            val[r] = static_cast<uint32_t>(i);
+        } else {
+            val[r] = i < count ? vals[i] : 0u;
+        }
+    }
+    __syncthreads();
+    if (tile >= n_tiles) return;  // no workgroup barrier below
+    int *next = next_all[wave];
+#pragma unroll
+    for (int k = 0; k < DIGITS / 64; ++k) next[lane + 64 * k] = digits[lane + 64 * k] + pos[(lane + 64 * k) * n_tiles + tile];
+    wave_lds_fence();
+    const uint64_t below = (1ull << lane) - 1ull;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const bool ok = base + r * 64 + lane < count;
+        const uint32_t d = (key[r] >> shift) & (DIGITS - 1u);
+        uint64_t peers = __builtin_amdgcn_ballot_w64(ok);  // lanes that hold the same digit
+#pragma unroll
+        for (int b = 0; b < BITS; ++b) {
+            const bool bit = (d >> b) & 1u;
+            const uint64_t with_bit = __builtin_amdgcn_ballot_w64(bit);
+            peers &= bit ? with_bit : ~with_bit;
+        }
+        const int rank = __popcll(peers & below);
+        const int first = ok ? next[d] : 0;
+        wave_lds_fence();
+        if (ok && rank == 0) next[d] = first + __popcll(peers);
+        wave_lds_fence();
+        if (ok) {
+            keys_out[first + rank] = key[r];
+            vals_out[first + rank] = val[r];
+        }
+    }
+}
+
+static size_t id_array_bytes(int n) { return align_up(static_cast<size_t>(n) * sizeof(uint32_t), 256); }
+
+size_t id_sort_ws(int n)
+{
+    if (n <= ID_RANK) return 2 * id_array_bytes(n);
+    return 4 * id_array_bytes(n) + 512 * sizeof(int) + align_up(static_cast<size_t>(512 * radix_tiles(n, radix_rounds(n))) * sizeof(int), 256);
+}
 
 int32_t launch_sort_ids(int n, const int *ids, int vocab, const uint32_t **keys, const uint32_t **order, void *ws, hipStream_t s)
 {
-    const size_t arr = align_up(static_cast<size_t>(n) * sizeof(uint32_t), 256);
+    const size_t arr = id_array_bytes(n);
     char *p = static_cast<char *>(ws);
-    uint32_t *k0 = reinterpret_cast<uint32_t *>(p), *v0 = reinterpret_cast<uint32_t *>(p + arr);
-    uint32_t *k1 = reinterpret_cast<uint32_t *>(p + 2 * arr), *v1 = reinterpret_cast<uint32_t *>(p + 3 * arr);
-    if (n > 0) hipLaunchKernelGGL(id_pairs_kernel, dim3(ceil_div(n, 256)), dim3(256), 0, s, n, ids, vocab, k0, v0);
-    uint32_t *kr, *vr;
-    const int32_t st = radix_sort_pairs(k0, v0, k1, v1, n, bit_length(static_cast<uint32_t>(vocab)), nullptr, &kr, &vr, p + 4 * arr, s, true);
-    *keys = kr;
-    *order = vr;
-    return st;
+    uint32_t *k[2] = {reinterpret_cast<uint32_t *>(p), reinterpret_cast<uint32_t *>(p + 2 * arr)};
+    uint32_t *v[2] = {reinterpret_cast<uint32_t *>(p + arr), reinterpret_cast<uint32_t *>(p + 3 * arr)};
+    *keys = k[0];
+    *order = v[0];
+    if (n == 0) return FTC_OK;
+    if (n <= ID_RANK) {
+        hipLaunchKernelGGL(id_rank_kernel, dim3(ceil_div(n, ID_RANK_EACH)), dim3(256), 0, s, n, ids, vocab, k[0], v[0]);
+        return launch_status("id sort");
+    }
+    int *totals = reinterpret_cast<int *>(p + 4 * arr), *table = totals + 512;
+    // digits of nine bits where they save a pass (vocab 65 536 to 262 143: two for three)
+    const int rounds = radix_rounds(n), bits = bit_length(static_cast<uint32_t>(vocab)), passes = bits > 9 ? (bits + 8) / 9 : 1;
+    const int digit = bits <= 8 * passes ? 8 : 9;
+    const int64_t n_tiles = radix_tiles(n, rounds);
+    const dim3 grid(static_cast<unsigned>((n_tiles + 3) / 4));
+    const uint32_t *ki = reinterpret_cast<const uint32_t *>(ids), *vi = nullptr;
+#define FTC_ID(KERNEL, B, R, ...)                                                                                   \
+    do {                                                                                                           \
+        if (pass == 0) hipLaunchKernelGGL((KERNEL<B, R, true>), grid, dim3(256), 0, s, __VA_ARGS__);                 \
+        else hipLaunchKernelGGL((KERNEL<B, R, false>), grid, dim3(256), 0, s, __VA_ARGS__);                          \
+    } while (0)
+#define FTC_ID_ROUNDS(KERNEL, B, ...)                                                                               \
+    do {                                                                                                           \
+        if (rounds == 8) FTC_ID(KERNEL, B, 8, __VA_ARGS__);                                                         \
+        else if (rounds == 16) FTC_ID(KERNEL, B, 16, __VA_ARGS__);                                                  \
+        else FTC_ID(KERNEL, B, RX_ROUNDS_MANY, __VA_ARGS__);                                                        \
+    } while (0)
+#define FTC_ID_BITS(KERNEL, ...)                                                                                    \
+    do {                                                                                                           \
+        if (digit == 8) FTC_ID_ROUNDS(KERNEL, 8, __VA_ARGS__);                                                      \
+        else FTC_ID_ROUNDS(KERNEL, 9, __VA_ARGS__);                                                                 \
+    } while (0)
+    for (int pass = 0; pass < passes; ++pass) {
+        uint32_t *ko = k[pass & 1], *vo = v[pass & 1];
+        FTC_ID_BITS(id_hist_kernel, ki, vocab, static_cast<int64_t>(n), digit * pass, n_tiles, table);
+        hipLaunchKernelGGL(id_scan_kernel, dim3(1 << digit), dim3(256), 0, s, n_tiles, table, totals);
+        FTC_ID_BITS(id_scatter_kernel, ki, vi, vocab, static_cast<int64_t>(n), digit * pass, n_tiles, table, totals, ko, vo);
+        ki = *keys = ko;
+        vi = *order = vo;
+    }
+#undef FTC_ID_BITS
+#undef FTC_ID_ROUNDS
+#undef FTC_ID
+    return launch_status("id sort");
 }
 
 // ---- label propagation ---------------------------------------------------------------------------

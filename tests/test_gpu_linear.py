@@ -26,7 +26,7 @@ def layer(n, d_in, d_out, dtype, act, seed=0, bias=True, residual=True, ldx=None
     return X, W, b, R
 
 
-SIZES = [(1, 1, 1), (1, 1024, 300), (3, 8, 5), (17, 33, 65), (64, 64, 64), (65, 63, 67), (130, 100, 129), (200, 129, 40), (257, 520, 264), (5, 2000, 70),
+SIZES = [(1, 1, 1), (1, 1024, 300), (2, 5001, 33), (4, 700, 90), (2, 40, 17000), (3, 8, 5), (17, 33, 65), (64, 64, 64), (65, 63, 67), (130, 100, 129), (200, 129, 40), (257, 520, 264), (5, 2000, 70),
          (1500, 16, 9), (2, 7, 1030)]
 
 
