@@ -419,15 +419,16 @@ int32_t ftc_linear(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t
 
 /*
  * Backward of ftc_linear for dL/dZ = dZ (n x d_out, `dtype`): dP = dZ * slope (slope NULL: no activation),
- *   dX = dP * W^T (n x d_in, dx_dtype),  dW = X^T * dP (d_in x d_out, contiguous),  db = column sums of dP;
+ *   dX = dP * W^T + dX_add (n x d_in, dx_dtype),  dW = X^T * dP (d_in x d_out, contiguous),  db = column sums of dP;
  * dX, dW, db may each be NULL (not computed); dW and db are of dw_dtype; dx_dtype and dw_dtype are fp32 or `dtype`.
- * The gradient of the residual is dZ.  dP is rounded to `dtype` for the products, db sums it unrounded.
+ * dX_add (n x d_in of `dtype`, may be NULL) is what reaches X on another way, as through a residual connection around
+ * the layer; it may be dX itself (same pointer, leading dimension and type).  The gradient of the residual is dZ.  dP is rounded to `dtype` for the products, db sums it unrounded.
  */
 size_t ftc_linear_backward_workspace_bytes(int32_t n, int32_t d_in, int32_t d_out);
 int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W,
-                            int32_t d_out, const void *slope, int32_t lds, const void *dZ, int32_t lddz, void *dX,
-                            int32_t lddx, int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws,
-                            size_t ws_bytes, void *stream);
+                            int32_t d_out, const void *slope, int32_t lds, const void *dZ, int32_t lddz,
+                            const void *dX_add, int32_t ldda, void *dX, int32_t lddx, int32_t dx_dtype, void *dW,
+                            void *db, int32_t dw_dtype, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Attention inside every graph of a packed batch.  Graph g has the query rows q_ptr[g] .. q_ptr[g+1] of Q and out,

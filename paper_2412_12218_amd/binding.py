@@ -64,7 +64,7 @@ _SIGNATURES = {
     "ftc_linear_workspace_bytes": (_Z, [_I, _I, _I]),
     "ftc_linear": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _Z, _P]),
     "ftc_linear_backward_workspace_bytes": (_Z, [_I, _I, _I]),
-    "ftc_linear_backward": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _P, _Z, _P]),
+    "ftc_linear_backward": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _P, _Z, _P]),
     "ftc_graph_attention_workspace_bytes": (_Z, [_I, _I, _I, _I, _I, _I]),
     "ftc_graph_attention": (_I, [_I, _P, _I, _P, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _F, _P, _I, _P, _P, _Z, _P]),
     "ftc_graph_attention_backward_workspace_bytes": (_Z, [_I, _I, _I, _I, _I, _I]),
@@ -533,8 +533,8 @@ def ftc_linear(X, W, bias=None, act=FTC_ACT_NONE, residual=None, out=None, out_d
 
 
 def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_db=True, dX=None, dx_dtype=None, dW=None, db=None,
-                        dw_dtype=torch.float32, ws=None):
-    """(dX, dW, db); dX in X's type unless given; dW and db share a type (dw_dtype where they are not given)."""
+                        dw_dtype=torch.float32, dX_add=None, ws=None):
+    """(dX, dW, db); dX in X's type unless given, dX_add (may be dX) added to it; dW and db share a type (dw_dtype where they are not given)."""
     n, d_in = X.shape
     d_out = W.shape[1]
     if dX is None and want_dX:
@@ -546,7 +546,7 @@ def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_d
         db = torch.empty(d_out, dtype=wdt, device=X.device)
     if ws is None:
         ws = _workspace(lib().ftc_linear_backward_workspace_bytes(n, d_in, d_out), X.device)
-    stream = _here(X, W, dZ, slope, dX, dW, db, ws)
+    stream = _here(X, W, dZ, slope, dX_add, dX, dW, db, ws)
     _ld(W, d_in, d_out, X.dtype)
     if not W.is_contiguous() or (dW is not None and not dW.is_contiguous()):
         raise ValueError("W and dW must be contiguous")
@@ -557,7 +557,8 @@ def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_d
     sdt = torch.float32 if X.dtype == torch.float32 else torch.int16
     _check(lib().ftc_linear_backward(n, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(slope),
                                      _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(dZ), _ld(dZ, n, d_out, X.dtype),
-                                     _ptr(dX), _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
+                                     _ptr(dX_add), _ld(dX_add, n, d_in, X.dtype) if dX_add is not None else 0, _ptr(dX),
+                                     _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
                                      _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), stream))
     return dX, dW, db
 

@@ -884,8 +884,9 @@ size_t ftc_linear_backward_workspace_bytes(int32_t n, int32_t d_in, int32_t d_ou
 }
 
 int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W, int32_t d_out,
-                            const void *slope, int32_t lds, const void *dZ, int32_t lddz, void *dX, int32_t lddx,
-                            int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws, size_t ws_bytes, void *stream)
+                            const void *slope, int32_t lds, const void *dZ, int32_t lddz, const void *dX_add, int32_t ldda, void *dX,
+                            int32_t lddx, int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws, size_t ws_bytes,
+                            void *stream)
 {
     const char *who = "ftc_linear_backward";
     if (n < 0 || d_in < 1 || d_out < 1) return fail(FTC_EINVAL, "%s: negative n, or a width below 1", who);
@@ -900,6 +901,9 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
         if (dX) {
             FTC_TRY(check_dense(dX, lddx, dx_dtype, d_in, who, "dX"));
             FTC_TRY(check_out_type(who, "dX", dtype, dx_dtype));
+            if (dX_add) FTC_TRY(check_dense(dX_add, ldda, dtype, d_in, who, "dX_add"));
+            if (dX_add == dX && (ldda != lddx || dx_dtype != dtype))
+                return fail(FTC_EINVAL, "%s: dX on top of dX_add needs its leading dimension and type", who);
         }
     }
     if (dW) FTC_TRY(check_dense(dW, d_out, dw_dtype, d_out, who, "dW"));
@@ -914,7 +918,8 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
     }
     FTC_TRY(check_ws(who, linear_backward_ws(n, d_in, d_out), ws, ws_bytes));
     const LinearShape p = {n, d_in, d_out, dtype, X, W, nullptr, nullptr, const_cast<void *>(slope), nullptr, ldx, 0, lds, 0, FTC_ACT_NONE, dtype};
-    const LinearGrads g = {dZ, dX, dW, db, lddz, lddx, dx_dtype, dw_dtype};
+    if (dX_add && (dX_add == dW || dX_add == db)) return fail(FTC_EINVAL, "%s: an output aliases an input", who);
+    const LinearGrads g = {dZ, dX_add, dX, dW, db, lddz, ldda, lddx, dx_dtype, dw_dtype};
     return launch_linear_backward(p, g, ws, static_cast<hipStream_t>(stream));
 }
 

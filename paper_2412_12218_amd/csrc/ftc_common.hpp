@@ -194,9 +194,9 @@ struct LinearShape {
     int ldx, ldr, lds, ldz, act, z_dtype;
 };
 struct LinearGrads {
-    const void *dZ;
+    const void *dZ, *dX_add;
     void *dX, *dW, *db;
-    int lddz, lddx, dx_dtype, dw_dtype;
+    int lddz, ldda, lddx, dx_dtype, dw_dtype;
 };
 size_t linear_ws(int n, int d_in, int d_out);
 int32_t launch_linear(const LinearShape &p, void *ws, hipStream_t s);

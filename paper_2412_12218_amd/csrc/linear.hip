@@ -229,7 +229,7 @@ static void linear_backward_t(const LinearShape &p, const LinearGrads &g, void *
         DenseArgs a = {};
         a.A = G; a.lda = ldg; a.B = p.W; a.ldb = p.d_out;
         a.M = p.n; a.N = p.d_in; a.K = p.d_out;
-        a.out = g.dX; a.ldo = g.lddx; a.out_dtype = g.dx_dtype;
+        a.residual = g.dX_add; a.ldr = g.ldda; a.out = g.dX; a.ldo = g.lddx; a.out_dtype = g.dx_dtype;
         dense<false, false>(a, p.dtype, q, s);
     }
     if (g.dW) {

@@ -74,6 +74,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void dense_rows_across_kernel(DenseAr
 template <class T, int R, int EACH>
 __global__ __launch_bounds__(256) void dense_rows_along_kernel(DenseArgs a)
 {
+    constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
     const int lane = threadIdx.x & 63, col = (blockIdx.x * 4 + (threadIdx.x >> 6)) * EACH;
     if (col >= a.N) return;
     float acc[R][EACH];
@@ -107,7 +108,10 @@ __global__ __launch_bounds__(256) void dense_rows_along_kernel(DenseArgs a)
             float v = acc[r][e];
             v += __shfl_xor(v, 32, 64);
             v = group_sum_dpp<32>(v);
-            if (lane == r * EACH + e && r < a.M && col + e < a.N) store_elem(a.out, r * a.ldo + col + e, a.out_dtype, v);
+            if (lane == r * EACH + e && r < a.M && col + e < a.N) {
+                if (a.residual) v += load_elem(a.residual, r * a.ldr + col + e, DT);
+                store_elem(a.out, r * a.ldo + col + e, a.out_dtype, v);
+            }
         }
 }
 

@@ -1,6 +1,7 @@
 """Layer chaining of the two benchmark models (Section VI: 2-layer GCN with hidden size 16,
 4-layer AGNN with hidden size 32): HotPath is the forward pass the benchmark times, TrainPath
-the forward + backward pass of the same two models, PlannedGraph the per-graph adaptation that the
+the forward + backward pass of the same two models, GraphTransformerPath the forward + backward
+pass of a graph transformer on a batch of graphs, PlannedGraph the per-graph adaptation that the
 paper's outlook (Section VII) names: statistics of the graph decide how it is prepared.
 
 Every step is a call into libftc through `binding`; this module only owns the device
@@ -234,3 +235,74 @@ class TrainPath:
         d_h0, dbeta = self.agnn_backward(betas, d_h, first_in_f32=True)
         _, dW_in = B.ftc_update_gemm_backward(X, W_in, d_h0, Z=self.agnn_h0, want_dX=False, ws=self.ws)
         return dW_in, dW_out, dbeta
+
+
+class GraphTransformerPath:
+    """Forward + backward of a graph transformer on a packed batch of graphs: node features looked up by id, layers of attention
+    between all nodes of a graph and of a feed-forward block (GELU), each with a residual connection around it, and a linear
+    head on every node.  graph_ptr: device int32, the graphs' first nodes and the end (n); heads share kv_heads K/V heads.
+
+    Weights are a dict: "table" (vocab x d), "head" and "head_bias", and "layers", a list of dicts "qkv" (d x (heads + 2 kv_heads) d / heads),
+    "out" (d x d), "up" (d x hidden), "down" (hidden x d) with a bias each ("qkv_bias", ...).  Gradients come in the same shape, in fp32.
+    Buffers are allocated here once; forward() keeps in them what backward() needs."""
+
+    LINEAR = ("qkv", "out", "up", "down")
+
+    def __init__(self, graph_ptr, n, vocab, d=64, heads=4, kv_heads=None, hidden=None, n_out=8, layers=2, act_dtype=torch.float16):
+        dev, L = graph_ptr.device, B.lib()
+        if d % heads:
+            raise ValueError("d is a multiple of heads")
+        self.graph_ptr, self.n, self.vocab, self.d, self.heads, self.n_out = graph_ptr, n, vocab, d, heads, n_out
+        self.kv_heads = heads if kv_heads is None else kv_heads
+        self.head_dim, self.hidden, self.layers = d // heads, 4 * d if hidden is None else hidden, layers
+        self.scale = float(d) ** 0.5                 # of the looked-up rows, as with tables shared with an output layer
+        kd = self.kv_heads * self.head_dim
+        self.columns = (slice(0, d), slice(d, d + kd), slice(d + kd, d + 2 * kd))      # of q, k, v
+        act = lambda c: torch.empty((n, c), dtype=act_dtype, device=dev)
+        self.h = [act(d) for _ in range(layers + 1)]           # input of every layer, and of the head
+        self.qkv = [act(d + 2 * kd) for _ in range(layers)]
+        self.attended = [act(d) for _ in range(layers)]
+        self.lse = [torch.empty((n, heads), dtype=torch.float32, device=dev) for _ in range(layers)]
+        self.middle = [act(d) for _ in range(layers)]          # between attention and feed-forward block
+        self.up = [act(self.hidden) for _ in range(layers)]
+        self.slope = [B.slope_like(t) for t in self.up]
+        self.logits = act(n_out)
+        self.d_h, self.d_attended, self.d_up, self.d_qkv = act(d), act(d), act(self.hidden), act(d + 2 * kd)
+        shapes = [(d, d + 2 * kd), (d, d), (d, self.hidden), (self.hidden, d), (d, n_out)]
+        sizes = (n, n, graph_ptr.numel() - 1, heads, self.kv_heads, self.head_dim)
+        self.ws = B._workspace(max([L.ftc_graph_attention_workspace_bytes(*sizes), L.ftc_graph_attention_backward_workspace_bytes(*sizes),
+                                    L.ftc_embedding_backward_workspace_bytes(n, vocab, d)] +
+                                   [f(n, *s) for f in (L.ftc_linear_workspace_bytes, L.ftc_linear_backward_workspace_bytes) for s in shapes]), dev)
+
+    def _attention_args(self, layer, mask):
+        q, k, v = (self.qkv[layer][:, c] for c in self.columns)
+        return (q, k, v, self.graph_ptr, self.graph_ptr), dict(heads=self.heads, kv_heads=self.kv_heads, kv_mask=mask, ws=self.ws)
+
+    def forward(self, ids, weights, mask=None):
+        """Logits (n x n_out).  mask: nodes with 0 are attended to by no node."""
+        B.ftc_embedding(ids, weights["table"], scale=self.scale, out=self.h[0])
+        for i, w in enumerate(weights["layers"]):
+            B.ftc_linear(self.h[i], w["qkv"], bias=w["qkv_bias"], out=self.qkv[i], ws=self.ws)
+            args, kw = self._attention_args(i, mask)
+            B.ftc_graph_attention(*args, out=self.attended[i], lse=self.lse[i], **kw)
+            B.ftc_linear(self.attended[i], w["out"], bias=w["out_bias"], residual=self.h[i], out=self.middle[i], ws=self.ws)
+            B.ftc_linear(self.middle[i], w["up"], bias=w["up_bias"], act=B.FTC_ACT_GELU, out=self.up[i], slope=self.slope[i], ws=self.ws)
+            B.ftc_linear(self.up[i], w["down"], bias=w["down_bias"], residual=self.middle[i], out=self.h[i + 1], ws=self.ws)
+        return B.ftc_linear(self.h[-1], weights["head"], bias=weights["head_bias"], out=self.logits, ws=self.ws)
+
+    def backward(self, ids, weights, d_out, mask=None):
+        """d_out = dL/d(logits), in the activation type; gradients of the weights that forward() was given."""
+        grads, back = dict(layers=[{} for _ in weights["layers"]]), B.ftc_linear_backward
+        _, grads["head"], grads["head_bias"] = back(self.h[-1], weights["head"], d_out, dX=self.d_h, ws=self.ws)
+        for i in reversed(range(self.layers)):
+            w, g = weights["layers"][i], grads["layers"][i]
+            # d_h goes through both blocks of the layer: what their residual connections carry is added in place
+            _, g["down"], g["down_bias"] = back(self.up[i], w["down"], self.d_h, dX=self.d_up, ws=self.ws)
+            _, g["up"], g["up_bias"] = back(self.middle[i], w["up"], self.d_up, slope=self.slope[i], dX=self.d_h, dX_add=self.d_h, ws=self.ws)
+            _, g["out"], g["out_bias"] = back(self.attended[i], w["out"], self.d_h, dX=self.d_attended, ws=self.ws)
+            args, kw = self._attention_args(i, mask)
+            dq, dk, dv = (self.d_qkv[:, c] for c in self.columns)
+            B.ftc_graph_attention_backward(*args, self.attended[i], self.lse[i], self.d_attended, dQ=dq, dK=dk, dV=dv, **kw)
+            _, g["qkv"], g["qkv_bias"] = back(self.h[i], w["qkv"], self.d_qkv, dX=self.d_h, dX_add=self.d_h, ws=self.ws)
+        grads["table"] = B.ftc_embedding_backward(ids, self.d_h, self.vocab, scale=self.scale, ws=self.ws)
+        return grads

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2412_12218_amd import binding as B
-from transformer_reference import check, linear, linear_backward, slope_values
+from transformer_reference import check, f64, linear, linear_backward, slope_values
 
 pytestmark = pytest.mark.gpu
 DTYPES = [torch.float32, torch.float16, torch.bfloat16]
@@ -78,6 +78,22 @@ def test_parts_of_the_gradient():
     only = lambda **k: B.ftc_linear_backward(X, W, dZ, slope=slope, **{**dict(want_dX=False, want_dW=False, want_db=False), **k})
     assert torch.equal(only(want_dX=True)[0], dX) and torch.equal(only(want_dW=True)[1], dW) and torch.equal(only(want_db=True)[2], db)
     assert only() == (None, None, None)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [1, 3, 70])
+def test_gradient_beside_a_residual_connection(dtype, n):
+    """dX_add, apart from dX and in place: as the sum, which has one rounding more than the product."""
+    X, W, b, _ = layer(n, 40, 50, dtype, "none", residual=False)
+    dZ, add = matrix(n, 50, dtype, 5), matrix(n, 40, dtype, 6, ld=43)
+    only = dict(want_dW=False, want_db=False)
+    alone, bound = linear_backward(X, W, dZ, None, torch.float32, torch.float32)[0]
+    got = B.ftc_linear_backward(X, W, dZ, dX_add=add, dx_dtype=torch.float32, **only)[0]
+    want = alone + f64(add)
+    check(f"dX + residual {dtype} {n}", got, want, bound + 2 * 2.0 ** -24 * np.abs(want))
+    there = add.clone()
+    B.ftc_linear_backward(X, W, dZ, dX_add=there, dX=there, **only)
+    assert torch.equal(there, B.ftc_linear_backward(X, W, dZ, dX_add=add, **only)[0])
 
 
 @pytest.mark.parametrize("act", list(ACTS))

@@ -30,7 +30,7 @@ def linear(**k):
 
 
 def linear_backward(**k):
-    a = dict(n=4, X=P(1), ldx=8, dtype=1, d_in=8, W=P(2), d_out=16, slope=P(3), lds=16, dZ=P(4), ldz=16, dX=P(5), lddx=8, dxt=1, dW=P(6), db=P(7), dwt=0,
+    a = dict(n=4, X=P(1), ldx=8, dtype=1, d_in=8, W=P(2), d_out=16, slope=P(3), lds=16, dZ=P(4), ldz=16, add=None, lda=0, dX=P(5), lddx=8, dxt=1, dW=P(6), db=P(7), dwt=0,
              ws=P(8), bytes=BIG) | k
     return B.lib().ftc_linear_backward(*a.values(), None)
 
@@ -67,7 +67,8 @@ CASES = [
     (linear_backward, dict(n=-1), INVALID), (linear_backward, dict(d_in=0), INVALID), (linear_backward, dict(X=None), INVALID),
     (linear_backward, dict(W=None), INVALID), (linear_backward, dict(dZ=None), INVALID), (linear_backward, dict(lds=3), INVALID),
     (linear_backward, dict(lddx=3), INVALID), (linear_backward, dict(dtype=4), UNSUPPORTED), (linear_backward, dict(dxt=2), UNSUPPORTED),
-    (linear_backward, dict(dwt=2), UNSUPPORTED), (linear_backward, dict(dX=P(4)), INVALID), (linear_backward, dict(dW=P(2)), INVALID),
+    (linear_backward, dict(add=P(9), lda=7), INVALID), (linear_backward, dict(add=P(5), lda=9), INVALID), (linear_backward, dict(add=P(6), lda=8), INVALID),
+    (linear_backward, dict(add=P(5), lda=8, dxt=0), INVALID), (linear_backward, dict(dwt=2), UNSUPPORTED), (linear_backward, dict(dX=P(4)), INVALID), (linear_backward, dict(dW=P(2)), INVALID),
     (linear_backward, dict(db=P(6)), INVALID), (linear_backward, dict(ws=None), WORKSPACE), (linear_backward, dict(ws=C.c_void_p(0x80008)), ALIGN),
 ]
 for call in (attention, attention_backward):
@@ -103,7 +104,7 @@ def test_calls_without_work():
 
 def test_workspace_queries():
     L = B.lib()
-    assert L.ftc_embedding_backward_workspace_bytes(-1, 4, 4) == 0 and L.ftc_embedding_backward_workspace_bytes(1000, 5, 64) >= 1000 * 16
+    assert L.ftc_embedding_backward_workspace_bytes(-1, 4, 4) == 0 and L.ftc_embedding_backward_workspace_bytes(1000, 5, 64) >= 1000 * 8
     assert L.ftc_linear_workspace_bytes(4, 0, 4) == 0 and L.ftc_linear_backward_workspace_bytes(100, 10, 10) >= 100 * 10 * 2
     assert L.ftc_graph_attention_workspace_bytes(4, 4, 1, 3, 2, 8) == 0
     assert L.ftc_graph_attention_workspace_bytes(1, 100_000, 1, 8, 2, 64) >= 8 * 64 * 4 * 2
