@@ -16,7 +16,7 @@
 // dQ and dK / dV are sums over different axes; two kernels (seven products a pair for five) add them up in a fixed order, where one would need
 // atomics.  Few queries (keys) and long graphs: the other axis is split over workgroups, whose parts join_*() adds up, in order.
 //
-// Probabilities and ds are rounded to the type of the inputs for the second product; scores, softmax statistics and sums are fp32.
+// Probabilities and ds are rounded to the type of the inputs for the second product (ds_in_two() apart); scores, softmax statistics and sums are fp32.
 #pragma once
 #include "matrix_frag.hpp"
 
@@ -244,6 +244,22 @@ __device__ __forceinline__ Frag<T> operand_of(const f32x16 &c, int step)  // row
     for (int j = 0; j < 8; ++j) x[j] = step == 0 ? c[j] : c[8 + j];
     return frag_of<T>(x);
 }
+
+template <class T>
+__device__ __forceinline__ Frag<T> rest_of(const f32x16 &c, int step, const Frag<T> &rounded)  // what the rounding left of them
+{
+    float x[8], y[8];
+    frag_numbers<T>(rounded, y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (step == 0 ? c[j] : c[8 + j]) - y[j];
+    return frag_of<T>(x);
+}
+
+// ds adds up to zero over a row's keys, so with few columns its rounding shows more than that of the result: for D up to 32 in 16
+// bits its products take what the rounding left as a second operand (dQ against 64 bits, fp16, D = 8: 1.58 times the error of a result that
+// is only rounded, 1.1 so; the exponentials, not the matrix cores, bound these kernels).
+template <class T, int DP>
+constexpr bool ds_in_two() { return T::BYTES == 2 && DP == 32; }
 
 // Keys in a tile of the kernels whose waves own queries.
 template <class T, int NW>

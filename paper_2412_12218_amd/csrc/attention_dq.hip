@@ -1,7 +1,11 @@
 // Attention between all nodes of a graph: the kernel of dQ.  See attention_common.hpp.
 //
-// delta = <dO, out> carries the rounding of out.  Where one tile holds all keys of a graph it is the sum of p <dO, v> instead, in fp32,
-// which the dK / dV kernel then finds in its place: one key gives ds = 0 exactly, and few keys, whose ds is small against delta, lose nothing.
+// delta' = <dO, out> carries the rounding of a 16-bit out, which in dQ shows beside that of ds (D = 8, graphs of 65 to 140 nodes: 1.62 times
+// the error of a result that is only rounded; 1.5 without it).  What is wrong with it is the sum of ds, which should be zero:
+// delta = delta' + sum_j ds'_j, which the dK / dV kernel finds in its place, and dQ = scale (sum_j ds'_j k_j - (sum_j ds'_j) sum_j p_j k_j), for which
+// the kernels with D up to 32 add up p k in one more product (D = 64, 48 x 400 nodes: 1.46 times the error without and 1.43 with it, but
+// 75 and 93 us).  Where one tile holds all keys delta is the sum of
+// p <dO, v> from the start: one key gives ds = 0 exactly.
 #include "attention_common.hpp"
 
 namespace ftc {
@@ -46,9 +50,15 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
     const float lse = there ? a.lse[at] : -INFINITY;
     const float minus_lse2 = lse == -INFINITY ? -INFINITY : -lse * LOG2E;  // a row without keys has no probabilities
     float delta = there && tiles > 1 ? a.delta[at] : 0.f;
-    f32x16 dq[DT];
+    constexpr bool MEAN = ds_in_two<T, DP>();
+    f32x16 dq[DT], mean[MEAN ? DT : 1];  // mean: sum of p k
+    float rest = 0.f;                    // sum of ds (a half's keys)
 #pragma unroll
     for (int d = 0; d < DT; ++d) dq[d] = zero16();
+    if constexpr (MEAN) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) mean[d] = zero16();
+    }
 
     // p and <dO, v> of 32 keys
     auto scores = [&](const char *K, const char *V, const float *bias, int u, f32x16 &p, f32x16 &dp) {
@@ -91,12 +101,23 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
             f32x16 p, dp;
             scores(K, V, bias, u, p, dp);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) p[e] *= dp[e] - delta;
+            for (int e = 0; e < 16; ++e) {
+                dp[e] = p[e] * (dp[e] - delta);
+                if constexpr (MEAN) rest += dp[e];
+            }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const Frag<T> ds = operand_of<T>(p, k);
+                const Frag<T> ds = operand_of<T>(dp, k);
+                Frag<T> pf, low;
+                if constexpr (MEAN) pf = operand_of<T>(p, k);
+                if constexpr (ds_in_two<T, DP>()) low = rest_of<T>(dp, k, ds);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) mma<T>(dq[d], L::along_column(K + (32 * u + 16 * k) * L::ROW, 4 * half, 4 * half + 8, 32 * d), ds);
+                for (int d = 0; d < DT; ++d) {
+                    const Frag<T> kf = L::along_column(K + (32 * u + 16 * k) * L::ROW, 4 * half, 4 * half + 8, 32 * d);
+                    mma<T>(dq[d], kf, ds);
+                    if constexpr (ds_in_two<T, DP>()) mma<T>(dq[d], kf, low);
+                    if constexpr (MEAN) mma<T>(mean[d], kf, pf);
+                }
             }
         }
     };
@@ -122,6 +143,12 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
     get(first, Ks[0], Vs[0], biases[0]);
     put(first, Ks[0], Vs[0], biases[0]);
     for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
+    if (MEAN && tiles > 1 && a.splits == 1) {
+        rest = both_halves_sum(rest);
+        if (there && half == 0) a.delta[at] = delta + rest;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dq[d] -= rest * mean[MEAN ? d : 0];
+    }
     if (!there) return;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
