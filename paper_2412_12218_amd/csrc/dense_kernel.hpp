@@ -209,6 +209,29 @@ struct Operand {
     }
 };
 
+// A wave's blocks of an fp32 product once more, from memory and on the fp32 instruction, for the sums that the pieces left not finite.
+template <bool AX, bool BX, int WM, int WN>
+__device__ __forceinline__ void dense_again(const DenseArgs &a, int row0, int col0, int k_begin, int k_end, f32x16 (&c)[WM][WN])
+{
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const float *A = static_cast<const float *>(a.A), *B = static_cast<const float *>(a.B);
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int j = 0; j < WN; ++j) {
+            const int64_t row = min(row0 + 32 * i + (lane & 31), a.M - 1), col = min(col0 + 32 * j + (lane & 31), a.N - 1);
+            f32x16 sum = zero16();
+            for (int k0 = k_begin; k0 < k_end; k0 += 2) {
+                const int64_t k = k0 + half;
+                const bool in = k < k_end;
+                const float x = in ? A[AX ? k * a.lda + row : row * a.lda + k] : 0.f, y = in ? B[BX ? k * a.ldb + col : col * a.ldb + k] : 0.f;
+                sum = __builtin_amdgcn_mfma_f32_32x32x2f32(y, x, sum, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) c[i][j][e] = fabsf(c[i][j][e]) < INFINITY ? c[i][j][e] : sum[e];
+        }
+}
+
 // Which tile a workgroup has.  Workgroups go round the eight XCDs, each of which has an L2: every XCD gets a range of consecutive
 // tiles (the rest keep their place), in the order of bands of eight tile rows, column by column inside a band, so that the tiles at
 // work in an XCD share rows of A and columns of B.
@@ -253,10 +276,22 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             if (s + 1 < KS) read(s + 1);
+            if constexpr (T::BYTES == 4) {
+                Pieces pa[WM], pb[WN];
 #pragma unroll
-            for (int i = 0; i < WM; ++i)
+                for (int i = 0; i < WM; ++i) pa[i] = pieces_of(fa[s & 1][i]);
 #pragma unroll
-                for (int j = 0; j < WN; ++j) mma<T>(c[i][j], fb[s & 1][j], fa[s & 1][i]);
+                for (int j = 0; j < WN; ++j) pb[j] = pieces_of(fb[s & 1][j]);
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) mma(c[i][j], pb[j], pa[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) mma<T>(c[i][j], fb[s & 1][j], fa[s & 1][i]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -308,6 +343,16 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
             multiply(A0, B0);
             __syncthreads();
         }
+    }
+    if constexpr (T::BYTES == 4) {
+        bool finite = true;
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+            for (int j = 0; j < WN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) finite = finite && fabsf(c[i][j][e]) < INFINITY;
+        if (__builtin_amdgcn_ballot_w64(!finite)) dense_again<AX, BX, WM, WN>(a, m0 + wm, n0 + wn, k_begin, k_end, c);
     }
     // A wave's 32 rows through LDS, where no other wave looks any more: neighbouring lanes then have neighbouring columns.
     constexpr int WIDTH = 32 * WN, PITCH = WIDTH * 4 + 16, EIGHTS = WIDTH / 8;

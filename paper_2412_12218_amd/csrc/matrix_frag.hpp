@@ -85,6 +85,40 @@ __device__ __forceinline__ void mma(f32x16 &c, const Frag<T> &a, const Frag<T> &
     }
 }
 
+// An fp32 operand in three bf16 pieces, a = a1 + a2 + a3 (bf16_split.hpp: six of the nine products are exact in fp32 and what is left out is below an
+// fp32 rounding), for products at six sixteenths of the time of v_mfma_f32_32x32x2.  Numbers below 2^-110 are held to 2^-126.  Infinities, numbers that
+// round to one, and sums of pieces that overflow show as results that are not finite.
+struct Pieces {
+    Frag<BF16> p[3];
+};
+__device__ __forceinline__ Pieces pieces_of(const Frag<F32> &a)
+{
+    Pieces s;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x = a.f[2 * j], y = a.f[2 * j + 1];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector((frag_f32x2{x, y}), frag_bf16x2));
+            s.p[q].w[j] = w;
+            if (q < 2) {
+                x -= __uint_as_float(w << 16);
+                y -= __uint_as_float(w & 0xffff0000u);
+            }
+        }
+    }
+    return s;
+}
+__device__ __forceinline__ void mma(f32x16 &c, const Pieces &a, const Pieces &b)  // the smallest first
+{
+    mma<BF16>(c, a.p[1], b.p[1]);
+    mma<BF16>(c, a.p[2], b.p[0]);
+    mma<BF16>(c, a.p[0], b.p[2]);
+    mma<BF16>(c, a.p[1], b.p[0]);
+    mma<BF16>(c, a.p[0], b.p[1]);
+    mma<BF16>(c, a.p[0], b.p[0]);
+}
+
 // ---- global memory ----------------------------------------------------------------------------------------
 // 16 bytes (T::VEC elements) at element `idx`, aligned to an element; elements from `left` on are zero and not read.
 template <class T>

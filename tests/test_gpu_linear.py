@@ -145,6 +145,42 @@ def test_infinities_and_nan(dtype):
         assert s[0] == 1 and abs(s[1]) < 1e-6 and np.isnan(s[2]) and abs(s[3] - (0.0 if act == "relu" else 0.5)) < 1e-6, (act, s)
 
 
+@pytest.mark.parametrize("n,d_in,d_out", [(70, 64, 130), (300, 33, 65)])
+def test_fp32_numbers_that_bf16_pieces_do_not_hold(n, d_in, d_out):
+    """Infinities, the largest numbers, sums that overflow, and tiny numbers, in fp32: as a product in fp32 gives them.  A number below 2^-110
+    may be off by 2^-126."""
+    X, W, _, _ = layer(n, d_in, d_out, torch.float32, "none", residual=False, bias=False)
+    big = torch.finfo(torch.float32).max
+    X[1, 2], X[5, 7], X[9, 0], X[40, 3] = float("inf"), float("-inf"), big, -big * 0.999
+    W[5, 11], W[0, 3] = float("inf"), 0.5
+    W[2, 20] = 0.0                                             # inf * 0
+    X[50] = 0.0
+    X[50, 4] = 2.0 ** -140
+    X[51] *= 2.0 ** -120
+    x, w = f64(X), f64(W)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = x @ w
+        want[np.abs(want) > big] = np.inf * np.sign(want[np.abs(want) > big])
+        bound = (np.abs(x) @ np.abs(w)) * (d_in + 8) * 2.0 ** -24 + 2.0 ** -125 * np.abs(w).sum(0)
+    bound[~np.isfinite(want)] = 0
+    check("large and small numbers", B.ftc_linear(X, W), want, bound)
+    with np.errstate(invalid="ignore", over="ignore"):
+        dZ = matrix(n, d_out, torch.float32, 3)
+        dZ[2, 9] = float("inf")
+        g = f64(dZ)
+        wantX, wantW = g @ w.T, x.T @ g
+        for m in (wantX, wantW):
+            m[np.abs(m) > big] = np.inf * np.sign(m[np.abs(m) > big])
+        finite = np.isfinite(wantW)
+        boundW = (np.abs(x).T @ np.abs(g)) * (n + 8) * 2.0 ** -24 + 2.0 ** -125 * np.abs(g).sum(0)
+        boundX = (np.abs(g) @ np.abs(w.T)) * (d_out + 8) * 2.0 ** -24 + 2.0 ** -125 * np.abs(g).sum(1)[:, None]
+    boundW[~finite] = 0
+    boundX[~np.isfinite(wantX)] = 0
+    dX, dW, _ = B.ftc_linear_backward(X, W, dZ, want_db=False)
+    check("dX", dX, wantX, np.nan_to_num(boundX, nan=0.0, posinf=0.0))
+    check("dW", dW, wantW, np.nan_to_num(boundW, nan=0.0, posinf=0.0))
+
+
 def test_residual_in_place_and_empty():
     X, W, b, _ = layer(50, 30, 44, torch.bfloat16, "silu", residual=False)
     R = matrix(50, 44, torch.bfloat16, 5)
