@@ -50,10 +50,9 @@ inline bool dense_whole_pieces(const void *p, int64_t ld, int width, int dtype)
 #if defined(__HIPCC__)
 constexpr int SLOPE_BITS = 14;
 
-// act(p) and act'(p).  Infinite p: the limits.  For fp32 from the functions of the device library; for 16-bit results, which have 11 bits, from
-// one exponential and one reciprocal: Phi(-|p|) = exp(-p^2 / 2) (a1 t + .. + a5 t^5) / 2 with t = 1 / (1 + 0.3275911 |p| / sqrt 2), off by at most
-// 0.75e-7 (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26), and sigma(p) = 1 / (1 + exp(-p)).
-template <class T>
+// act(p) and act'(p), from one exponential and one reciprocal (a step of fp32 each).  Infinite p: the limits.
+//   Phi(-|p|) = exp(-p^2 / 2) (a1 t + .. + a5 t^5) / 2 with t = 1 / (1 + 0.3275911 |p| / sqrt 2), off by at most 0.75e-7, half a step of fp32 at
+//   one (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26); sigma(p) = 1 / (1 + exp(-p))
 __device__ __forceinline__ float activation(float p, int act, float &slope)
 {
     slope = 1.f;
@@ -63,24 +62,15 @@ __device__ __forceinline__ float activation(float p, int act, float &slope)
     }
     if (act == FTC_ACT_GELU) {
         const float q = p < -40.f ? -40.f : p > 40.f ? 40.f : p;
-        float cdf, density;
-        if constexpr (T::BYTES == 4) {
-            cdf = 0.5f * (1.f + erff(q * 0.70710678118654752f));
-            density = 0.39894228040143268f * expf(-0.5f * q * q);
-        } else {
-            const float e = __builtin_amdgcn_exp2f(q * q * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(fmaf(fabsf(q), 0.23164188f, 1.f));
-            const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-            cdf = q < 0.f ? tail : 1.f - tail;
-            density = 0.39894228040143268f * e;
-        }
-        slope = fmaf(q, density, cdf);
+        const float e = __builtin_amdgcn_exp2f(q * q * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(fmaf(fabsf(q), 0.23164188f, 1.f));
+        const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+        const float cdf = q < 0.f ? tail : 1.f - tail;
+        slope = fmaf(q * 0.39894228040143268f, e, cdf);
         return p > 40.f ? p : q * cdf;
     }
     if (act == FTC_ACT_SILU) {
         const float q = p < -80.f ? -80.f : p > 80.f ? 80.f : p;
-        float g;
-        if constexpr (T::BYTES == 4) g = 1.f / (1.f + expf(-q));
-        else g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(q * -1.4426950408889634f));
+        const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(q * -1.4426950408889634f));
         slope = g * fmaf(q, 1.f - g, 1.f);
         return p > 80.f ? p : p < -80.f ? 0.f : q * g;
     }
@@ -96,42 +86,74 @@ __device__ __forceinline__ float slope_value(int16_t c)
     return c == INT16_MIN ? __builtin_nanf("") : c * (1.f / (1 << SLOPE_BITS));
 }
 
-// Eight neighbouring numbers of a row of the result, `left` of them inside it; bias: theirs.
+// Eight neighbouring numbers of a row of the result, `left` of them inside it; bias: theirs.  Bias, activation and its slope.
 template <class T>
-__device__ __forceinline__ void epilogue(const DenseArgs &a, int row, int col, int left, const float (&bias)[8], float (&x)[8])
+__device__ __forceinline__ void activate(const DenseArgs &a, int row, int col, int left, const float (&bias)[8], float (&x)[8])
 {
     float slope[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] += bias[j];
-    if (a.act != FTC_ACT_NONE || a.slope) {  // uniform
+    if (a.act == FTC_ACT_NONE && !a.slope) return;  // uniform
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = activation<T>(x[j], a.act, slope[j]);
+    for (int j = 0; j < 8; ++j) x[j] = activation(x[j], a.act, slope[j]);
+    if (!a.slope) return;
+    if constexpr (T::BYTES == 4) {
+        store_eight_numbers(a.slope, row * a.lds + col, FTC_F32, left, slope);
+    } else {
+        int16_t *to = static_cast<int16_t *>(a.slope) + row * a.lds + col;
+        typedef int16_t s8 __attribute__((ext_vector_type(8), aligned(2)));
+        s8 code;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) code[j] = slope_code(slope[j]);
+        if (left >= 8) {
+            *reinterpret_cast<s8 *>(to) = code;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < left) to[j] = code[j];
+        }
     }
+}
+template <class T>
+__device__ __forceinline__ void epilogue(const DenseArgs &a, int row, int col, int left, const float (&bias)[8], float (&x)[8])
+{
+    activate<T>(a, row, col, left, bias, x);
     if (a.residual) {
         float add[8];
         load_eight_numbers<T>(a.residual, row * a.ldr + col, left, add);
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] += add[j];
     }
-    if (a.slope) {
-        if constexpr (T::BYTES == 4) {
-            store_eight_numbers(a.slope, row * a.lds + col, FTC_F32, left, slope);
-        } else {
-            int16_t *to = static_cast<int16_t *>(a.slope) + row * a.lds + col;
-            typedef int16_t s8 __attribute__((ext_vector_type(8), aligned(2)));
-            s8 code;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) code[j] = slope_code(slope[j]);
-            if (left >= 8) {
-                *reinterpret_cast<s8 *>(to) = code;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 7; ++j)
-                    if (j < left) to[j] = code[j];
-            }
-        }
-    }
     store_eight_numbers(a.out, row * a.ldo + col, a.out_dtype, left, x);
+}
+
+// Elements moved to places s lower (0 < s < VEC, or all of it), zeros behind; and those from n on zeros.
+template <class T>
+__device__ __forceinline__ void move_down(ftc_u32x4 &w, int s)
+{
+    if constexpr (T::BYTES == 2) {
+        if (s & 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (w[j] >> 16) | (j < 3 ? w[j + 1] << 16 : 0u);
+        }
+        s >>= 1;
+    }
+#pragma unroll
+    for (int b = 1; b <= 2; b *= 2)
+        if (s & b) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = j + b < 4 ? w[j + b] : 0u;
+        }
+    if (s >= 4) w = ftc_u32x4{0u, 0u, 0u, 0u};
+}
+template <class T>
+__device__ __forceinline__ void keep_first(ftc_u32x4 &w, int n)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (T::BYTES == 4) w[j] = j < n ? w[j] : 0u;
+        else w[j] = 2 * j + 1 < n ? w[j] : 2 * j < n ? w[j] & 0xffffu : 0u;
+    }
 }
 
 // One operand's tile: SIDE rows of the result's side and STEP of the contraction, staged by WAVES waves.
@@ -180,23 +202,44 @@ struct Operand {
         for (int e = 0; e < EACH; ++e) *reinterpret_cast<ftc_u32x4 *>(tile + (e * WAVES * 64 + static_cast<int>(threadIdx.x)) * 16) = w[e];
     }
 
-    // ---- through registers; `side`, `k_end`: where zeros begin
+    // ---- through registers; `side`, `k_end`: where zeros begin.  A piece that a row ends in is loaded as the last 16 bytes of the row, and
+    // its numbers move to their places when it is stored, so that no lane waits for its loads one by one
     ftc_u32x4 v[EACH];
-    __device__ __forceinline__ void load(const void *base, int64_t ld, int side0, int side, int k0, int k_end)
+    __device__ __forceinline__ void load(const void *base, int64_t ld, int side0, int side, int k0, int k_end, int width)
     {
-        const int row0 = ACROSS ? k0 : side0, rows = ACROSS ? k_end : side, col0 = ACROSS ? side0 : k0, cols = ACROSS ? side : k_end;
+        const int row0 = ACROSS ? k0 : side0, rows = ACROSS ? k_end : side, col0 = ACROSS ? side0 : k0;
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x), r = row0 + id / L::PIECES, c = col0 + id % L::PIECES * T::VEC;
-            v[e] = load_piece<T>(base, r * ld + c, r < rows ? cols - c : 0);
+            v[e] = ftc_u32x4{0u, 0u, 0u, 0u};
+            if (r < rows && c < width) {
+                RawVec<T, T::VEC> w;
+                load_raw_any<T>(base, r * ld + min(c, width - T::VEC), w);
+                v[e] = ftc_u32x4{w.w[0], w.w[1], w.w[2], w.w[3]};
+            }
         }
     }
-    __device__ __forceinline__ void store(char *tile) const
+    // the rows of an operand are shorter than a piece
+    __device__ __forceinline__ void load_short(const void *base, int64_t ld, int side0, int side, int k0, int k_end, int width)
     {
+        const int row0 = ACROSS ? k0 : side0, rows = ACROSS ? k_end : side, col0 = ACROSS ? side0 : k0;
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x);
-            L::store(tile, id / L::PIECES, id % L::PIECES, v[e]);
+            const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x), r = row0 + id / L::PIECES, c = col0 + id % L::PIECES * T::VEC;
+            v[e] = load_piece<T>(base, r * ld + c, r < rows ? width - c : 0);
+        }
+    }
+    // columns from `end` on (of the part of the contraction, where the rows run along it) are zeros; brief: after load_short()
+    __device__ __forceinline__ void store(char *tile, int side0, int k0, int k_end, int width, bool brief)
+    {
+        const int col0 = ACROSS ? side0 : k0, end = ACROSS ? width : k_end;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int id = e * WAVES * 64 + static_cast<int>(threadIdx.x), c = col0 + id % L::PIECES * T::VEC;
+            ftc_u32x4 w = v[e];
+            if (!brief && c + T::VEC > width) move_down<T>(w, c + T::VEC - width);
+            if (!ACROSS && c + T::VEC > end) keep_first<T>(w, end - c);
+            L::store(tile, id / L::PIECES, id % L::PIECES, w);
         }
     }
 
@@ -330,19 +373,34 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
             __syncthreads();
         }
     } else {
+        const int wa = AX ? a.M : a.K, wb = BX ? a.N : a.K;  // the operands' rows
+        const bool brief = wa < T::VEC || wb < T::VEC;
         auto load = [&](int k) {
-            oa.load(a.A, a.lda, m0, a.M, k, k_end);
-            ob.load(a.B, a.ldb, n0, a.N, k, k_end);
+            if (brief) {
+                oa.load_short(a.A, a.lda, m0, a.M, k, k_end, wa);
+                ob.load_short(a.B, a.ldb, n0, a.N, k, k_end, wb);
+            } else {
+                oa.load(a.A, a.lda, m0, a.M, k, k_end, wa);
+                ob.load(a.B, a.ldb, n0, a.N, k, k_end, wb);
+            }
         };
-        load(k_begin);
-        for (int k = k_begin; k < k_end; k += STEP) {
-            oa.store(A0);
-            ob.store(B0);
-            __syncthreads();
+        // one buffer is multiplied while the next step, loaded before, goes to the other
+        auto turn = [&](int k, const char *__restrict__ A, const char *__restrict__ B, char *__restrict__ An, char *__restrict__ Bn) {
             if (k + STEP < k_end) load(k + STEP);
-            multiply(A0, B0);
+            multiply(A, B);
+            if (k + STEP < k_end) {
+                oa.store(An, m0, k + STEP, k_end, wa, brief);
+                ob.store(Bn, n0, k + STEP, k_end, wb, brief);
+            }
             __syncthreads();
+        };
+        if (k_begin < k_end) {
+            load(k_begin);
+            oa.store(A0, m0, k_begin, k_end, wa, brief);
+            ob.store(B0, n0, k_begin, k_end, wb, brief);
         }
+        __syncthreads();
+        for (int k = k_begin, b = 0; k < k_end; k += STEP, b ^= 1) turn(k, b ? A1 : A0, b ? B1 : B0, b ? A0 : A1, b ? B0 : B1);
     }
     if constexpr (T::BYTES == 4) {
         bool finite = true;
@@ -371,14 +429,48 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
                 *reinterpret_cast<ftc_f32x4 *>(area + (lane & 31) * PITCH + (32 * j + 8 * b + 4 * (lane >> 5)) * 4) =
                     ftc_f32x4{c[i][j][4 * b], c[i][j][4 * b + 1], c[i][j][4 * b + 2], c[i][j][4 * b + 3]};
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 2
-        for (int r = lane / EIGHTS; r < 32; r += 64 / EIGHTS) {
-            const int row = m0 + wm + 32 * i + r;
+        constexpr int ROWS = 64 / EIGHTS, TURNS = 32 / ROWS;  // rows at a time
+        const int r0 = lane / EIGHTS, row0 = m0 + wm + 32 * i;
+        const bool adds = a.residual && a.splits == 1;
+        Frag<T> add[TURNS];  // all on their way while the activation is computed
+        if (adds) {
+#pragma unroll
+            for (int t = 0; t < TURNS; ++t) {
+                const int row = row0 + r0 + t * ROWS;
+                add[t] = load_frag<T>(a.residual, row * a.ldr + col, row < a.M ? left : 0);
+            }
+        }
+#pragma unroll 1
+        for (int r = r0; r < 32; r += ROWS) {
+            const int row = row0 + r;
             if (row >= a.M || left <= 0) break;
-            const ftc_f32x4 u = *reinterpret_cast<const ftc_f32x4 *>(area + r * PITCH + 32 * q), v = *reinterpret_cast<const ftc_f32x4 *>(area + r * PITCH + 32 * q + 16);
+            float *at = reinterpret_cast<float *>(area + r * PITCH + 32 * q);
+            const ftc_f32x4 u = *reinterpret_cast<const ftc_f32x4 *>(at), v = *reinterpret_cast<const ftc_f32x4 *>(at + 4);
             float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-            if (a.splits > 1) store_eight_numbers(a.part, (static_cast<int64_t>(blockIdx.y) * a.M + row) * a.N + col, FTC_F32, left, x);
-            else epilogue<T>(a, row, col, left, bias, x);
+            if (a.splits > 1) {
+                store_eight_numbers(a.part, (static_cast<int64_t>(blockIdx.y) * a.M + row) * a.N + col, FTC_F32, left, x);
+                continue;
+            }
+            activate<T>(a, row, col, left, bias, x);
+            if (adds) {  // back to where this lane took them from
+                *reinterpret_cast<ftc_f32x4 *>(at) = ftc_f32x4{x[0], x[1], x[2], x[3]};
+                *reinterpret_cast<ftc_f32x4 *>(at + 4) = ftc_f32x4{x[4], x[5], x[6], x[7]};
+            } else {
+                store_eight_numbers(a.out, row * a.ldo + col, a.out_dtype, left, x);
+            }
+        }
+        if (adds) {
+#pragma unroll
+            for (int t = 0; t < TURNS; ++t) {
+                const int r = r0 + t * ROWS, row = row0 + r;
+                if (row >= a.M || left <= 0) break;
+                const float *at = reinterpret_cast<const float *>(area + r * PITCH + 32 * q);
+                float x[8], y[8];
+                frag_numbers<T>(add[t], y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = at[j] + y[j];
+                store_eight_numbers(a.out, row * a.ldo + col, a.out_dtype, left, x);
+            }
         }
     }
 }

@@ -11,83 +11,102 @@
 
 namespace ftc {
 
-template <class T>
+// The parts' sums, eight columns of a row for LANES neighbouring lanes, which take the parts in turn.
+template <class T, int LANES>
 __global__ __launch_bounds__(256) void dense_join_kernel(DenseArgs a)
 {
-    const int eights = (a.N + 7) / 8;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (id >= static_cast<int64_t>(a.M) * eights) return;
-    const int row = static_cast<int>(id / eights), col = static_cast<int>(id % eights) * 8, left = a.N - col;
+    const int eights = (a.N + 7) / 8, z0 = threadIdx.x % LANES;
+    const int64_t id = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / LANES;
+    const bool there = id < static_cast<int64_t>(a.M) * eights;
+    const int row = there ? static_cast<int>(id / eights) : 0, col = there ? static_cast<int>(id % eights) * 8 : 0, left = a.N - col;
     float x[8], bias[8];
     load_eight_numbers<T>(a.bias, col, a.bias ? left : 0, bias);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = 0.f;
 #pragma unroll 4
-    for (int z = 0; z < a.splits; ++z) {
+    for (int z = z0; z < a.splits; z += LANES) {
         float v[8];
         load_eight_numbers<F32>(a.part, (static_cast<int64_t>(z) * a.M + row) * a.N + col, left, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] += v[j];
     }
-    epilogue<T>(a, row, col, left, bias, x);
+#pragma unroll
+    for (int m = 1; m < LANES; m *= 2)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] += __shfl_xor(x[j], m, 64);
+    if (there && z0 == 0) epilogue<T>(a, row, col, left, bias, x);
 }
 
-// dP = dZ act'(P) (dP NULL: not written) and, for BIAS_ROWS rows at a time, its column sums (sums NULL: none).  A thread has the 16
-// bytes of VEC columns of every eighth row.
-constexpr int BIAS_ROWS = 128;
+// dP = dZ act'(P) (dP NULL: not written) and, for the rows of a workgroup, its column sums (sums NULL: none).  2^log_lanes threads have the 16
+// bytes of VEC columns each of a row; a thread has DP_ROWS rows, all of them on their way at once.
+constexpr int DP_ROWS = 4;
+static int dp_lanes(int width, int vec)
+{
+    int b = 0;
+    while (b < 5 && (vec << b) < width) ++b;
+    return b;
+}
+static int dp_rows(int log_lanes) { return (256 >> log_lanes) * DP_ROWS; }  // of a workgroup
 template <class T>
 __global__ __launch_bounds__(256) void linear_dp_kernel(int n, int width, const void *__restrict__ dZ, int64_t ldz, const void *__restrict__ slope,
-                                                        int64_t lds, void *__restrict__ dP, float *__restrict__ sums)
+                                                        int64_t lds, void *__restrict__ dP, float *__restrict__ sums, int log_lanes)
 {
     constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16, V = T::VEC;
-    __shared__ float part[8][32 * V];
-    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5, col = (blockIdx.y * 32 + lane) * V, left = width - col;
-    const int row0 = blockIdx.x * BIAS_ROWS, row1 = row0 + min(n - row0, BIAS_ROWS);
+    __shared__ float part[256 * V];
+    const int lanes = 1 << log_lanes, groups = 256 >> log_lanes;
+    const int lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> log_lanes, col = (blockIdx.y * lanes + lane) * V, left = width - col;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * groups * DP_ROWS + sub;
+    ftc_u32x4 w[DP_ROWS], u[DP_ROWS];
+#pragma unroll
+    for (int i = 0; i < DP_ROWS; ++i) {
+        const int64_t row = row0 + i * groups;
+        w[i] = load_piece<T>(dZ, row * ldz + col, row < n ? left : 0);
+        if (slope) u[i] = load_piece<T>(slope, row * lds + col, row < n ? left : 0);
+    }
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.f;
-    if (left > 0) {
-#pragma unroll 4
-        for (int row = row0 + sub; row < row1; row += 8) {
-            const ftc_u32x4 w = load_piece<T>(dZ, row * ldz + col, left);
-            RawVec<T, V> r;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r.w[j] = w[j];
-            float g[V];
-            unpack<T, V>(r, g);
-            if (slope) {
-                const ftc_u32x4 u = load_piece<T>(slope, row * lds + col, left);
+    for (int i = 0; i < DP_ROWS; ++i) {
+        const int64_t row = row0 + i * groups;
+        RawVec<T, V> r;
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    if constexpr (T::BYTES == 4) g[j] *= __uint_as_float(u[j]);
-                    else g[j] *= slope_value(static_cast<int16_t>(u[j / 2] >> (16 * (j & 1))));
-                }
+        for (int j = 0; j < 4; ++j) r.w[j] = w[i][j];
+        float g[V];
+        unpack<T, V>(r, g);
+        if (slope) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if constexpr (T::BYTES == 4) g[j] *= __uint_as_float(u[i][j]);
+                else g[j] *= slope_value(static_cast<int16_t>(u[i][j / 2] >> (16 * (j & 1))));
             }
+        }
+        if (row >= n) continue;
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum[j] += g[j];
-            if (dP) {
-                const int64_t at = static_cast<int64_t>(row) * width + col;
-                if (left >= V) {
-                    store_vec_any<V>(dP, at, DT, g);
-                } else {
+        for (int j = 0; j < V; ++j) sum[j] += g[j];
+        if (dP && left > 0) {
+            const int64_t at = row * width + col;
+            if (left >= V) {
+                store_vec_any<V>(dP, at, DT, g);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < V - 1; ++j)
-                        if (j < left) store_elem(dP, at + j, DT, g[j]);
-                }
+                for (int j = 0; j < V - 1; ++j)
+                    if (j < left) store_elem(dP, at + j, DT, g[j]);
             }
         }
     }
     if (!sums) return;
 #pragma unroll
-    for (int j = 0; j < V; ++j) part[sub][lane * V + j] = sum[j];
+    for (int j = 0; j < V; ++j) part[(sub * lanes + lane) * V + j] = sum[j];
     __syncthreads();
-    const int c = blockIdx.y * 32 * V + threadIdx.x;
-    if (static_cast<int>(threadIdx.x) < 32 * V && c < width) {
-        float x = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x += part[k][threadIdx.x];
-        sums[static_cast<int64_t>(blockIdx.x) * width + c] = x;
+    // halves of the rows' sums onto the other half, in the same order every time
+    const int columns = lanes * V;
+    for (int half = groups / 2; half > 0; half /= 2) {
+        for (int i = threadIdx.x; i < half * columns; i += 256) part[i] += part[i + half * columns];
+        __syncthreads();
     }
+    for (int i = threadIdx.x; i < columns; i += 256)
+        if (blockIdx.y * columns + i < static_cast<unsigned>(width)) sums[static_cast<int64_t>(blockIdx.x) * width + blockIdx.y * columns + i] = part[i];
 }
 
 // db = sum of the rows' sums: 16 columns a workgroup, 16 threads a column.
@@ -97,7 +116,7 @@ __global__ __launch_bounds__(256) void linear_db_kernel(int parts, int width, co
     const int c = threadIdx.x & 15, sub = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     float x = 0.f;
     if (col < width) {
-#pragma unroll 4
+#pragma unroll 8
         for (int p = sub; p < parts; p += 16) x += sums[static_cast<int64_t>(p) * width + col];
     }
     part[sub][c] = x;
@@ -125,28 +144,30 @@ static int64_t dense_tiles(int M, int N, int tile) { return static_cast<int64_t>
 // has a compute unit to itself and `shared` for each of the workgroups of one that is full, `most` of them; parts cost the second kernel, and
 // writing and reading them once.  us, from products of 8192^3 (1780 with tiles of 64 / 1080 of 128 / 900 of 256), 4096 x 1024 x 1024 (16 / 15 / 31
 // for Z, 22 / 25 / 30 for dW at the best number of parts), 20 000 x 768 x 768 (40 / 34 / 30, 52 / 49 / 50) and 65 536 x 1024 x 4096
-// (852 / 652 / 582, 1000 / 596 / 485), the last two with parts of up to 16 tried: more lose (4096 x 1024 x 1024, dW of 2 / 4 / 8 / 16 parts: 28 / 25 / 27 / 39).
+// (852 / 652 / 582, 1000 / 596 / 485), the last two with parts of up to 16 tried: more lose (4096 x 1024 x 1024, dW of 2 / 4 / 8 / 16 parts: 28 / 25 / 27 / 39).  fp32, tiles of 64 / 128:
+// 16 384 x 2048 x 2048 1069 / 748, 1032 x 3696 x 2920 209 / 180, 2708 x 1432 x 128 21 (four parts) / 25 (six).
 struct DenseCost {
     float alone, shared;
     int most;
 };
-static DensePlan dense_plan(int M, int N, int K, bool f32, bool large)
+static DensePlan dense_plan(int M, int N, int K, bool f32, bool fast)
 {
-    static constexpr DenseCost cost[2][3] = {{{0.45f, 0.22f, 5}, {0.79f, 0.53f, 2}, {1.74f, 1.74f, 1}}, {{0.55f, 0.44f, 4}, {1.75f, 1.75f, 2}, {0.f, 0.f, 0}}};
+    static constexpr DenseCost cost[2][3] = {{{0.45f, 0.22f, 5}, {0.79f, 0.53f, 2}, {1.74f, 1.74f, 1}}, {{0.75f, 0.49f, 4}, {1.55f, 1.46f, 2}, {0.f, 0.f, 0}}};
     constexpr float JOIN_US = 5.f, PART_BYTES_US = 4e6f;
     DensePlan best = {DENSE_64, 1, 64};
     if (M < 1 || N < 1 || K < 1) return best;
     float least = INFINITY;
     const int step = f32 ? 32 : 64;
-    for (int tile = DENSE_64; tile <= (large && !f32 ? DENSE_256 : DENSE_128); ++tile) {
+    for (int tile = DENSE_64; tile <= (fast && !f32 ? DENSE_256 : DENSE_128); ++tile) {
         const DenseCost &c = cost[f32][tile];
+        const float alone = fast ? c.alone : 1.5f * c.alone;  // rows that are not whole pieces: through registers
         const int64_t tiles = dense_tiles(M, N, tile);
         for (int want = 1; want <= 64; want = want < 8 ? want + 1 : want + want / 4) {
             DensePlan p = {tile, 1, static_cast<int>(align_up(ceil_div(K, want), 64))};
             p.splits = ceil_div(K, p.k_each);
             if (p.splits != want) continue;
             const int64_t groups = tiles * p.splits, room = 256ll * c.most, full = groups / room, rest = groups % room;
-            const auto each = [&](int64_t n) { return n * c.shared > c.alone ? n * c.shared : c.alone; };
+            const auto each = [&](int64_t n) { return n * c.shared > alone ? n * c.shared : alone; };
             float us = ceil_div(p.k_each, step) * (full * each(c.most) + (rest ? each((rest + 255) / 256) : 0.f));
             if (p.splits > 1) us += JOIN_US + 8.f * p.splits * M * N / PART_BYTES_US;
             if (us < least) {
@@ -161,8 +182,8 @@ static DensePlan dense_plan(int M, int N, int K, bool f32, bool large)
 static size_t dense_ws(int M, int N, int K)
 {
     int most = 1;
-    for (int v = 0; v < 3; ++v) {
-        const DensePlan p = dense_plan(M, N, K, v == 0, v == 2);
+    for (int v = 0; v < 4; ++v) {
+        const DensePlan p = dense_plan(M, N, K, v & 1, v & 2);
         if (p.splits > most) most = p.splits;
     }
     return most > 1 ? align_up(static_cast<size_t>(most) * M * N * sizeof(float), 256) : 0;
@@ -182,16 +203,29 @@ static void dense(DenseArgs a, int dtype, void *ws, hipStream_t s)
     a.part = static_cast<float *>(ws);
     launch_dense<AX, BX>(a, dtype, p.tile, s);
     if (p.splits > 1) {
-        const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(a.M) * ceil_div(a.N, 8) + 255) / 256));
-        if (dtype == FTC_F32) hipLaunchKernelGGL(dense_join_kernel<F32>, grid, dim3(256), 0, s, a);
-        else if (dtype == FTC_F16) hipLaunchKernelGGL(dense_join_kernel<F16>, grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL(dense_join_kernel<BF16>, grid, dim3(256), 0, s, a);
+        // a lane a result where there are many, eight for a few results of many parts
+        const int64_t results = static_cast<int64_t>(a.M) * ceil_div(a.N, 8);
+        const bool many = results >= (1 << 15) || p.splits < 8;
+        const dim3 grid(static_cast<unsigned>(((many ? results : 8 * results) + 255) / 256));
+#define FTC_JOIN(T)                                                                                \
+    do {                                                                                           \
+        if (many) hipLaunchKernelGGL((dense_join_kernel<T, 1>), grid, dim3(256), 0, s, a);          \
+        else hipLaunchKernelGGL((dense_join_kernel<T, 8>), grid, dim3(256), 0, s, a);               \
+    } while (0)
+        if (dtype == FTC_F32) FTC_JOIN(F32);
+        else if (dtype == FTC_F16) FTC_JOIN(F16);
+        else FTC_JOIN(BF16);
+#undef FTC_JOIN
     }
 }
 
 size_t linear_ws(int n, int d_in, int d_out) { return dense_ws(n, d_out, d_in); }
 
-static size_t linear_sums_bytes(int n, int d_out) { return align_up(static_cast<size_t>(ceil_div(n, BIAS_ROWS)) * d_out * sizeof(float), 256); }
+static size_t linear_sums_bytes(int n, int d_out)
+{
+    const int rows = dp_rows(dp_lanes(d_out, 4));  // those of fp32 are at most as many as those of 16 bits
+    return align_up(static_cast<size_t>(ceil_div(n, rows)) * d_out * sizeof(float), 256);
+}
 
 size_t linear_backward_ws(int n, int d_in, int d_out)
 {
@@ -216,15 +250,16 @@ static void linear_backward_t(const LinearShape &p, const LinearGrads &g, void *
     char *q = static_cast<char *>(ws);
     void *dP = q; q += align_up(static_cast<size_t>(p.n) * p.d_out * sizeof(float), 256);
     float *sums = reinterpret_cast<float *>(q); q += linear_sums_bytes(p.n, p.d_out);
+    const int lanes = dp_lanes(p.d_out, T::VEC), parts = ceil_div(p.n, dp_rows(lanes));
     const void *G = p.slope ? dP : g.dZ;
     const int64_t ldg = p.slope ? p.d_out : g.lddz;
     if (p.slope || g.db) {
-        const dim3 grid(ceil_div(p.n, BIAS_ROWS), ceil_div(p.d_out, 32 * T::VEC));
+        const dim3 grid(parts, ceil_div(p.d_out, T::VEC << lanes));
         if (p.n > 0) hipLaunchKernelGGL(linear_dp_kernel<T>, grid, dim3(256), 0, s, p.n, p.d_out, g.dZ, static_cast<int64_t>(g.lddz), p.slope,
-                           static_cast<int64_t>(p.lds), p.slope ? dP : nullptr, g.db ? sums : nullptr);
+                           static_cast<int64_t>(p.lds), p.slope ? dP : nullptr, g.db ? sums : nullptr, lanes);
     }
     if (g.db)
-        hipLaunchKernelGGL(linear_db_kernel, dim3(ceil_div(p.d_out, 16)), dim3(256), 0, s, ceil_div(p.n, BIAS_ROWS), p.d_out, sums, g.db, g.dw_dtype);
+        hipLaunchKernelGGL(linear_db_kernel, dim3(ceil_div(p.d_out, 16)), dim3(256), 0, s, parts, p.d_out, sums, g.db, g.dw_dtype);
     if (g.dX && p.n > 0) {
         DenseArgs a = {};
         a.A = G; a.lda = ldg; a.B = p.W; a.ldb = p.d_out;
