@@ -57,33 +57,46 @@ __device__ __forceinline__ void split_row(const AttnArgs &a, int row, int &query
 }
 
 // Tile b of the tiles of all graphs: graph g has its tiles from [ptr[g] mult / rows] + g on, which leaves room for the rows of
-// every graph without a pass over the lengths.  Wave-uniform; a 64-way search.  -1: no graph.
+// every graph without a pass over the lengths.  Wave-uniform.  The 63 graphs around the place where b is among `tiles` are looked at first: it is one of
+// them where the graphs' sizes are alike, and small graphs have little else to wait for.  Else a 64-way search.
 struct Tile {
-    int graph, index;
+    int graph, index, begin, end;  // graph -1: none; begin, end: ptr of the graph
 };
 __device__ __forceinline__ int clamped(const int *ptr, int i, int n)
 {
     const int v = ptr[i];
     return v < 0 ? 0 : v > n ? n : v;
 }
-__device__ __forceinline__ Tile find_tile(const int *__restrict__ ptr, int graphs, int n, int mult, int rows, int b)
+template <int ROWS>
+__device__ __forceinline__ Tile find_tile(const int *__restrict__ ptr, int graphs, int n, int mult, int b, int tiles)
 {
     const int lane = threadIdx.x & 63;
-    auto start = [&](int g) { return static_cast<int>(static_cast<int64_t>(clamped(ptr, g, n)) * mult / rows) + g; };
-    int lo = 0, hi = graphs;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64, g = lo + lane * step;
-        const uint64_t below = __builtin_amdgcn_ballot_w64(g < hi && start(g) <= b);
-        const int count = __popcll(below);
-        const int next = lo + (count > 0 ? count - 1 : 0) * step;
-        hi = min(hi, next + step);
-        lo = next;
-    }
+    auto start = [&](int p, int g) { return static_cast<int>(static_cast<uint64_t>(p) * mult / ROWS) + g; };
+    int lo = static_cast<int>(static_cast<int64_t>(b) * graphs / tiles) - 31;
+    lo = max(min(lo, graphs - 63), 0);
     Tile t;
-    const int s = start(lo);
-    t.graph = __builtin_amdgcn_readfirstlane(s <= b ? lo : -1);
-    t.index = __builtin_amdgcn_readfirstlane(b - s);
-    return t;
+    for (int first = 0, end = graphs;;) {  // the graph is in [first, end), if there is one; twice at most
+        const int g = min(lo + lane, graphs), p = clamped(ptr, g, n), s = start(p, g);
+        const uint64_t below = __builtin_amdgcn_ballot_w64(g < end && s <= b);
+        const int last = below ? 63 - __builtin_clzll(below) : -1;
+        if ((last >= 0 || lo == first) && last < 63) {  // lane 63 does not know its graph's end
+            const int at = max(last, 0);
+            t.begin = __builtin_amdgcn_readlane(p, at);
+            t.end = __builtin_amdgcn_readlane(p, min(at + 1, 63));
+            t.index = b - __builtin_amdgcn_readlane(s, at);
+            t.graph = last >= 0 ? lo + at : -1;
+            return t;
+        }
+        if (last < 0) end = lo;
+        else first = lo + 63;
+        while (end - first > 63) {
+            const int step = (end - first + 63) / 64, h = first + lane * step;
+            const uint64_t under = __builtin_amdgcn_ballot_w64(h < end && start(clamped(ptr, h, n), h) <= b);
+            first += max(__popcll(under) - 1, 0) * step;
+            end = min(end, first + step);
+        }
+        lo = first;
+    }
 }
 
 // A tile of ROWS rows in LDS, and this thread's pieces of it: piece number e * threads + thread, as it lies there.

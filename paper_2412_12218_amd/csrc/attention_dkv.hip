@@ -26,11 +26,12 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
     __shared__ __align__(16) float lses[2][TQ], deltas[2][TQ];
     const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % NW, set = (threadIdx.x >> 6) / NW, col = lane & 31, half = lane >> 5;
     const Place here = place_of(a);
-    const Tile tile = find_tile(a.kv_ptr, a.graphs, a.n_kv, 1, TK, here.tile);
+    const Tile tile = find_tile<TK>(a.kv_ptr, a.graphs, a.n_kv, 1, here.tile, a.tiles);
     if (tile.graph < 0) return;
-    const int k0 = clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
+    const int k0 = tile.begin, k1 = tile.end;
     if (k1 <= k0 || static_cast<int64_t>(tile.index) * TK >= k1 - k0) return;
-    const int q0 = clamped(a.q_ptr, tile.graph, a.n_q), q1 = clamped(a.q_ptr, tile.graph + 1, a.n_q);
+    const bool same = a.kv_ptr == a.q_ptr && a.n_kv == a.n_q;  // uniform
+    const int q0 = same ? k0 : clamped(a.q_ptr, tile.graph, a.n_q), q1 = same ? k1 : clamped(a.q_ptr, tile.graph + 1, a.n_q);
     const int rows = max(q1 - q0, 0) * a.group, tiles = (rows + TQ - 1) / TQ;
     const int each = (tiles + a.splits - 1) / a.splits, first = here.part * each, last = min(tiles, first + each);
 

@@ -10,6 +10,9 @@
 
 namespace ftc {
 
+template <class T, int DP, int NW>
+constexpr bool scores_kept() { return key_rows<T, NW>() == 32 || DP == 32; }
+
 template <class T, int DP, int NW, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void attention_dq_kernel(AttnArgs a)
 {
@@ -20,12 +23,13 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
     __shared__ __align__(16) float biases[2][TK];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
     const Place here = place_of(a);
-    const Tile tile = find_tile(a.q_ptr, a.graphs, a.n_q, a.group, TQ, here.tile);
+    const Tile tile = find_tile<TQ>(a.q_ptr, a.graphs, a.n_q, a.group, here.tile, a.tiles);
     if (tile.graph < 0) return;
-    const int q0 = clamped(a.q_ptr, tile.graph, a.n_q), q1 = clamped(a.q_ptr, tile.graph + 1, a.n_q);
+    const int q0 = tile.begin, q1 = tile.end;
     const int rows = (q1 - q0) * a.group;
     if (q1 <= q0 || static_cast<int64_t>(tile.index) * TQ >= rows) return;
-    const int k0 = clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
+    const bool same = a.kv_ptr == a.q_ptr && a.n_kv == a.n_q;  // uniform
+    const int k0 = same ? q0 : clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = same ? q1 : clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
     const int keys = max(k1 - k0, 0), tiles = (keys + TK - 1) / TK;
     const int each = (tiles + a.splits - 1) / a.splits, first = here.part * each, last = min(tiles, first + each);
 
@@ -76,48 +80,62 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
             for (int i = 0; i < 4; ++i) p[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(p[4 * b + i], scale2, w[i] + minus_lse2));
         }
     };
-    auto attend = [&](const char *K, const char *V, const float *bias) {
-        if (tiles == 1) {
-            float sum = 0.f, d = 0.f;
-#pragma unroll 1
-            for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 1
-                for (int u = 0; u < SUB; ++u) {
-                    f32x16 p, dp;
-                    scores(K, V, bias, u, p, dp);
+    // delta of a row whose keys are all here, from p and <dO, v> of SUB 32 keys, which are kept where they fit in registers
+    auto settle = [&](auto get_scores) {
+        float sum = 0.f, d = 0.f;
+        f32x16 p, dp;
+#pragma unroll (scores_kept<T, DP, NW>() ? key_rows<T, NW>() / 32 : 1)
+        for (int u = 0; u < SUB; ++u) {
+            get_scores(u, p, dp);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        if (pass == 0) sum += p[e];
-                        else d = p[e] != 0.f ? fmaf(p[e] / sum, dp[e], d) : d;
-                    }
-                }
-                if (pass == 0) sum = both_halves_sum(sum);
-            }
-            delta = both_halves_sum(d);
-            if (there && half == 0) a.delta[at] = delta;
+            for (int e = 0; e < 16; ++e) sum += p[e];
+        }
+        sum = both_halves_sum(sum);
+#pragma unroll (scores_kept<T, DP, NW>() ? key_rows<T, NW>() / 32 : 1)
+        for (int u = 0; u < SUB; ++u) {
+            get_scores(u, p, dp);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) d = p[e] != 0.f ? fmaf(p[e] / sum, dp[e], d) : d;
+        }
+        delta = both_halves_sum(d);
+        if (there && half == 0) a.delta[at] = delta;
+    };
+    auto gather = [&](const char *K, int u, const f32x16 &p, f32x16 &ds) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            ds[e] = p[e] * (ds[e] - delta);
+            if constexpr (MEAN) rest += ds[e];
         }
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            f32x16 p, dp;
-            scores(K, V, bias, u, p, dp);
+        for (int k = 0; k < 2; ++k) {
+            const Frag<T> df = operand_of<T>(ds, k);
+            Frag<T> pf, low;
+            if constexpr (MEAN) pf = operand_of<T>(p, k);
+            if constexpr (ds_in_two<T, DP>()) low = rest_of<T>(ds, k, df);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                dp[e] = p[e] * (dp[e] - delta);
-                if constexpr (MEAN) rest += dp[e];
+            for (int d = 0; d < DT; ++d) {
+                const Frag<T> kf = L::along_column(K + (32 * u + 16 * k) * L::ROW, 4 * half, 4 * half + 8, 32 * d);
+                mma<T>(dq[d], kf, df);
+                if constexpr (ds_in_two<T, DP>()) mma<T>(dq[d], kf, low);
+                if constexpr (MEAN) mma<T>(mean[d], kf, pf);
             }
+        }
+    };
+    auto attend = [&](const char *K, const char *V, const float *bias) {
+        if constexpr (scores_kept<T, DP, NW>()) {
+            f32x16 p[SUB], dp[SUB];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const Frag<T> ds = operand_of<T>(dp, k);
-                Frag<T> pf, low;
-                if constexpr (MEAN) pf = operand_of<T>(p, k);
-                if constexpr (ds_in_two<T, DP>()) low = rest_of<T>(dp, k, ds);
+            for (int u = 0; u < SUB; ++u) scores(K, V, bias, u, p[u], dp[u]);
+            if (tiles == 1) settle([&](int u, f32x16 &x, f32x16 &y) { x = p[u]; y = dp[u]; });
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const Frag<T> kf = L::along_column(K + (32 * u + 16 * k) * L::ROW, 4 * half, 4 * half + 8, 32 * d);
-                    mma<T>(dq[d], kf, ds);
-                    if constexpr (ds_in_two<T, DP>()) mma<T>(dq[d], kf, low);
-                    if constexpr (MEAN) mma<T>(mean[d], kf, pf);
-                }
+            for (int u = 0; u < SUB; ++u) gather(K, u, p[u], dp[u]);
+        } else {
+            if (tiles == 1) settle([&](int u, f32x16 &x, f32x16 &y) { scores(K, V, bias, u, x, y); });
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                f32x16 p, dp;
+                scores(K, V, bias, u, p, dp);
+                gather(K, u, p, dp);
             }
         }
     };

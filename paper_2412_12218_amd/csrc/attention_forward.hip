@@ -16,12 +16,13 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
     __shared__ __align__(16) float biases[2][TK];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
     const Place here = place_of(a);
-    const Tile tile = find_tile(a.q_ptr, a.graphs, a.n_q, a.group, TQ, here.tile);
+    const Tile tile = find_tile<TQ>(a.q_ptr, a.graphs, a.n_q, a.group, here.tile, a.tiles);
     if (tile.graph < 0) return;
-    const int q0 = clamped(a.q_ptr, tile.graph, a.n_q), q1 = clamped(a.q_ptr, tile.graph + 1, a.n_q);
+    const int q0 = tile.begin, q1 = tile.end;
     const int rows = (q1 - q0) * a.group;  // virtual rows of the graph
     if (q1 <= q0 || static_cast<int64_t>(tile.index) * TQ >= rows) return;
-    const int k0 = clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
+    const bool same = a.kv_ptr == a.q_ptr && a.n_kv == a.n_q;  // uniform
+    const int k0 = same ? q0 : clamped(a.kv_ptr, tile.graph, a.n_kv), k1 = same ? q1 : clamped(a.kv_ptr, tile.graph + 1, a.n_kv);
     const int keys = max(k1 - k0, 0), tiles = (keys + TK - 1) / TK;
     const int each = (tiles + a.splits - 1) / a.splits, first = here.part * each, last = min(tiles, first + each);
 

@@ -4,30 +4,51 @@
 
 namespace ftc {
 
-// Adds up the parts of the forward pass, one wave a query and head.  Rows that belong to no graph stay as they are.
-template <class T>
+// Adds up the parts of the forward pass, WAVES waves a query and head, which take the parts in turn; at most 64 parts, lane z has the maximum
+// and the sum of part z.  Rows that belong to no graph stay as they are.
+template <class T, int WAVES>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
 {
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6), all = static_cast<int64_t>(a.n_q) * a.heads;
-    const int lane = threadIdx.x & 63;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, mine = wave % WAVES;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / WAVES) + wave / WAVES, all = static_cast<int64_t>(a.n_q) * a.heads;
     if (row >= all) return;
     const int query = static_cast<int>(row / a.heads), head = static_cast<int>(row % a.heads);
-    if (!in_a_graph(a.q_ptr, a.graphs, a.n_q, query)) return;
-    float m = -INFINITY;
-    for (int z = 0; z < a.splits; ++z) m = fmaxf(m, a.part_ml[2 * (z * all + row)]);
-    const float shift = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int z = 0; z < a.splits; ++z) {
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (z * all + row));
-        l += ml.y * __builtin_amdgcn_exp2f(ml.x - shift);
-    }
+    if (!in_a_graph(a.q_ptr, a.graphs, a.n_q, query)) return;  // of WAVES = 4 the whole workgroup
+    float2 ml = {-INFINITY, 0.f};
+    if (lane < a.splits) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (lane * all + row));
+    float m = ml.x;
+#pragma unroll
+    for (int b = 1; b < 64; b *= 2) m = fmaxf(m, __shfl_xor(m, b, 64));
+    const float shift = m == -INFINITY ? 0.f : m, weight = __builtin_amdgcn_exp2f(ml.x - shift);
+    float l = ml.y * weight;
+#pragma unroll
+    for (int b = 1; b < 64; b *= 2) l += __shfl_xor(l, b, 64);
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
-    for (int c = lane; c < a.D; c += 64) {
-        float x = 0.f;
-        for (int z = 0; z < a.splits; ++z)
-            x = fmaf(a.part[(z * all + row) * a.D + c], __builtin_amdgcn_exp2f(a.part_ml[2 * (z * all + row)] - shift), x);
-        store_elem(a.out, query * a.ldo + head * a.D + c, DT, x * inv);
+    __shared__ float sums[WAVES][128];
+    float x[2] = {0.f, 0.f};  // columns lane and lane + 64
+#pragma unroll 8
+    for (int z = mine; z < a.splits; z += WAVES) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), __builtin_amdgcn_readfirstlane(z)));
+        const float *part = a.part + (z * all + row) * a.D;
+        x[0] = fmaf(part[lane < a.D ? lane : 0], w, x[0]);
+        if (a.D > 64) x[1] = fmaf(part[lane + 64 < a.D ? lane + 64 : 0], w, x[1]);
+    }
+    if constexpr (WAVES > 1) {
+        sums[mine][lane] = x[0];
+        sums[mine][lane + 64] = x[1];
+        __syncthreads();
+        if (mine > 0) return;
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) {
+            x[0] += sums[k][lane];
+            x[1] += sums[k][lane + 64];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = lane + 64 * k;
+        if (c < a.D) store_elem(a.out, query * a.ldo + head * a.D + c, DT, x[k] * inv);
     }
     if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
@@ -67,21 +88,25 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(const float *__restr
     const int row = static_cast<int>(id / width), c = static_cast<int>(id % width);
     if (id >= static_cast<int64_t>(n) * width || !in_a_graph(ptr, graphs, n, row)) return;
     float x = 0.f;
+#pragma unroll 8
     for (int z = 0; z < splits; ++z) x += part[z * stride + id];
     constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
     store_elem(out, row * ld + c, DT, x);
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
-// Waves of a workgroup: one where a graph's rows are hardly more than a wave's, else four.
-static int attn_waves(int64_t rows, int graphs) { return rows <= 48ll * graphs ? 1 : 4; }
+// Waves of a workgroup: one where a graph has about two waves' rows at most, else four.  us of the forward and backward passes with one and four, 100 000
+// nodes, 8 heads, bf16: D = 32, graphs of 30 nodes 62 / 120 and 238 / 544, of 60 65 / 72 and 238 / 335, of 100 73 / 65 and 292 / 279; D = 64,
+// of 60 114 / 132 and 428 / 541, of 100 141 / 117 and 568 / 419.
+static int attn_waves(int64_t rows, int graphs) { return rows <= 64ll * graphs ? 1 : 4; }
 static int attn_tiles(int64_t rows, int graphs, int waves) { return static_cast<int>(rows / (32 * waves)) + graphs; }
-// Parts of the other axis where there are fewer workgroups than two for each compute unit; a part is four tiles at least.
+// Parts of the other axis where there are fewer waves than eight for each compute unit; a part is four tiles at least.
 static int attn_splits(int64_t rows, int64_t other, int graphs, int kv_heads)
 {
-    const int64_t groups = static_cast<int64_t>(attn_tiles(rows, graphs, attn_waves(rows, graphs))) * kv_heads;
+    const int nw = attn_waves(rows, graphs);
+    const int64_t groups = static_cast<int64_t>(attn_tiles(rows, graphs, nw)) * kv_heads;
     if (groups < 1) return 1;
-    const int64_t want = (512 + groups - 1) / groups, most = other / 256;
+    const int64_t want = (2048 / nw + groups - 1) / groups, most = other / 256;
     const int64_t s = want < most ? want : most;
     return static_cast<int>(s < 1 ? 1 : s > 64 ? 64 : s);
 }
@@ -110,6 +135,13 @@ static unsigned attn_grid(AttnArgs &a, int64_t rows, int nw)
     return static_cast<unsigned>(a.tiles) * a.kv_heads * a.splits;
 }
 
+#define FTC_ATTN_TYPED_N(KERNEL, N, GRID, ...)                                                                         \
+    do {                                                                                                               \
+        const dim3 grid__(static_cast<unsigned>(GRID));                                                                \
+        if (dtype == FTC_F32) hipLaunchKernelGGL((KERNEL<F32, N>), grid__, dim3(256), 0, s, __VA_ARGS__);               \
+        else if (dtype == FTC_F16) hipLaunchKernelGGL((KERNEL<F16, N>), grid__, dim3(256), 0, s, __VA_ARGS__);          \
+        else hipLaunchKernelGGL((KERNEL<BF16, N>), grid__, dim3(256), 0, s, __VA_ARGS__);                               \
+    } while (0)
 #define FTC_ATTN_TYPED(KERNEL, GRID, ...)                                                                              \
     do {                                                                                                               \
         const dim3 grid__(static_cast<unsigned>(GRID));                                                                \
@@ -128,7 +160,8 @@ static void forward(AttnArgs a, int dtype, void *ws, hipStream_t s)
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + align_up(static_cast<size_t>(a.splits) * rows * a.D * sizeof(float), 256));
     const unsigned grid = attn_grid(a, virt, nw);
     launch_attention_forward(a, dtype, nw, whole, grid, s);
-    if (a.splits > 1) FTC_ATTN_TYPED(attention_join_kernel, (rows + 3) / 4, a);
+    if (a.splits >= 16) FTC_ATTN_TYPED_N(attention_join_kernel, 4, rows, a);
+    else if (a.splits > 1) FTC_ATTN_TYPED_N(attention_join_kernel, 1, (rows + 3) / 4, a);
 }
 
 static void backward(AttnArgs a, int dtype, void *ws, hipStream_t s)
