@@ -7,8 +7,8 @@
 
 namespace ftc {
 
-template <class T, int DP>
-constexpr int query_rows() { return T::BYTES == 2 ? 64 : 32; }
+template <class T, int NW>
+constexpr int query_rows() { return T::BYTES == 2 && NW > 1 ? 64 : 32; }
 
 // Sets of waves that share the keys.
 template <class T, int DP, int NW>
@@ -18,12 +18,12 @@ template <class T, int DP, int NW, bool WHOLE>
 __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (wave_sets<T, DP, NW>()) == 1 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
 {
     constexpr int SETS = wave_sets<T, DP, NW>(), THREADS = 64 * NW * SETS;
-    constexpr int TK = 32 * NW, TQ = query_rows<T, DP>(), SUB = TQ / 32 / SETS, KS = DP / 16, DT = DP / 32;
+    constexpr int TK = 32 * NW, TQ = query_rows<T, NW>(), SUB = TQ / 32 / SETS, KS = DP / 16, DT = DP / 32, BUFFERS = tile_buffers<NW>();
     typedef LdsTile<T, DP> L;
     typedef Rows<T, DP, TQ, THREADS, WHOLE> R;
     typedef Rows<T, DP, TK, THREADS, WHOLE> KeyRows;
-    __shared__ __align__(16) char Qs[2][R::BYTES], Gs[2][R::BYTES], Ks[SETS == 2 ? KeyRows::BYTES : 16], Vs[SETS == 2 ? KeyRows::BYTES : 16];
-    __shared__ __align__(16) float lses[2][TQ], deltas[2][TQ];
+    __shared__ __align__(16) char Qs[BUFFERS][R::BYTES], Gs[BUFFERS][R::BYTES], Ks[SETS == 2 ? KeyRows::BYTES : 16], Vs[SETS == 2 ? KeyRows::BYTES : 16];
+    __shared__ __align__(16) float lses[BUFFERS][TQ], deltas[BUFFERS][TQ];
     const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % NW, set = (threadIdx.x >> 6) / NW, col = lane & 31, half = lane >> 5;
     const Place here = place_of(a);
     const Tile tile = find_tile<TK>(a.kv_ptr, a.graphs, a.n_kv, 1, here.tile, a.tiles);
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
         }
         __syncthreads();
     };
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < BUFFERS; ++b) {
         R::clear(Qs[b], a.D);
         R::clear(Gs[b], a.D);
     }
@@ -198,16 +198,25 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
             gather(Q, G, u0, p0, ds0);
         }
     };
-    // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
-    auto turn = [&](int t, const char *__restrict__ Q, const char *__restrict__ G, const float *__restrict__ row_lse,
-                    const float *__restrict__ row_delta, char *__restrict__ Qn, char *__restrict__ Gn, float *__restrict__ lse_n,
-                    float *__restrict__ delta_n) {
-        get(t + 1, Qn, Gn);
-        attend(Q, G, row_lse, row_delta);
-        put(t + 1, Qn, Gn, lse_n, delta_n);
-    };
-    put(first, Qs[0], Gs[0], lses[0], deltas[0]);
-    for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Qs[b], Gs[b], lses[b], deltas[b], Qs[b ^ 1], Gs[b ^ 1], lses[b ^ 1], deltas[b ^ 1]);
+    if constexpr (BUFFERS == 1) {
+        for (int t = first; t < last; ++t) {
+            if (t > first) get(t, Qs[0], Gs[0]);
+            put(t, Qs[0], Gs[0], lses[0], deltas[0]);
+            attend(Qs[0], Gs[0], lses[0], deltas[0]);
+            __syncthreads();
+        }
+    } else {
+        // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
+        auto turn = [&](int t, const char *__restrict__ Q, const char *__restrict__ G, const float *__restrict__ row_lse,
+                        const float *__restrict__ row_delta, char *__restrict__ Qn, char *__restrict__ Gn, float *__restrict__ lse_n,
+                        float *__restrict__ delta_n) {
+            get(t + 1, Qn, Gn);
+            attend(Q, G, row_lse, row_delta);
+            put(t + 1, Qn, Gn, lse_n, delta_n);
+        };
+        put(first, Qs[0], Gs[0], lses[0], deltas[0]);
+        for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Qs[b], Gs[b], lses[b], deltas[b], Qs[b ^ 1], Gs[b ^ 1], lses[b ^ 1], deltas[b ^ 1]);
+    }
     if constexpr (SETS == 2) {  // dK, then dV of the second set, where the queries were
         static_assert(sizeof(Qs) + sizeof(Gs) >= NW * DT * 4 * 1024, "room for a sum of every wave");
         auto add = [&](f32x16(&sum)[DT]) {

@@ -9,11 +9,11 @@ namespace ftc {
 template <class T, int DP, int NW, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void attention_forward_kernel(AttnArgs a)
 {
-    constexpr int TQ = 32 * NW, TK = key_rows<T, NW>(), SUB = TK / 32, KS = DP / 16, DT = DP / 32;
+    constexpr int TQ = 32 * NW, TK = key_rows<T, NW>(), SUB = TK / 32, KS = DP / 16, DT = DP / 32, BUFFERS = tile_buffers<NW>();
     typedef LdsTile<T, DP> L;
     typedef Keys<T, DP, TK, 64 * NW, WHOLE> Tiles;
-    __shared__ __align__(16) char Ks[2][Tiles::BYTES], Vs[2][Tiles::BYTES];
-    __shared__ __align__(16) float biases[2][TK];
+    __shared__ __align__(16) char Ks[BUFFERS][Tiles::BYTES], Vs[BUFFERS][Tiles::BYTES];
+    __shared__ __align__(16) float biases[BUFFERS][TK];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
     const Place here = place_of(a);
     const Tile tile = find_tile<TQ>(a.q_ptr, a.graphs, a.n_q, a.group, here.tile, a.tiles);
@@ -100,19 +100,27 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         if (t < last) next.put(K, V, bias);
         __syncthreads();
     };
-    // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
-    auto turn = [&](int t, const char *__restrict__ K, const char *__restrict__ V, const float *__restrict__ bias, char *__restrict__ Kn,
-                    char *__restrict__ Vn, float *__restrict__ bias_n) {
-        get(t + 1, Kn, Vn, bias_n);
-        attend(K, V, bias, a.mask || (t + 1) * TK > keys);
-        put(t + 1, Kn, Vn, bias_n);
-    };
-    Tiles::clear(a, Ks[0], Vs[0]);
-    Tiles::clear(a, Ks[1], Vs[1]);
+    for (int b = 0; b < BUFFERS; ++b) Tiles::clear(a, Ks[b], Vs[b]);
     if (WHOLE && a.D < DP) __syncthreads();
-    get(first, Ks[0], Vs[0], biases[0]);
-    put(first, Ks[0], Vs[0], biases[0]);
-    for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
+    if constexpr (BUFFERS == 1) {
+        for (int t = first; t < last; ++t) {
+            get(t, Ks[0], Vs[0], biases[0]);
+            put(t, Ks[0], Vs[0], biases[0]);
+            attend(Ks[0], Vs[0], biases[0], a.mask || (t + 1) * TK > keys);
+            __syncthreads();
+        }
+    } else {
+        // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
+        auto turn = [&](int t, const char *__restrict__ K, const char *__restrict__ V, const float *__restrict__ bias, char *__restrict__ Kn,
+                        char *__restrict__ Vn, float *__restrict__ bias_n) {
+            get(t + 1, Kn, Vn, bias_n);
+            attend(K, V, bias, a.mask || (t + 1) * TK > keys);
+            put(t + 1, Kn, Vn, bias_n);
+        };
+        get(first, Ks[0], Vs[0], biases[0]);
+        put(first, Ks[0], Vs[0], biases[0]);
+        for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
+    }
     l = both_halves_sum(l);
     m *= scale2;
     if (!there) return;
