@@ -95,18 +95,23 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(const float *__restr
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
-// Waves of a workgroup: one where a graph has about two waves' rows at most, else four.  us of the forward and backward passes with one and four, 100 000
-// nodes, 8 heads, bf16: D = 32, graphs of 30 nodes 62 / 120 and 238 / 544, of 60 65 / 72 and 238 / 335, of 100 73 / 65 and 292 / 279; D = 64,
-// of 60 114 / 132 and 428 / 541, of 100 141 / 117 and 568 / 419.
-static int attn_waves(int64_t rows, int graphs) { return rows <= 64ll * graphs ? 1 : 4; }
-static int attn_tiles(int64_t rows, int graphs, int waves) { return static_cast<int>(rows / (32 * waves)) + graphs; }
-// Parts of the other axis where there are fewer waves than eight for each compute unit; a part is four tiles at least.
-static int attn_splits(int64_t rows, int64_t other, int graphs, int kv_heads)
+// Waves of a workgroup: one for short graphs, whose rows would not fill four, else four, which share the other side's tiles.  us of the forward and
+// backward passes with one and four, 50 000 nodes, 8 heads: bf16, D = 64, graphs of 80 nodes 49 / 59 and 197 / 220, of 100 57 / 52 and 223 / 198,
+// of 160 60 / 66 and 232 / 237, of 300 97 / 80 and 309 / 267; fp32, D = 16, of 160 100 / 124 and 339 / 429.  With D = 128, where K, V and
+// their gradients leave a SIMD one wave, of 160 135 / 135 and 710 / 579.
+static int attn_waves(int64_t rows, int64_t other, int graphs, int D)
 {
-    const int nw = attn_waves(rows, graphs);
+    const int64_t most = (D <= 64 ? 160ll : 64ll) * graphs;
+    return rows <= 64ll * graphs || (rows <= most && other <= most) ? 1 : 4;
+}
+static int attn_tiles(int64_t rows, int graphs, int waves) { return static_cast<int>(rows / (32 * waves)) + graphs; }
+// Parts of the other axis where there are fewer waves than eight for each compute unit; a part of a graph of the mean size is four tiles at least.
+static int attn_splits(int64_t rows, int64_t other, int graphs, int kv_heads, int D)
+{
+    const int nw = attn_waves(rows, other, graphs, D);
     const int64_t groups = static_cast<int64_t>(attn_tiles(rows, graphs, nw)) * kv_heads;
-    if (groups < 1) return 1;
-    const int64_t want = (2048 / nw + groups - 1) / groups, most = other / 256;
+    if (groups < 1 || graphs < 1) return 1;
+    const int64_t want = (2048 / nw + groups - 1) / groups, most = other / graphs / 256;
     const int64_t s = want < most ? want : most;
     return static_cast<int>(s < 1 ? 1 : s > 64 ? 64 : s);
 }
@@ -114,7 +119,7 @@ static int attn_splits(int64_t rows, int64_t other, int graphs, int kv_heads)
 size_t attention_ws(int n_q, int n_kv, int graphs, int heads, int kv_heads, int D)
 {
     const int64_t rows = static_cast<int64_t>(n_q) * heads;
-    const int s = attn_splits(static_cast<int64_t>(n_q) * (heads / kv_heads), n_kv, graphs, kv_heads);
+    const int s = attn_splits(static_cast<int64_t>(n_q) * (heads / kv_heads), n_kv, graphs, kv_heads, D);
     if (s == 1) return 0;
     return align_up(static_cast<size_t>(s) * rows * D * sizeof(float), 256) + align_up(static_cast<size_t>(s) * rows * 2 * sizeof(float), 256);
 }
@@ -122,7 +127,7 @@ size_t attention_ws(int n_q, int n_kv, int graphs, int heads, int kv_heads, int 
 size_t attention_backward_ws(int n_q, int n_kv, int graphs, int heads, int kv_heads, int D)
 {
     const int64_t rows = static_cast<int64_t>(n_q) * heads, group = heads / kv_heads;
-    const int sq = attn_splits(n_q * group, n_kv, graphs, kv_heads), sk = attn_splits(n_kv, n_q * group, graphs, kv_heads);
+    const int sq = attn_splits(n_q * group, n_kv, graphs, kv_heads, D), sk = attn_splits(n_kv, n_q * group, graphs, kv_heads, D);
     const size_t parts_q = sq > 1 ? static_cast<size_t>(sq) * rows * D * sizeof(float) : 0;
     const size_t parts_k = sk > 1 ? static_cast<size_t>(sk) * 2 * n_kv * kv_heads * D * sizeof(float) : 0;
     return align_up(static_cast<size_t>(rows) * sizeof(float), 256) + align_up(parts_q > parts_k ? parts_q : parts_k, 256);
@@ -154,8 +159,8 @@ static void forward(AttnArgs a, int dtype, void *ws, hipStream_t s)
 {
     const int64_t rows = static_cast<int64_t>(a.n_q) * a.heads, virt = static_cast<int64_t>(a.n_q) * a.group;
     const bool whole = attn_whole(a.Q, a.ldq, a.D, dtype) && attn_whole(a.K, a.ldk, a.D, dtype) && attn_whole(a.V, a.ldv, a.D, dtype);
-    const int nw = attn_waves(virt, a.graphs);
-    a.splits = attn_splits(virt, a.n_kv, a.graphs, a.kv_heads);
+    const int nw = attn_waves(virt, a.n_kv, a.graphs, a.D);
+    a.splits = attn_splits(virt, a.n_kv, a.graphs, a.kv_heads, a.D);
     a.part = static_cast<float *>(ws);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + align_up(static_cast<size_t>(a.splits) * rows * a.D * sizeof(float), 256));
     const unsigned grid = attn_grid(a, virt, nw);
@@ -173,8 +178,8 @@ static void backward(AttnArgs a, int dtype, void *ws, hipStream_t s)
     a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + align_up(static_cast<size_t>(rows) * sizeof(float), 256));
     if (rows > 0) {
         FTC_ATTN_TYPED(attention_delta_kernel, (rows + 15) / 16, a);
-        const int nw = attn_waves(virt, a.graphs);
-        a.splits = attn_splits(virt, a.n_kv, a.graphs, a.kv_heads);
+        const int nw = attn_waves(virt, a.n_kv, a.graphs, a.D);
+        a.splits = attn_splits(virt, a.n_kv, a.graphs, a.kv_heads, a.D);
         const unsigned grid = attn_grid(a, virt, nw);
         launch_attention_dq(a, dtype, nw, whole, grid, s);
         const int width = a.heads * a.D;
@@ -182,8 +187,8 @@ static void backward(AttnArgs a, int dtype, void *ws, hipStream_t s)
         if (a.splits > 1) FTC_ATTN_TYPED(attention_sum_kernel, (count + 255) / 256, a.part, count, a.splits, a.q_ptr, a.graphs, a.n_q, width, a.dQ, a.lddq);
     }
     if (a.n_kv > 0) {
-        const int nw = attn_waves(a.n_kv, a.graphs);
-        a.splits = attn_splits(a.n_kv, virt, a.graphs, a.kv_heads);
+        const int nw = attn_waves(a.n_kv, virt, a.graphs, a.D);
+        a.splits = attn_splits(a.n_kv, virt, a.graphs, a.kv_heads, a.D);
         const unsigned grid = attn_grid(a, a.n_kv, nw);
         launch_attention_dkv(a, dtype, nw, whole, grid, s);
         const int width = a.kv_heads * a.D;
