@@ -139,7 +139,14 @@ struct Rows {
                                                  (lds_ptr)(tile + e * THREADS * 16 + wave * 1024), 16, 0, 0);
             }
         } else {
-            v[e] = load_piece<T>(base, at, D - col(e));
+            // the last piece of a row is the last 16 bytes of the row; put() moves them, so that no load is waited for here
+            if (D < T::VEC) {
+                v[e] = load_piece<T>(base, at, D - col(e));
+            } else {
+                RawVec<T, T::VEC> r;
+                load_raw_any<T>(base, at - max(col(e) + T::VEC - D, 0), r);
+                v[e] = ftc_u32x4{r.w[0], r.w[1], r.w[2], r.w[3]};
+            }
         }
     }
     __device__ __forceinline__ void get_zeros(char *tile, int e)
@@ -147,11 +154,14 @@ struct Rows {
         if constexpr (WHOLE) *place(tile, e) = ftc_u32x4{0u, 0u, 0u, 0u};
         else v[e] = ftc_u32x4{0u, 0u, 0u, 0u};
     }
-    __device__ __forceinline__ void put(char *tile) const
+    __device__ __forceinline__ void put(char *tile, int D)
     {
         if constexpr (!WHOLE) {
 #pragma unroll
-            for (int e = 0; e < EACH; ++e) *place(tile, e) = v[e];
+            for (int e = 0; e < EACH; ++e) {
+                if (D >= T::VEC && col(e) + T::VEC > D) move_down<T>(v[e], col(e) + T::VEC - D);
+                *place(tile, e) = v[e];
+            }
         }
     }
 };
@@ -165,8 +175,19 @@ __device__ __forceinline__ const char *head_of(const void *p, int64_t row, int64
 template <class T, bool WHOLE>
 __device__ __forceinline__ Frag<T> operand_at(const char *row, int c, int D, bool there)
 {
-    if constexpr (!WHOLE) return load_frag<T>(row, c, there ? D - c : 0);
     Frag<T> a;
+    if constexpr (!WHOLE) {
+        const ftc_u32x4 x = load_piece_of_row<T>(row, c, D);
+        if constexpr (T::BYTES == 4) {
+            const ftc_u32x4 y = load_piece_of_row<T>(row, c + 4, D);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { a.f[j] = there ? __uint_as_float(x[j]) : 0.f; a.f[4 + j] = there ? __uint_as_float(y[j]) : 0.f; }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a.w[j] = there ? x[j] : 0u;
+        }
+        return a;
+    }
     if constexpr (T::BYTES == 4) {
         const bool x_ok = there && c < D, y_ok = there && c + 4 < D;
         const ftc_f32x4 x = *reinterpret_cast<const ftc_f32x4 *>(row + (x_ok ? c : 0) * 4), y = *reinterpret_cast<const ftc_f32x4 *>(row + (y_ok ? c + 4 : 0) * 4);
@@ -235,10 +256,10 @@ struct Keys {
         }
         if (WHOLE && static_cast<int>(threadIdx.x) < TK) bias[threadIdx.x] = mine;
     }
-    __device__ __forceinline__ void put(char *K, char *V, float *bias) const
+    __device__ __forceinline__ void put(const AttnArgs &a, char *K, char *V, float *bias)
     {
-        k.put(K);
-        v.put(V);
+        k.put(K, a.D);
+        v.put(V, a.D);
         if (!WHOLE && static_cast<int>(threadIdx.x) < TK) bias[threadIdx.x] = mine;
     }
 };

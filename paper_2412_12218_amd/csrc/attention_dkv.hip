@@ -81,8 +81,8 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
     };
     auto put = [&](int t, char *Q, char *G, float *row_lse, float *row_delta) {
         if (t < last) {
-            qs.put(Q);
-            gs.put(G);
+            qs.put(Q, a.D);
+            gs.put(G, a.D);
             if (static_cast<int>(threadIdx.x) < TQ) {
                 row_lse[threadIdx.x] = my_lse;
                 row_delta[threadIdx.x] = my_delta;
@@ -116,8 +116,8 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
                 vr.get_zeros(Vs, e);
             }
         }
-        kr.put(Ks);
-        vr.put(Vs);
+        kr.put(Ks, a.D);
+        vr.put(Vs, a.D);
     } else {
         const char *k_row = head_of<T>(a.K, seen ? key : k0, a.ldk, here.share * a.D), *v_row = head_of<T>(a.V, seen ? key : k0, a.ldv, here.share * a.D);
 #pragma unroll

@@ -14,7 +14,7 @@ template <class T, int DP, int NW>
 constexpr bool scores_kept() { return key_rows<T, NW>() == 32 || DP == 32; }
 
 template <class T, int DP, int NW, bool WHOLE>
-__global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void attention_dq_kernel(AttnArgs a)
+__global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 1 : 2) void attention_dq_kernel(AttnArgs a)
 {
     constexpr int TQ = 32 * NW, TK = key_rows<T, NW>(), SUB = TK / 32, KS = DP / 16, DT = DP / 32, BUFFERS = tile_buffers<NW>();
     typedef LdsTile<T, DP> L;
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         next.look(a, k0 + (t + 1) * TK, k1);
     };
     auto put = [&](int t, char *K, char *V, float *bias) {
-        if (t < last) next.put(K, V, bias);
+        if (t < last) next.put(a, K, V, bias);
         __syncthreads();
     };
     for (int b = 0; b < BUFFERS; ++b) Tiles::clear(a, Ks[b], Vs[b]);

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         next.look(a, k0 + (t + 1) * TK, k1);
     };
     auto put = [&](int t, char *K, char *V, float *bias) {
-        if (t < last) next.put(K, V, bias);
+        if (t < last) next.put(a, K, V, bias);
         __syncthreads();
     };
     for (int b = 0; b < BUFFERS; ++b) Tiles::clear(a, Ks[b], Vs[b]);

@@ -127,35 +127,6 @@ __device__ __forceinline__ void epilogue(const DenseArgs &a, int row, int col, i
     store_eight_numbers(a.out, row * a.ldo + col, a.out_dtype, left, x);
 }
 
-// Elements moved to places s lower (0 < s < VEC, or all of it), zeros behind; and those from n on zeros.
-template <class T>
-__device__ __forceinline__ void move_down(ftc_u32x4 &w, int s)
-{
-    if constexpr (T::BYTES == 2) {
-        if (s & 1) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = (w[j] >> 16) | (j < 3 ? w[j + 1] << 16 : 0u);
-        }
-        s >>= 1;
-    }
-#pragma unroll
-    for (int b = 1; b <= 2; b *= 2)
-        if (s & b) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = j + b < 4 ? w[j + b] : 0u;
-        }
-    if (s >= 4) w = ftc_u32x4{0u, 0u, 0u, 0u};
-}
-template <class T>
-__device__ __forceinline__ void keep_first(ftc_u32x4 &w, int n)
-{
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (T::BYTES == 4) w[j] = j < n ? w[j] : 0u;
-        else w[j] = 2 * j + 1 < n ? w[j] : 2 * j < n ? w[j] & 0xffffu : 0u;
-    }
-}
-
 // One operand's tile: SIDE rows of the result's side and STEP of the contraction, staged by WAVES waves.
 template <class T, int SIDE, int STEP, bool ACROSS, int WAVES>
 struct Operand {

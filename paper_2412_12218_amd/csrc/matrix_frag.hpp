@@ -156,6 +156,48 @@ __device__ __forceinline__ Frag<T> load_frag(const void *base, int64_t idx, int 
     return a;
 }
 
+// Elements moved to places s lower (0 < s < VEC, or all of it), zeros behind; and those from n on zeros.
+template <class T>
+__device__ __forceinline__ void move_down(ftc_u32x4 &w, int s)
+{
+    if constexpr (T::BYTES == 2) {
+        if (s & 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (w[j] >> 16) | (j < 3 ? w[j + 1] << 16 : 0u);
+        }
+        s >>= 1;
+    }
+#pragma unroll
+    for (int b = 1; b <= 2; b *= 2)
+        if (s & b) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = j + b < 4 ? w[j + b] : 0u;
+        }
+    if (s >= 4) w = ftc_u32x4{0u, 0u, 0u, 0u};
+}
+template <class T>
+__device__ __forceinline__ void keep_first(ftc_u32x4 &w, int n)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (T::BYTES == 4) w[j] = j < n ? w[j] : 0u;
+        else w[j] = 2 * j + 1 < n ? w[j] : 2 * j < n ? w[j] & 0xffffu : 0u;
+    }
+}
+
+// The piece from element c on of a row of `width` elements that is readable from `row` on, zeros behind it, without a branch for the row's last piece:
+// the last 16 bytes of the row, moved.
+template <class T>
+__device__ __forceinline__ ftc_u32x4 load_piece_of_row(const void *row, int c, int width)
+{
+    if (width < T::VEC) return load_piece<T>(row, c, width - c);  // uniform
+    RawVec<T, T::VEC> r;
+    load_raw_any<T>(row, min(c, width - T::VEC), r);
+    ftc_u32x4 v = {r.w[0], r.w[1], r.w[2], r.w[3]};
+    if (c + T::VEC > width) move_down<T>(v, c + T::VEC - width);
+    return v;
+}
+
 // The eight numbers of an operand in fp32.
 template <class T>
 __device__ __forceinline__ void frag_numbers(const Frag<T> &a, float (&x)[8])
