@@ -379,7 +379,8 @@ int32_t ftc_agnn_layer_backward_fused(const ftc_csr *g, const ftc_windows *w, co
  * Layers of models that learn features per node id and attend between all nodes of a graph: the rows of a
  * table by id, the dense layer with its epilogue, and attention over a batch of graphs, each with its
  * gradients.  Matrices are row-major with a leading dimension at any alignment of an element (16-byte aligned
- * rows are fastest), sums and softmax statistics fp32, results the same in every run.
+ * rows are fastest), sums and softmax statistics fp32, results the same in every run.  Counts and widths are at most 2^30, and
+ * sizes that do not fit one launch (2^32 threads) are refused with FTC_EUNSUPPORTED.
  */
 
 /*
@@ -422,7 +423,8 @@ int32_t ftc_linear(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t
  *   dX = dP * W^T + dX_add (n x d_in, dx_dtype),  dW = X^T * dP (d_in x d_out, contiguous),  db = column sums of dP;
  * dX, dW, db may each be NULL (not computed); dW and db are of dw_dtype; dx_dtype and dw_dtype are fp32 or `dtype`.
  * dX_add (n x d_in of `dtype`, may be NULL) is what reaches X on another way, as through a residual connection around
- * the layer; it may be dX itself (same pointer, leading dimension and type).  The gradient of the residual is dZ.  dP is rounded to `dtype` for the products, db sums it unrounded.
+ * the layer; it may be dX itself (same pointer, leading dimension and type).  The gradient of the residual is dZ.
+ * dP is rounded to `dtype` for the products, db sums it unrounded.
  */
 size_t ftc_linear_backward_workspace_bytes(int32_t n, int32_t d_in, int32_t d_out);
 int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W,
@@ -440,7 +442,7 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
  * zeros.  Rows in front of the first and behind the last graph are neither read nor written.  lse (n_q x heads floats, may be NULL)
  * receives log sum_j exp(s_ij) (-inf without a key), what the backward pass needs.  All matrices are of `dtype`; D <= 128,
  * n_q * heads and n_kv * kv_heads at most 2^30.  Offsets outside [0, n_q] ([0, n_kv]) are taken as the nearest end.
- * In 16 bits the probabilities are rounded to `dtype` before they multiply V.
+ * In 16 bits the probabilities are rounded to `dtype` before they multiply V (fp16: 2^15 times them).
  */
 size_t ftc_graph_attention_workspace_bytes(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads,
                                            int32_t kv_heads, int32_t D);
@@ -456,7 +458,8 @@ int32_t ftc_graph_attention(int32_t n_q, const int32_t *q_ptr, int32_t n_kv, con
  *   dV_j = sum_i p_ij dOut_i,  ds_ij = p_ij (<dOut_i, v_j> - <dOut_i, out_i>),
  *   dQ_i = scale sum_j ds_ij k_j,  dK_j = scale sum_i ds_ij q_i   (sums over the heads that share a K/V head).
  * All matrices are of `dtype`; rows of dK and dV of masked keys are zeros.  dQ, dK, dV must not overlap an input.  In 16 bits
- * p and ds are rounded to `dtype` for their products.
+ * p (fp16: 2^15 p) and ds are rounded to `dtype` for their products; ds below 2^-14 has fewer bits in fp16, as every gradient of
+ * that size: scale the loss.
  */
 size_t ftc_graph_attention_backward_workspace_bytes(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads,
                                                     int32_t kv_heads, int32_t D);

@@ -804,6 +804,16 @@ static int32_t check_out_type(const char *who, const char *name, int32_t dtype, 
     return FTC_OK;
 }
 
+// Counts and widths: indexes of a whole tile, its end behind the last row included, are int32.
+static constexpr int32_t MOST_ROWS = 1 << 30;
+static int32_t check_sizes(const char *who, int32_t a, int32_t b, int32_t c, LaunchSize (*size)(int, int, int))
+{
+    if (a > MOST_ROWS || b > MOST_ROWS || c > MOST_ROWS) return fail(FTC_EUNSUPPORTED, "%s: counts and widths are at most 2^30", who);
+    if (!size(a, b, c).fits()) return fail(FTC_EUNSUPPORTED, "%s: too large for one launch", who);
+    return FTC_OK;
+}
+static LaunchSize lookup_size(int n, int, int D) { return embedding_size(n, D); }
+
 int32_t ftc_embedding(int32_t n, const int32_t *ids, int32_t vocab, const void *E, int32_t lde, int32_t dtype, int32_t D,
                       float scale, void *out, int32_t ldo, int32_t out_dtype, void *stream)
 {
@@ -815,6 +825,7 @@ int32_t ftc_embedding(int32_t n, const int32_t *ids, int32_t vocab, const void *
     if (!valid_dtype(dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for E", who);
     FTC_TRY(check_dense(out, ldo, out_dtype, D, who, "out"));
     if (out == E) return fail(FTC_EINVAL, "%s: out aliases E", who);
+    FTC_TRY(check_sizes(who, n, vocab, D, lookup_size));
     return launch_embedding(n, ids, vocab, E, lde, dtype, D, scale, out, ldo, out_dtype, static_cast<hipStream_t>(stream));
 }
 
@@ -838,6 +849,7 @@ int32_t ftc_embedding_backward(int32_t n, const int32_t *ids, int32_t vocab, con
     if (!valid_dtype(dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for dOut", who);
     FTC_TRY(check_dense(dE, ldde, de_dtype, D, who, "dE"));
     if (dE == dOut) return fail(FTC_EINVAL, "%s: dE aliases dOut", who);
+    FTC_TRY(check_sizes(who, n, vocab, D, embedding_backward_size));
     FTC_TRY(check_ws(who, embedding_backward_ws(n, vocab, D), ws, ws_bytes));
     return launch_embedding_backward(n, ids, vocab, dOut, lddo, dtype, D, scale, dE, ldde, de_dtype, ws,
                                      static_cast<hipStream_t>(stream));
@@ -872,6 +884,7 @@ int32_t ftc_linear(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t
         return fail(FTC_EINVAL, "%s: an output aliases an input or the other output", who);
     if (Z == residual && (ldz != ldr || z_dtype != dtype))
         return fail(FTC_EINVAL, "%s: Z on top of the residual needs its leading dimension and type", who);
+    FTC_TRY(check_sizes(who, n, d_in, d_out, linear_size));
     FTC_TRY(check_ws(who, linear_ws(n, d_in, d_out), ws, ws_bytes));
     const LinearShape p = {n, d_in, d_out, dtype, X, W, bias, residual, slope, Z, ldx, ldr, lds, ldz, act, z_dtype};
     return launch_linear(p, ws, static_cast<hipStream_t>(stream));
@@ -916,6 +929,7 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
         for (int j = 0; j < i; ++j)
             if (outs[i] && outs[i] == outs[j]) return fail(FTC_EINVAL, "%s: two outputs are the same", who);
     }
+    FTC_TRY(check_sizes(who, n, d_in, d_out, linear_backward_size));
     FTC_TRY(check_ws(who, linear_backward_ws(n, d_in, d_out), ws, ws_bytes));
     const LinearShape p = {n, d_in, d_out, dtype, X, W, nullptr, nullptr, const_cast<void *>(slope), nullptr, ldx, 0, lds, 0, FTC_ACT_NONE, dtype};
     if (dX_add && (dX_add == dW || dX_add == db)) return fail(FTC_EINVAL, "%s: an output aliases an input", who);
@@ -941,6 +955,8 @@ static int32_t check_attention(const char *who, const AttnShape &p)
     if (p.D < 1) return fail(FTC_EINVAL, "%s: need D >= 1", who);
     if (!attention_sizes_ok(p.n_q, p.n_kv, p.graphs, p.heads, p.kv_heads, p.D))
         return fail(FTC_EUNSUPPORTED, "%s: D is at most 128, kv_heads 65535, n_q * heads and n_kv * kv_heads 2^30", who);
+    if (!attention_size(p.n_q, p.n_kv, p.graphs, p.heads, p.kv_heads, p.D).fits())
+        return fail(FTC_EUNSUPPORTED, "%s: too many graphs and heads for one launch", who);
     if (!valid_dtype(p.dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype", who);
     if (p.graphs > 0 && (!p.q_ptr || !p.kv_ptr)) return fail(FTC_EINVAL, "%s: q_ptr or kv_ptr is NULL", who);
     if (static_cast<int64_t>(p.heads) * p.D > INT32_MAX) return fail(FTC_EUNSUPPORTED, "%s: heads * D does not fit 32 bits", who);

@@ -16,7 +16,7 @@
 // dQ and dK / dV are sums over different axes; two kernels (seven products a pair for five) add them up in a fixed order, where one would need
 // atomics.  Few queries (keys) and long graphs: the other axis is split over workgroups, whose parts join_*() adds up, in order.
 //
-// Probabilities and ds are rounded to the type of the inputs for the second product (ds_in_two() apart); scores, softmax statistics and sums are fp32.
+// Probabilities and ds are rounded to the type of the inputs for the second product (see ds_in_two() and p_bits()); scores, softmax statistics and sums are fp32.
 #pragma once
 #include "matrix_frag.hpp"
 
@@ -294,6 +294,11 @@ __device__ __forceinline__ Frag<T> rest_of(const f32x16 &c, int step, const Frag
 // is only rounded, 1.1 so; the exponentials, not the matrix cores, bound these kernels).
 template <class T, int DP>
 constexpr bool ds_in_two() { return T::BYTES == 2 && DP == 32; }
+
+// Probabilities are 2^p_bits() times as large in fp16: one key of a hundred thousand has 1e-5, which fp16 holds with 8 bits, and 2^15 p with 11; the
+// largest is 2^15.  Sums of them are taken back in fp32.
+template <class T>
+constexpr int p_bits() { return std::is_same<T, F16>::value ? 15 : 0; }
 
 // Tiles of the other side in LDS: one wave has no others that read while it waits, so it has one, and more workgroups find room beside it (D = 20,
 // fp32, 2000 graphs of 8 to 38 nodes, 4 heads, the forward pass: 48 us with two, 38 with one; the readout of 12 x 10 000 nodes 16 and 17).

@@ -19,6 +19,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
 {
     constexpr int SETS = wave_sets<T, DP, NW>(), THREADS = 64 * NW * SETS;
     constexpr int TK = 32 * NW, TQ = query_rows<T, NW>(), SUB = TQ / 32 / SETS, KS = DP / 16, DT = DP / 32, BUFFERS = tile_buffers<NW>();
+    constexpr float P_BACK = 1.f / (1 << p_bits<T>());
     typedef LdsTile<T, DP> L;
     typedef Rows<T, DP, TQ, THREADS, WHOLE> R;
     typedef Rows<T, DP, TK, THREADS, WHOLE> KeyRows;
@@ -74,8 +75,8 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
                 split_row(a, r, query, head);
                 const int64_t at = static_cast<int64_t>(q0 + query) * a.heads + here.share * a.group + head;
                 const float lse = a.lse[at];
-                my_lse = lse == -INFINITY ? -INFINITY : -lse * LOG2E;
-                my_delta = a.delta[at];
+                my_lse = lse == -INFINITY ? -INFINITY : fmaf(-lse, LOG2E, p_bits<T>());
+                my_delta = a.delta[at] * P_BACK;
             }
         }
     };
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
             mma<T>(ds, L::along_row(G + 32 * u * L::ROW, col, 2 * s + half), value_operand(s));
         }
     };
-    // p and ds from them
+    // 2^p_bits p and ds from them
     auto weights = [&](const float *row_lse, const float *row_delta, int u, f32x16 &p, f32x16 &ds) {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 p[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(p[4 * b + i], scale2, w[i] + bias));
-                ds[4 * b + i] = p[4 * b + i] * (ds[4 * b + i] - x[i]);
+                ds[4 * b + i] = p[4 * b + i] * fmaf(ds[4 * b + i], P_BACK, -x[i]);
             }
         }
     };
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
         for (int b = 0; b < 4; ++b) {
             const int c = 32 * d + 8 * b + 4 * half;
             const float x[4] = {dk[d][4 * b] * a.scale, dk[d][4 * b + 1] * a.scale, dk[d][4 * b + 2] * a.scale, dk[d][4 * b + 3] * a.scale};
-            const float y[4] = {dv[d][4 * b], dv[d][4 * b + 1], dv[d][4 * b + 2], dv[d][4 * b + 3]};
+            const float y[4] = {dv[d][4 * b] * P_BACK, dv[d][4 * b + 1] * P_BACK, dv[d][4 * b + 2] * P_BACK, dv[d][4 * b + 3] * P_BACK};
             if (a.splits > 1) {
                 const int64_t row = (static_cast<int64_t>(here.part) * 2 * a.n_kv + key) * a.kv_heads + here.share;
                 store_four<F32>(a.part, row * a.D + c, a.D - c, x);

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         for (int u = 0; u < SUB; ++u) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], scale2, -shift));
+                s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], scale2, p_bits<T>() - shift));
                 l += s[u][e];
             }
 #pragma unroll
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
             const float x[4] = {o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv};
             store_four<T>(a.out, query * a.ldo + head * a.D + c, a.D - c, x);
         }
-    if (a.lse && half == 0) a.lse[static_cast<int64_t>(query) * a.heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    if (a.lse && half == 0) a.lse[static_cast<int64_t>(query) * a.heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - p_bits<T>()) * LN2;
 }
 
 template <class T, int DP, int NW>

@@ -299,6 +299,17 @@ static int log_of(int x)
     return b;
 }
 
+// Threads of the largest launch, along x, and workgroups along y; of the lookup, and of the gradient.
+LaunchSize embedding_size(int n, int D)
+{
+    LaunchSize z;
+    for (int vec = 4; vec <= 8; vec *= 2) {
+        const int lanes = row_lanes(D, vec);
+        z.add(256ll * ceil_div(n, 256 / lanes * LOOKUP_ROWS), ceil_div(D, lanes * vec));
+    }
+    return z;
+}
+
 int32_t launch_embedding(int n, const int *ids, int vocab, const void *E, int lde, int dt, int D, float scale, void *out, int ldo, int odt,
                          hipStream_t s)
 {
@@ -325,6 +336,18 @@ static int chunk_tokens(int n, int D, int vec)
 static size_t partial_row_bytes(int n, int D, int vec)
 {
     return align_up(static_cast<size_t>(ceil_div(n, chunk_tokens(n, D, vec) * (256 / row_lanes(D, vec)))) * align_up(D, 8) * sizeof(float), 256);
+}
+
+LaunchSize embedding_backward_size(int n, int vocab, int D)
+{
+    LaunchSize z;
+    for (int vec = 4; vec <= 8; vec *= 2) {
+        const int lanes = row_lanes(D, vec);
+        const int64_t spans = ceil_div(n, chunk_tokens(n, D, vec) * (256 / lanes));
+        z.add(256 * spans, ceil_div(D, lanes * vec));
+        z.add(FINISH * (spans / (FINISH / row_lanes(D, 4)) + 1 + ceil_div(vocab, ABSENT)), 1);
+    }
+    return z;
 }
 
 size_t embedding_backward_ws(int n, int vocab, int D)

@@ -181,6 +181,21 @@ int32_t launch_build_windows(const ftc_csr &g, ftc_windows &w, void *ws, size_t 
 size_t id_sort_ws(int n);
 int32_t launch_sort_ids(int n, const int *ids, int vocab, const uint32_t **keys, const uint32_t **order, void *ws, hipStream_t s);
 // embedding.hip
+// The threads along x and the workgroups along y of an entry point's launches, at most, and whether a launch can have them.
+struct LaunchSize {
+    int64_t x = 0, y = 0;
+    void add(int64_t threads, int64_t groups)
+    {
+        x = threads > x ? threads : x;
+        y = groups > y ? groups : y;
+    }
+    bool fits() const { return x <= UINT32_MAX && y <= 65535; }
+};
+LaunchSize embedding_size(int n, int D);
+LaunchSize embedding_backward_size(int n, int vocab, int D);
+LaunchSize linear_size(int n, int d_in, int d_out);
+LaunchSize linear_backward_size(int n, int d_in, int d_out);
+LaunchSize attention_size(int n_q, int n_kv, int graphs, int heads, int kv_heads, int D);
 int32_t launch_embedding(int n, const int *ids, int vocab, const void *E, int lde, int dt, int D, float scale, void *out, int ldo, int odt,
                          hipStream_t s);
 size_t embedding_backward_ws(int n, int vocab, int D);

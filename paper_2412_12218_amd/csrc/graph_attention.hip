@@ -50,33 +50,37 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
         const int c = lane + 64 * k;
         if (c < a.D) store_elem(a.out, query * a.ldo + head * a.D + c, DT, x[k] * inv);
     }
-    if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - p_bits<T>()) * LN2;
 }
 
 // ---- backward: delta -----------------------------------------------------------------------------------------
-// 16 lanes a query and head.
+// 16 lanes a query and head; DELTA_GROUPS workgroups at most, which go on with the next rows.
+constexpr int DELTA_GROUPS = 1 << 20;
 template <class T>
 __global__ __launch_bounds__(256) void attention_delta_kernel(AttnArgs a)
 {
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4), all = static_cast<int64_t>(a.n_q) * a.heads;
+    const int64_t all = static_cast<int64_t>(a.n_q) * a.heads;
     const int lane = threadIdx.x & 15;
-    const bool there = row < all;
-    const int query = there ? static_cast<int>(row / a.heads) : 0, head = there ? static_cast<int>(row % a.heads) : 0;
-    float sum = 0.f;
-    for (int c = lane * T::VEC; c < a.D; c += 16 * T::VEC) {
-        const int left = there ? a.D - c : 0;
-        const ftc_u32x4 x = load_piece<T>(a.O, query * a.ldo + head * a.D + c, left), y = load_piece<T>(a.dO, query * a.lddo + head * a.D + c, left);
-        RawVec<T, T::VEC> u, v;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * 16; first < all; first += static_cast<int64_t>(gridDim.x) * 16) {
+        const int64_t row = first + (threadIdx.x >> 4);
+        const bool there = row < all;
+        const int query = there ? static_cast<int>(row / a.heads) : 0, head = there ? static_cast<int>(row % a.heads) : 0;
+        float sum = 0.f;
+        for (int c = lane * T::VEC; c < a.D; c += 16 * T::VEC) {
+            const int left = there ? a.D - c : 0;
+            const ftc_u32x4 x = load_piece<T>(a.O, query * a.ldo + head * a.D + c, left), y = load_piece<T>(a.dO, query * a.lddo + head * a.D + c, left);
+            RawVec<T, T::VEC> u, v;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { u.w[j] = x[j]; v.w[j] = y[j]; }
-        float f[T::VEC], g[T::VEC];
-        unpack<T, T::VEC>(u, f);
-        unpack<T, T::VEC>(v, g);
+            for (int j = 0; j < 4; ++j) { u.w[j] = x[j]; v.w[j] = y[j]; }
+            float f[T::VEC], g[T::VEC];
+            unpack<T, T::VEC>(u, f);
+            unpack<T, T::VEC>(v, g);
 #pragma unroll
-        for (int j = 0; j < T::VEC; ++j) sum = fmaf(f[j], g[j], sum);
+            for (int j = 0; j < T::VEC; ++j) sum = fmaf(f[j], g[j], sum);
+        }
+        sum = group_sum_dpp<16>(sum);
+        if (there && lane == 0) a.delta[row] = sum;
     }
-    sum = group_sum_dpp<16>(sum);
-    if (there && lane == 0) a.delta[row] = sum;
 }
 
 // out[row, :] = sum over the parts, for the rows of the graphs; `width` elements a row, parts `stride` elements apart.
@@ -118,6 +122,19 @@ static int attn_splits(int64_t rows, int64_t other, int graphs, int kv_heads, in
     return static_cast<int>(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 
+LaunchSize attention_size(int n_q, int n_kv, int graphs, int heads, int kv_heads, int D)
+{
+    const int64_t virt = static_cast<int64_t>(n_q) * (heads / kv_heads);
+    LaunchSize z;
+    for (int side = 0; side < 2; ++side) {
+        const int64_t rows = side ? n_kv : virt, other = side ? virt : n_kv;
+        const int nw = attn_waves(rows, other, graphs, D), splits = attn_splits(rows, other, graphs, kv_heads, D);
+        z.add(static_cast<int64_t>(attn_tiles(rows, graphs, nw)) * kv_heads * splits * (nw == 1 ? 64 : 512), 1);
+        if (splits > 1) z.add((side ? static_cast<int64_t>(n_kv) * kv_heads : static_cast<int64_t>(n_q) * heads) * (D > 64 ? D : 64), 1);
+    }
+    return z;
+}
+
 size_t attention_ws(int n_q, int n_kv, int graphs, int heads, int kv_heads, int D)
 {
     const int64_t rows = static_cast<int64_t>(n_q) * heads;
@@ -139,7 +156,7 @@ size_t attention_backward_ws(int n_q, int n_kv, int graphs, int heads, int kv_he
 static unsigned attn_grid(AttnArgs &a, int64_t rows, int nw)
 {
     a.tiles = attn_tiles(rows, a.graphs, nw);
-    return static_cast<unsigned>(a.tiles) * a.kv_heads * a.splits;
+    return static_cast<unsigned>(a.tiles) * a.kv_heads * a.splits;  // attention_size()
 }
 
 #define FTC_ATTN_TYPED_N(KERNEL, N, GRID, ...)                                                                         \
@@ -179,7 +196,7 @@ static void backward(AttnArgs a, int dtype, void *ws, hipStream_t s)
     a.delta = static_cast<float *>(ws);
     a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + align_up(static_cast<size_t>(rows) * sizeof(float), 256));
     if (rows > 0) {
-        FTC_ATTN_TYPED(attention_delta_kernel, (rows + 15) / 16, a);
+        FTC_ATTN_TYPED(attention_delta_kernel, (rows + 15) / 16 < DELTA_GROUPS ? (rows + 15) / 16 : DELTA_GROUPS, a);
         const int nw = attn_waves(virt, a.n_kv, a.graphs, a.D);
         a.splits = attn_splits(virt, a.n_kv, a.graphs, a.kv_heads, a.D);
         const unsigned grid = attn_grid(a, virt, nw);

@@ -219,6 +219,35 @@ static void dense(DenseArgs a, int dtype, void *ws, hipStream_t s)
     }
 }
 
+static void add_dense_size(LaunchSize &z, int M, int N, int K)
+{
+    for (int v = 0; v < 4; ++v) {
+        const DensePlan p = dense_plan(M, N, K, v & 1, v & 2);
+        z.add(dense_tiles(M, N, p.tile) * (p.tile == DENSE_256 ? 512 : 256), p.splits);
+    }
+    if (M <= 4) z.add(16ll * N, 1);  // linear_rows.hip
+    z.add(static_cast<int64_t>(M) * ceil_div(N, 8), 1);  // the join of parts
+}
+// Of ftc_linear, and of its backward pass.
+LaunchSize linear_size(int n, int d_in, int d_out)
+{
+    LaunchSize z;
+    add_dense_size(z, n, d_out, d_in);
+    return z;
+}
+LaunchSize linear_backward_size(int n, int d_in, int d_out)
+{
+    LaunchSize z;
+    add_dense_size(z, n, d_in, d_out);
+    add_dense_size(z, d_in, d_out, n);
+    for (int vec = 4; vec <= 8; vec *= 2) {
+        const int lanes = dp_lanes(d_out, vec);
+        z.add(256ll * ceil_div(n, dp_rows(lanes)), ceil_div(d_out, vec << lanes));
+    }
+    z.add(16ll * d_out, 1);
+    return z;
+}
+
 size_t linear_ws(int n, int d_in, int d_out) { return dense_ws(n, d_out, d_in); }
 
 static size_t linear_sums_bytes(int n, int d_out)

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import transformer_reference
 from paper_2412_12218_amd import binding as B
 from transformer_reference import attention, check
 
@@ -171,6 +172,26 @@ def test_gradient_against_differences():
         want = float((got[name].double() * d.double()).sum())
         size = float(b.dO.double().norm())
         assert abs((up - down) / (2 * h) - want) <= size * (60 * h * h / 6 + 64 * 2.0 ** -24 * 4 / h), name
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_weights_below_the_normal_range(dtype, monkeypatch):
+    """Probabilities of 5e-5 and, one key apart, of 1.5e-8: fp16 holds them as 2^15 times as much, of which the step below the normal range
+    is 2^-24, half of it 2^-25, 2^-40 of the probability.  V and dO are 1 and more, so that no result is that small."""
+    monkeypatch.setitem(transformer_reference.TINY, torch.float16, 2.0 ** -40)
+    b = Batch([20000], 16, 1, 8, dtype, qlens=[200], seed=11)
+    b.V.copy_(b.V.abs() + 1)
+    b.dO.copy_(b.dO.abs() + 1)
+    got, want = b.run(), attention(*b.args(), 16, 1, b.scale, None, b.dO)
+    for key in ("out", "lse", "dV"):
+        check(f"{dtype} 20000 keys {key}", got[key], *want[key])
+    b = Batch([100001, 40], 1, 1, 8, dtype, qlens=[1, 50], seed=12)
+    b.Q.zero_(), b.K.zero_(), b.V.fill_(9)
+    b.Q[:, 0], b.K[0, 0], b.V[0] = 18, 1, 1
+    b.scale = 1.0
+    got, want = b.run(False), attention(*b.args(), 1, 1, 1.0)
+    for key in ("out", "lse"):
+        check(f"{dtype} one key above 100 000 {key}", got[key], *want[key])
 
 
 def test_longer_graphs_than_a_part():

@@ -91,6 +91,22 @@ def test_refused(call, change, code):
     assert B.lib().ftc_last_error().startswith(b"ftc_")
 
 
+M30 = 1 << 30
+LARGE = [
+    (embedding, dict(n=M30 + 1)), (embedding, dict(vocab=M30 + 1)), (embedding, dict(n=M30, D=4096, lde=4096, ldo=4096)),
+    (embedding, dict(D=M30, lde=M30, ldo=M30)), (embedding_backward, dict(n=M30 + 1)), (embedding_backward, dict(vocab=M30 + 7)),
+    (linear, dict(n=M30 + 1)), (linear, dict(n=M30, d_out=64, ldr=64, lds=64, ldz=64)), (linear, dict(n=1, d_out=M30, ldr=M30, lds=M30, ldz=M30)),
+    (linear_backward, dict(n=M30, d_out=64, lds=64, ldz=64)), (linear_backward, dict(d_out=M30, lds=M30, ldz=M30)),
+    (attention, dict(graphs=M30)), (attention, dict(graphs=1 << 26, kv_heads=4, ldk=32, ldv=32)), (attention_backward, dict(graphs=M30)),
+]
+
+
+@pytest.mark.parametrize("call,change", LARGE, ids=lambda v: v.__name__ if callable(v) else "-".join(f"{k}={x}" for k, x in v.items())[:40])
+def test_sizes_beyond_a_launch_are_refused(call, change):
+    assert call(**change) == UNSUPPORTED
+    assert b"2^30" in B.lib().ftc_last_error() or b"launch" in B.lib().ftc_last_error()
+
+
 def test_calls_without_work():
     """Nothing to compute: no pointer is needed, nothing is launched."""
     assert embedding(n=0, ids=None, E=None, out=None) == B.FTC_OK
