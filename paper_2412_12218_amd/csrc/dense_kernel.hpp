@@ -7,11 +7,16 @@
 //   whole pieces (FAST)  rows and widths of whole 16-byte pieces at 16-byte alignment: global_load_lds, no registers on the way.  An instruction
 //                        fills 64 consecutive pieces of LDS, so the lanes fetch the pieces that the swizzle puts there.  Rows and columns behind the
 //                        result's ends are those at the end once more: what they give is not stored.
-//   else                 through registers, element by element at the ends.
+//   else                 through registers, the last piece of a row as the row's last 16 bytes, moved to their place.
 // The indices that a last step lacks are zeros in both operands.
 //
 // Results go through LDS once more, so that neighbouring lanes have neighbouring columns: bias, activation, residual and the store work on
 // eight numbers of a row.
+//
+// Bound by the matrix instructions for wide layers: 8192^3 in bf16 902 us, 1219 TFLOP/s (a library product of that size 804 to 960); 65 536 x 1024 -> 4096 635 us, 866
+// TFLOP/s, 763 with GELU, which the vector units compute for every result while no other workgroup multiplies.  20 000 x 768 -> 768: 30 us, 42 with GELU, 57
+// with SiLU, its slope and a residual (124 MB at 2.2 TB/s; tiles of 64, 128 and 256 56 to 58, the residual's rows asked for before the activation).
+// Unaligned: 30 001 x 333 -> 777 61 us, 255 TFLOP/s.  fp32 runs six products of bf16 pieces: 1032 x 3696 -> 2920 197 us, 113 TFLOP/s of fp32.
 #pragma once
 #include "matrix_frag.hpp"
 
@@ -50,31 +55,42 @@ inline bool dense_whole_pieces(const void *p, int64_t ld, int width, int dtype)
 #if defined(__HIPCC__)
 constexpr int SLOPE_BITS = 14;
 
-// act(p) and act'(p), from one exponential and one reciprocal (a step of fp32 each).  Infinite p: the limits.
-//   Phi(-|p|) = exp(-p^2 / 2) (a1 t + .. + a5 t^5) / 2 with t = 1 / (1 + 0.3275911 |p| / sqrt 2), off by at most 0.75e-7, half a step of fp32 at
-//   one (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26); sigma(p) = 1 / (1 + exp(-p))
-__device__ __forceinline__ float activation(float p, int act, float &slope)
+// act(p) and, if asked for, act'(p), from one exponential and one reciprocal (a step of fp32 each).
+//   GELU  p Phi(p) = max(p, 0) - |p| Phi(-|p|), with Phi(-a) = exp(-a^2 / 2) (a1 t + .. + a5 t^5) / 2 and t = 1 / (1 + 0.3275911 a / sqrt 2), off by at
+//         most 0.75e-7, half a step of fp32 at one (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26)
+//   SiLU  p sigma(p), sigma(p) = 1 / (1 + exp(-p))
+// Infinite p: the limits, as the factor that is infinite is cut off where the other is zero.  NaN: through the exponential, which takes p as it is.
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activation(float p, float &slope)
 {
-    slope = 1.f;
-    if (act == FTC_ACT_RELU) {
+    if constexpr (ACT == FTC_ACT_RELU) {
         slope = p > 0.f ? 1.f : p != p ? p : 0.f;
         return p > 0.f ? p : p != p ? p : 0.f;
+    } else if constexpr (ACT == FTC_ACT_GELU) {
+        const float e = __builtin_amdgcn_exp2f(p * p * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(fmaf(fabsf(p), 0.23164188f, 1.f));
+        const float tail = e * (t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f));
+        if constexpr (SLOPE) slope = fmaf(__builtin_amdgcn_fmed3f(p, -40.f, 40.f) * 0.39894228040143268f, e, p > 0.f ? 1.f - tail : tail);
+        return fmaf(-fminf(fabsf(p), 40.f), tail, fmaxf(p, 0.f));
+    } else if constexpr (ACT == FTC_ACT_SILU) {
+        const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(p * -1.4426950408889634f));
+        if constexpr (SLOPE) slope = g * fmaf(__builtin_amdgcn_fmed3f(p, -88.f, 88.f), 1.f - g, 1.f);
+        return fmaxf(p, -88.f) * g;
+    } else {
+        slope = 1.f;
+        return p;
     }
-    if (act == FTC_ACT_GELU) {
-        const float q = p < -40.f ? -40.f : p > 40.f ? 40.f : p;
-        const float e = __builtin_amdgcn_exp2f(q * q * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(fmaf(fabsf(q), 0.23164188f, 1.f));
-        const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-        const float cdf = q < 0.f ? tail : 1.f - tail;
-        slope = fmaf(q * 0.39894228040143268f, e, cdf);
-        return p > 40.f ? p : q * cdf;
-    }
-    if (act == FTC_ACT_SILU) {
-        const float q = p < -80.f ? -80.f : p > 80.f ? 80.f : p;
-        const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(q * -1.4426950408889634f));
-        slope = g * fmaf(q, 1.f - g, 1.f);
-        return p > 80.f ? p : p < -80.f ? 0.f : q * g;
-    }
-    return p;
+}
+template <bool SLOPE>
+__device__ __forceinline__ void activations(int act, float (&x)[8], float (&slope)[8])  // act: uniform
+{
+    auto all = [&](auto code) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = activation<decltype(code)::value, SLOPE>(x[j], slope[j]);
+    };
+    if (act == FTC_ACT_GELU) all(std::integral_constant<int, FTC_ACT_GELU>());
+    else if (act == FTC_ACT_SILU) all(std::integral_constant<int, FTC_ACT_SILU>());
+    else if (act == FTC_ACT_RELU) all(std::integral_constant<int, FTC_ACT_RELU>());
+    else all(std::integral_constant<int, FTC_ACT_NONE>());
 }
 
 __device__ __forceinline__ int16_t slope_code(float s)
@@ -93,10 +109,11 @@ __device__ __forceinline__ void activate(const DenseArgs &a, int row, int col, i
     float slope[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] += bias[j];
-    if (a.act == FTC_ACT_NONE && !a.slope) return;  // uniform
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = activation(x[j], a.act, slope[j]);
-    if (!a.slope) return;
+    if (!a.slope) {  // uniform
+        if (a.act != FTC_ACT_NONE) activations<false>(a.act, x, slope);
+        return;
+    }
+    activations<true>(a.act, x, slope);
     if constexpr (T::BYTES == 4) {
         store_eight_numbers(a.slope, row * a.lds + col, FTC_F32, left, slope);
     } else {
