@@ -264,6 +264,19 @@ struct Keys {
     }
 };
 
+// What is added to the scores of 32 keys, as the result that their product begins with.
+__device__ __forceinline__ f32x16 bias_of(const float *bias, int half)
+{
+    f32x16 c;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const ftc_f32x4 w = *reinterpret_cast<const ftc_f32x4 *>(&bias[8 * b + 4 * half]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[4 * b + i] = w[i];
+    }
+    return c;
+}
+
 __device__ __forceinline__ float both_halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
 __device__ __forceinline__ float both_halves_sum(float v) { return v + __shfl_xor(v, 32, 64); }
 

@@ -139,7 +139,8 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
         if constexpr (SETS == 2) return L::along_row(Vs + 32 * wave * L::ROW, col, 2 * s + half);
         else return v[s];
     };
-    const float scale2 = a.scale * LOG2E, bias = seen ? 0.f : -INFINITY;
+    const float scale2 = a.scale * LOG2E;
+    const bool busy = k0 + tile.index * TK + wave * 32 < k1;  // uniform in the wave, which has keys
     f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) { dk[d] = zero16(); dv[d] = zero16(); }
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
             const ftc_f32x4 x = *reinterpret_cast<const ftc_f32x4 *>(&row_delta[32 * u + 8 * b + 4 * half]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                p[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(p[4 * b + i], scale2, w[i] + bias));
+                p[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(p[4 * b + i], scale2, w[i]));
                 ds[4 * b + i] = p[4 * b + i] * fmaf(ds[4 * b + i], P_BACK, -x[i]);
             }
         }
@@ -185,6 +186,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
     };
     // The products of one 32 rows run beside the exponentials of the other (a wave's matrix instructions take 32 cycles, 4 to issue).
     auto attend = [&](const char *Q, const char *G, const float *row_lse, const float *row_delta) {
+        if (!busy) return;
         f32x16 p0, ds0, p1, ds1;
         const int u0 = SETS == 2 ? set : 0;
         scores(Q, G, u0, p0, ds0);
@@ -259,8 +261,12 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const int c = 32 * d + 8 * b + 4 * half;
-            const float x[4] = {dk[d][4 * b] * a.scale, dk[d][4 * b + 1] * a.scale, dk[d][4 * b + 2] * a.scale, dk[d][4 * b + 3] * a.scale};
-            const float y[4] = {dv[d][4 * b] * P_BACK, dv[d][4 * b + 1] * P_BACK, dv[d][4 * b + 2] * P_BACK, dv[d][4 * b + 3] * P_BACK};
+            float x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {  // a key that is not seen was a column of zeros like any other so far
+                x[i] = seen ? dk[d][4 * b + i] * a.scale : 0.f;
+                y[i] = seen ? dv[d][4 * b + i] * P_BACK : 0.f;
+            }
             if (a.splits > 1) {
                 const int64_t row = (static_cast<int64_t>(here.part) * 2 * a.n_kv + key) * a.kv_heads + here.share;
                 store_four<F32>(a.part, row * a.D + c, a.D - c, x);

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
     Tiles next;
     next.look(a, k0 + first * TK, first < last ? k1 : 0);
     const int r = tile.index * TQ + wave * 32 + col;
-    const bool there = r < rows;
+    const bool there = r < rows, busy = tile.index * TQ + wave * 32 < rows;  // busy: uniform in the wave, which has rows
     int query, head;
     split_row(a, there ? r : 0, query, head);
     query += q0;
@@ -49,9 +49,11 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
     for (int s = 0; s < KS; ++s) {
         const int c = 16 * s + 8 * half;
         q[s] = operand_at<T, WHOLE>(q_row, c, a.D, there);
+        if (a.scale < 0.f) frag_negate<T>(q[s]);
         g[s] = operand_at<T, WHOLE>(g_row, c, a.D, there);
     }
-    const float scale2 = a.scale * LOG2E;
+    // scale has the sign of +, which the -infinity of hidden keys keeps
+    const float scale2 = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);
     const int64_t at = static_cast<int64_t>(query) * a.heads + head;
     const float lse = there ? a.lse[at] : -INFINITY;
     const float minus_lse2 = lse == -INFINITY ? -INFINITY : -lse * LOG2E;  // a row without keys has no probabilities
@@ -68,7 +70,7 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
 
     // p and <dO, v> of 32 keys
     auto scores = [&](const char *K, const char *V, const float *bias, int u, f32x16 &p, f32x16 &dp) {
-        p = zero16();
+        p = bias_of(bias + 32 * u, half);
         dp = zero16();
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
@@ -76,11 +78,7 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
             mma<T>(dp, L::along_row(V + 32 * u * L::ROW, col, 2 * k + half), g[k]);
         }
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const ftc_f32x4 w = *reinterpret_cast<const ftc_f32x4 *>(&bias[32 * u + 8 * b + 4 * half]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(p[4 * b + i], scale2, w[i] + minus_lse2));
-        }
+        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], scale2, minus_lse2));
     };
     // delta of a row whose keys are all here, from p and <dO, v> of SUB 32 keys, which are kept where they fit in registers
     auto settle = [&](auto get_scores) {
@@ -124,6 +122,7 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
         }
     };
     auto attend = [&](const char *K, const char *V, const float *bias) {
+        if (!busy) return;
         if constexpr (scores_kept<T, DP, NW>()) {
             f32x16 p[SUB], dp[SUB];
 #pragma unroll

@@ -33,7 +33,7 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
     Tiles next;
     next.look(a, k0 + first * TK, first < last ? k1 : 0);
     const int r = tile.index * TQ + wave * 32 + col;
-    const bool there = r < rows;
+    const bool there = r < rows, busy = tile.index * TQ + wave * 32 < rows;  // busy: uniform in the wave, which has rows
     int query, head;
     split_row(a, there ? r : 0, query, head);
     query += q0;
@@ -53,22 +53,15 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = zero16();
 
-    auto attend = [&](const char *K, const char *V, const float *bias, bool ragged) {
+    auto attend = [&](const char *K, const char *V, const float *bias) {
+        if (!busy) return;
         f32x16 s[SUB];
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            s[u] = zero16();
+            s[u] = bias_of(bias + 32 * u, half);
 #pragma unroll
             for (int k = 0; k < KS; ++k) mma<T>(s[u], L::along_row(K + 32 * u * L::ROW, col, 2 * k + half), q[k]);
-            if (ragged) {
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const ftc_f32x4 w = *reinterpret_cast<const ftc_f32x4 *>(&bias[32 * u + 8 * b + 4 * half]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[u][4 * b + i] += w[i];
-                }
-            }
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
         }
@@ -110,7 +103,7 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         for (int t = first; t < last; ++t) {
             get(t, Ks[0], Vs[0], biases[0]);
             put(t, Ks[0], Vs[0], biases[0]);
-            attend(Ks[0], Vs[0], biases[0], a.mask || (t + 1) * TK > keys);
+            attend(Ks[0], Vs[0], biases[0]);
             __syncthreads();
         }
     } else {
@@ -118,7 +111,7 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         auto turn = [&](int t, const char *__restrict__ K, const char *__restrict__ V, const float *__restrict__ bias, char *__restrict__ Kn,
                         char *__restrict__ Vn, float *__restrict__ bias_n) {
             get(t + 1, Kn, Vn, bias_n);
-            attend(K, V, bias, a.mask || (t + 1) * TK > keys);
+            attend(K, V, bias);
             put(t + 1, Kn, Vn, bias_n);
         };
         get(first, Ks[0], Vs[0], biases[0]);

@@ -109,7 +109,8 @@ static int attn_waves(int64_t rows, int64_t other, int graphs, int D)
     return rows <= 64ll * graphs || (rows <= most && other <= most) ? 1 : 4;
 }
 static int attn_tiles(int64_t rows, int graphs, int waves) { return static_cast<int>(rows / (32 * waves)) + graphs; }
-// Parts of the other axis where there are fewer waves than eight for each compute unit.  A part of a graph of the mean size has at least two tiles of one
+// Parts of the other axis where there are at most four waves for each compute unit, up to eight (parts and their join cost a pass over fp32 results: 8
+// graphs of 799 nodes, 8 heads, D = 64, bf16, in two parts 47 us, whole 27).  A part of a graph of the mean size has at least two tiles of one
 // wave's workgroups (parts of 64 / 128 / 256: 121 graphs of 557 nodes, one query, D = 37, bf16 18 / 26 / 54 us, 19 of 350, D = 96, fp32 47 / 87 / 157),
 // four of four waves'.
 static int attn_splits(int64_t rows, int64_t other, int graphs, int kv_heads, int D)
@@ -117,7 +118,7 @@ static int attn_splits(int64_t rows, int64_t other, int graphs, int kv_heads, in
     const int nw = attn_waves(rows, other, graphs, D);
     const int64_t groups = static_cast<int64_t>(attn_tiles(rows, graphs, nw)) * kv_heads;
     if (groups < 1 || graphs < 1) return 1;
-    const int64_t want = (2048 / nw + groups - 1) / groups, most = other / graphs / (nw == 1 ? 64 : 256);
+    const int64_t want = 2048 / nw / groups, most = other / graphs / (nw == 1 ? 64 : 256);
     const int64_t s = want < most ? want : most;
     return static_cast<int>(s < 1 ? 1 : s > 64 ? 64 : s);
 }

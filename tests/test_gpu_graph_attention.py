@@ -134,6 +134,17 @@ def test_masks_that_leave_nothing_and_what_they_hide(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [-0.25, 0.0])
+def test_scales_that_are_not_positive(dtype, scale):
+    """Hidden keys stay hidden where the scale turns signs or leaves nothing of the scores."""
+    for lens in ([90, 5, 33], [300, 170]):
+        b = Batch(lens, 4, 2, 32, dtype, masked=0.3, seed=13)
+        b.scale = scale
+        got = b.check(f"{dtype} scale {scale}")
+        assert bool((got["dK"][b.mask == 0] == 0).all()) and bool((got["dV"][b.mask == 0] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_large_scores(dtype):
     """Scores of hundreds: one key has all the weight, no exponential overflows."""
     Batch([90, 33], 2, 2, 64, dtype, seed=3, spread=6.0).check(f"{dtype} large scores")
