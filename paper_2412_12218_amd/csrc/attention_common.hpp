@@ -304,7 +304,8 @@ __device__ __forceinline__ Frag<T> rest_of(const f32x16 &c, int step, const Frag
 
 // ds adds up to zero over a row's keys, so with few columns its rounding shows more than that of the result: for D up to 32 in 16
 // bits its products take what the rounding left as a second operand (dQ against 64 bits, fp16, D = 8: 1.58 times the error of a result that
-// is only rounded, 1.1 so; the exponentials, not the matrix cores, bound these kernels).
+// is only rounded, 1.1 so; the exponentials, not the matrix cores, bound these kernels).  So do those of any D in one wave's workgroups for graphs
+// of one tile, whose few sums do not average it (three nodes, D = 37, bf16: 1.69 times), and which are bound by latency.
 template <class T, int DP>
 constexpr bool ds_in_two() { return T::BYTES == 2 && DP == 32; }
 

@@ -173,14 +173,15 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
         for (int s = 0; s < 2; ++s) {
             const Frag<T> pf = operand_of<T>(p, s), df = operand_of<T>(ds, s);
             Frag<T> low;
-            if constexpr (ds_in_two<T, DP>()) low = rest_of<T>(ds, s, df);
+            const bool two = ds_in_two<T, DP>() || (T::BYTES == 2 && NW == 1 && tiles == 1);
+            if (two) low = rest_of<T>(ds, s, df);
             const int r0 = (32 * u + 16 * s) * L::ROW;
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 mma<T>(dv[d], L::along_column(G + r0, 4 * half, 4 * half + 8, 32 * d), pf);
                 const Frag<T> qf = L::along_column(Q + r0, 4 * half, 4 * half + 8, 32 * d);
                 mma<T>(dk[d], qf, df);
-                if constexpr (ds_in_two<T, DP>()) mma<T>(dk[d], qf, low);
+                if (two) mma<T>(dk[d], qf, low);
             }
         }
     };

@@ -111,12 +111,13 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
             const Frag<T> df = operand_of<T>(ds, k);
             Frag<T> pf, low;
             if constexpr (MEAN) pf = operand_of<T>(p, k);
-            if constexpr (ds_in_two<T, DP>()) low = rest_of<T>(ds, k, df);
+            const bool two = ds_in_two<T, DP>() || (T::BYTES == 2 && NW == 1 && tiles == 1);
+            if (two) low = rest_of<T>(ds, k, df);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 const Frag<T> kf = L::along_column(K + (32 * u + 16 * k) * L::ROW, 4 * half, 4 * half + 8, 32 * d);
                 mma<T>(dq[d], kf, df);
-                if constexpr (ds_in_two<T, DP>()) mma<T>(dq[d], kf, low);
+                if (two) mma<T>(dq[d], kf, low);
                 if constexpr (MEAN) mma<T>(mean[d], kf, pf);
             }
         }

@@ -134,6 +134,13 @@ def test_masks_that_leave_nothing_and_what_they_hide(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_one_side_empty(dtype):
+    """No key, or no query, in any graph: zeros on the other side, nothing read."""
+    for lens, qlens in (([0, 0, 0], [40, 1, 200]), ([40, 1, 200], [0, 0, 0])):
+        Batch(lens, 2, 1, 24, dtype, qlens=qlens, seed=14).check(f"{dtype} {sum(qlens)} over {sum(lens)}")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("scale", [-0.25, 0.0])
 def test_scales_that_are_not_positive(dtype, scale):
     """Hidden keys stay hidden where the scale turns signs or leaves nothing of the scores."""
