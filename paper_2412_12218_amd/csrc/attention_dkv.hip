@@ -4,7 +4,7 @@
 // would leave a SIMD one wave (16 bits, D above 64), K and V of the workgroup's keys are in LDS instead and a second set of waves has the
 // same keys and every second 32 rows; the two sums are added at the end.
 //
-// Measured as the forward kernel: D = 64 95 us, 409 TFLOP/s; D = 128 1900 us, 683 TFLOP/s (four products).  There a CU's four waves read 192 KB of LDS, 1500 cycles, for
+// Measured as the forward kernel: D = 64 93 us, 418 TFLOP/s; D = 128 1900 us, 683 TFLOP/s (four products).  There a CU's four waves read 192 KB of LDS, 1500 cycles, for
 // every 1024 cycles of matrix instructions; K and V in registers, one wave a SIMD, took 2951 us.
 #include "attention_common.hpp"
 

@@ -7,7 +7,7 @@
 // 75 and 93 us).  Where one tile holds all keys delta is the sum of
 // p <dO, v> from the start: one key gives ds = 0 exactly.
 //
-// Measured as the forward kernel: D = 64 75 us, 389 TFLOP/s; D = 128 1040 us, 936 TFLOP/s (three products).
+// Measured as the forward kernel: D = 64 73 us, 400 TFLOP/s; D = 128 1040 us, 936 TFLOP/s (three products).
 #include "attention_common.hpp"
 
 namespace ftc {

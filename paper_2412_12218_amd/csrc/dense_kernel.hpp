@@ -14,8 +14,8 @@
 // eight numbers of a row.
 //
 // Bound by the matrix instructions for wide layers: 8192^3 in bf16 902 us, 1219 TFLOP/s (a library product of that size 804 to 960); 65 536 x 1024 -> 4096 635 us, 866
-// TFLOP/s, 763 with GELU, which the vector units compute for every result while no other workgroup multiplies.  20 000 x 768 -> 768: 30 us, 42 with GELU, 57
-// with SiLU, its slope and a residual (124 MB at 2.2 TB/s; tiles of 64, 128 and 256 56 to 58, the residual's rows asked for before the activation).
+// TFLOP/s, 681 with GELU, which the vector units compute for every result while no other workgroup multiplies.  20 000 x 768 -> 768: 31 us, 37 with GELU, 53
+// with SiLU, its slope and a residual (124 MB at 2.3 TB/s; tiles of 64, 128 and 256 are level; the residual's rows are asked for before the activation).
 // Unaligned: 30 001 x 333 -> 777 61 us, 255 TFLOP/s.  fp32 runs six products of bf16 pieces: 1032 x 3696 -> 2920 197 us, 113 TFLOP/s of fp32.
 #pragma once
 #include "matrix_frag.hpp"

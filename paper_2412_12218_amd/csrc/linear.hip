@@ -8,7 +8,7 @@
 // (P in bf16 would move dP by a third of its own rounding), and the backward pass needs no activation function.  dP is rounded to the type of
 // X for the products; db is the sum of the unrounded ones.
 //
-// A training step of 20 000 x 768 -> 768 in bf16 (SiLU, bias, residual) takes 164 us: Z 57, dP and its sums 21 (92 MB at 4.4 TB/s), db 6, dX 35, dW 42 in twelve
+// A training step of 20 000 x 768 -> 768 in bf16 (SiLU, bias, residual) takes 164 us: Z 53, dP and its sums 21 (92 MB at 4.4 TB/s), db 6, dX 35, dW 42 in twelve
 // parts and 8 to join them.
 #include "dense_kernel.hpp"
 
