@@ -133,6 +133,18 @@ def test_masks_that_leave_nothing_and_what_they_hide(dtype):
     assert bool((got["out"][:50] == 0).all()) and bool((got["dQ"][:50] == 0).all()) and bool((got["dK"][hidden] == 0).all())
 
 
+MANY = {"empty first": [0] * 700 + [300] + [1] * 200 + [64, 5] * 40, "large first": [900, 500] + [2] * 300 + [0] * 400 + [70],
+        "large last": [1, 0, 3] * 150 + [600], "all empty but one": [0] * 333 + [41] + [0] * 500}
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens", MANY.values(), ids=MANY.keys())
+def test_many_graphs_of_very_different_sizes(dtype, lens):
+    """A tile's graph is far from where it would be among graphs of one size."""
+    Batch(lens, 3, 1, 16, dtype, masked=0.1, before=5, behind=2, seed=15).check(f"{dtype} {len(lens)} graphs")
+    Batch(lens, 2, 2, 16, dtype, qlens=[1] * len(lens), seed=16).check(f"{dtype} {len(lens)} readouts")
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_one_side_empty(dtype):
     """No key, or no query, in any graph: zeros on the other side, nothing read."""
