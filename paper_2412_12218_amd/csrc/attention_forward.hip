@@ -5,7 +5,7 @@
 //
 // Bound by the exponentials and what a softmax does beside the products for D up to 64 (48 graphs of 1 to 799 nodes, 8 heads, D = 64, bf16 62 us, 313
 // TFLOP/s), for D = 128 by both (5 graphs of 1 to 7999 nodes, 12 heads over 4, fp16 805 us, 806 TFLOP/s); readouts by the rows' bytes (12 graphs of 1 to 19 999 nodes, 17 us, 3.6 TB/s,
-// and 7 to join 39 parts); batches of small graphs by the latency of three dependent loads a workgroup (2000 molecules, fp32 38 us).
+// and 4 to join 39 parts); batches of small graphs by the latency of three dependent loads a workgroup (2000 molecules, fp32 38 us).
 #include "attention_common.hpp"
 
 namespace ftc {

@@ -4,18 +4,27 @@
 
 namespace ftc {
 
-// Adds up the parts of the forward pass, WAVES waves a query and head, which take the parts in turn; at most 64 parts, lane z has the maximum
-// and the sum of part z.  Rows that belong to no graph stay as they are.
+// Adds up the parts of the forward pass, WAVES waves a query and head, which take the parts in turn, at most JOIN_EACH each: all of them on their way before
+// anything is known about them (7.2 us for 96 rows of 39 parts, 3.9 so).  Lane z has the maximum and the sum of part z.  Rows that belong to no graph stay as they are.
+constexpr int JOIN_EACH = 16;
 template <class T, int WAVES>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
 {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, mine = wave % WAVES;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, mine = __builtin_amdgcn_readfirstlane(wave % WAVES);
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / WAVES) + wave / WAVES, all = static_cast<int64_t>(a.n_q) * a.heads;
     if (row >= all) return;
-    const int query = static_cast<int>(row / a.heads), head = static_cast<int>(row % a.heads);
-    if (!in_a_graph(a.q_ptr, a.graphs, a.n_q, query)) return;  // of WAVES = 4 the whole workgroup
+    float v[2][JOIN_EACH];  // columns lane and lane + 64
+#pragma unroll
+    for (int i = 0; i < JOIN_EACH; ++i) {
+        const int z = mine + i * WAVES;
+        const float *part = a.part + (z * all + row) * a.D;
+        v[0][i] = z < a.splits ? part[lane < a.D ? lane : 0] : 0.f;
+        v[1][i] = z < a.splits && a.D > 64 ? part[lane + 64 < a.D ? lane + 64 : 0] : 0.f;
+    }
     float2 ml = {-INFINITY, 0.f};
     if (lane < a.splits) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (lane * all + row));
+    const int query = static_cast<int>(row / a.heads), head = static_cast<int>(row % a.heads);
+    if (!in_a_graph(a.q_ptr, a.graphs, a.n_q, query)) return;  // of WAVES = 4 the whole workgroup
     float m = ml.x;
 #pragma unroll
     for (int b = 1; b < 64; b *= 2) m = fmaxf(m, __shfl_xor(m, b, 64));
@@ -26,13 +35,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
     __shared__ float sums[WAVES][128];
-    float x[2] = {0.f, 0.f};  // columns lane and lane + 64
-#pragma unroll 8
-    for (int z = mine; z < a.splits; z += WAVES) {
-        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), __builtin_amdgcn_readfirstlane(z)));
-        const float *part = a.part + (z * all + row) * a.D;
-        x[0] = fmaf(part[lane < a.D ? lane : 0], w, x[0]);
-        if (a.D > 64) x[1] = fmaf(part[lane + 64 < a.D ? lane + 64 : 0], w, x[1]);
+    float x[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < JOIN_EACH; ++i) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), mine + i * WAVES));  // 0 behind the last part
+        x[0] = fmaf(v[0][i], w, x[0]);
+        x[1] = fmaf(v[1][i], w, x[1]);
     }
     if constexpr (WAVES > 1) {
         sums[mine][lane] = x[0];
@@ -185,7 +193,7 @@ static void forward(AttnArgs a, int dtype, void *ws, hipStream_t s)
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + align_up(static_cast<size_t>(a.splits) * rows * a.D * sizeof(float), 256));
     const unsigned grid = attn_grid(a, virt, nw);
     launch_attention_forward(a, dtype, nw, whole, grid, s);
-    if (a.splits >= 16) FTC_ATTN_TYPED_N(attention_join_kernel, 4, rows, a);
+    if (a.splits > JOIN_EACH) FTC_ATTN_TYPED_N(attention_join_kernel, 4, rows, a);
     else if (a.splits > 1) FTC_ATTN_TYPED_N(attention_join_kernel, 1, (rows + 3) / 4, a);
 }
 
