@@ -18,6 +18,7 @@
 // with SiLU, its slope and a residual (124 MB at 2.3 TB/s; tiles of 64, 128 and 256 are level; the residual's rows are asked for before the activation).
 // Unaligned: 30 001 x 333 -> 777 61 us, 255 TFLOP/s.  fp32 runs six products of bf16 pieces: 1032 x 3696 -> 2920 197 us, 113 TFLOP/s of fp32.
 #pragma once
+#include "dense_plan.hpp"
 #include "matrix_frag.hpp"
 
 namespace ftc {
@@ -32,10 +33,6 @@ struct DenseArgs {
     int64_t ldr, lds, ldo;
     int act, out_dtype;
 };
-
-// Tiles of the result.
-enum { DENSE_64 = 0, DENSE_128 = 1, DENSE_256 = 2 };
-constexpr int dense_side(int tile) { return 64 << tile; }
 
 // One launch for each place of the operands' rows: Z (A along, B across), dX (both along), dW (both across).
 template <bool AX, bool BX>

@@ -141,51 +141,6 @@ extern template void launch_dense<false, true>(const DenseArgs &a, int dtype, in
 extern template void launch_dense<false, false>(const DenseArgs &a, int dtype, int tile, hipStream_t s);
 extern template void launch_dense<true, true>(const DenseArgs &a, int dtype, int tile, hipStream_t s);
 
-struct DensePlan {
-    int tile, splits, k_each;
-};
-
-static int64_t dense_tiles(int M, int N, int tile) { return static_cast<int64_t>(ceil_div(M, dense_side(tile))) * ceil_div(N, dense_side(tile)); }
-
-// Tile and parts of the contraction by an estimate of the time.  A step (128 bytes of the contraction) of a workgroup takes `alone` where it
-// has a compute unit to itself and `shared` for each of the workgroups of one that is full, `most` of them; parts cost the second kernel, and
-// writing and reading them once.  us, from products of 8192^3 (1780 with tiles of 64 / 1080 of 128 / 900 of 256), 4096 x 1024 x 1024 (16 / 15 / 31
-// for Z, 22 / 25 / 30 for dW at the best number of parts), 20 000 x 768 x 768 (40 / 34 / 30, 52 / 49 / 50) and 65 536 x 1024 x 4096
-// (852 / 652 / 582, 1000 / 596 / 485), the last two with parts of up to 16 tried: more lose (4096 x 1024 x 1024, dW of 2 / 4 / 8 / 16 parts: 28 / 25 / 27 / 39).  fp32, tiles of 64 / 128:
-// 16 384 x 2048 x 2048 1069 / 748, 1032 x 3696 x 2920 209 / 180, 2708 x 1432 x 128 21 (four parts) / 25 (six).
-struct DenseCost {
-    float alone, shared;
-    int most;
-};
-static DensePlan dense_plan(int M, int N, int K, bool f32, bool fast)
-{
-    static constexpr DenseCost cost[2][3] = {{{0.45f, 0.22f, 5}, {0.79f, 0.53f, 2}, {1.74f, 1.74f, 1}}, {{0.75f, 0.49f, 4}, {1.55f, 1.46f, 2}, {0.f, 0.f, 0}}};
-    constexpr float JOIN_US = 5.f, PART_BYTES_US = 4e6f;
-    DensePlan best = {DENSE_64, 1, 64};
-    if (M < 1 || N < 1 || K < 1) return best;
-    float least = INFINITY;
-    const int step = f32 ? 32 : 64;
-    for (int tile = DENSE_64; tile <= (fast && !f32 ? DENSE_256 : DENSE_128); ++tile) {
-        const DenseCost &c = cost[f32][tile];
-        const float alone = fast ? c.alone : 1.5f * c.alone;  // rows that are not whole pieces: through registers
-        const int64_t tiles = dense_tiles(M, N, tile);
-        for (int want = 1; want <= 64; want = want < 8 ? want + 1 : want + want / 4) {
-            DensePlan p = {tile, 1, static_cast<int>(align_up(ceil_div(K, want), 64))};
-            p.splits = ceil_div(K, p.k_each);
-            if (p.splits != want) continue;
-            const int64_t groups = tiles * p.splits, room = 256ll * c.most, full = groups / room, rest = groups % room;
-            const auto each = [&](int64_t n) { return n * c.shared > alone ? n * c.shared : alone; };
-            float us = ceil_div(p.k_each, step) * (full * each(c.most) + (rest ? each((rest + 255) / 256) : 0.f));
-            if (p.splits > 1) us += JOIN_US + 8.f * p.splits * M * N / PART_BYTES_US;
-            if (us < least) {
-                least = us;
-                best = p;
-            }
-            if (tiles * want >= 2048) break;  // more workgroups than the chip holds
-        }
-    }
-    return best;
-}
 static size_t dense_ws(int M, int N, int K)
 {
     int most = 1;
