@@ -178,12 +178,15 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
         for (int d = 0; d < DT; ++d) dq[d] -= rest * mean[MEAN ? d : 0];
     }
     if (!there) return;
+    const bool none = lse == -INFINITY;  // without a key dq is zero, and not what hidden ones, zeros in LDS, make of a query of NaN or infinities
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const int c = 32 * d + 8 * b + 4 * half;
-            const float x[4] = {dq[d][4 * b] * a.scale, dq[d][4 * b + 1] * a.scale, dq[d][4 * b + 2] * a.scale, dq[d][4 * b + 3] * a.scale};
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = none ? 0.f : dq[d][4 * b + i] * a.scale;
             if (a.splits > 1) store_four<F32>(a.part, (static_cast<int64_t>(here.part) * a.n_q * a.heads + at) * a.D + c, a.D - c, x);
             else store_four<T>(a.dQ, query * a.lddq + head * a.D + c, a.D - c, x);
         }

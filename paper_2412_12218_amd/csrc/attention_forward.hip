@@ -119,6 +119,19 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
     }
     l = both_halves_sum(l);
+    // A query that holds NaN or an infinity makes NaN of hidden keys, which are zeros in LDS.  Where a key is seen the row is NaN anyway; where none is, as
+    // in a graph of padding, the row has no weights.
+    if (__builtin_amdgcn_ballot_w64(l != l)) {
+        bool sees = false;
+        const int end = min(k1, k0 + last * TK);
+        for (int j = k0 + first * TK + lane; j < end; j += 64) sees = sees || !a.mask || a.mask[j];
+        if (!__builtin_amdgcn_ballot_w64(sees)) {
+            m = -INFINITY;
+            l = 0.f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = zero16();
+        }
+    }
     m *= scale2;
     if (!there) return;
     if (a.splits > 1) {
