@@ -13,6 +13,7 @@ namespace ftc {
 template <class T, int DP, int NW, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void attention_forward_kernel(AttnArgs a)
 {
+#pragma clang fp contract(off)  // m scale2 is the same rounded number wherever it is used
     constexpr int TQ = 32 * NW, TK = key_rows<T, NW>(), SUB = TK / 32, KS = DP / 16, DT = DP / 32, BUFFERS = tile_buffers<NW>();
     typedef LdsTile<T, DP> L;
     typedef Keys<T, DP, TK, 64 * NW, WHOLE> Tiles;
@@ -67,7 +68,9 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
         }
         const float m_new = fmaxf(m, both_halves_max(top)), shift = m_new == -INFINITY ? 0.f : m_new * scale2;
         if (__builtin_amdgcn_ballot_w64(m_new != m)) {
-            const float fade = __builtin_amdgcn_exp2f(fmaf(m, scale2, -shift));
+            // between the shifts that the exponentials were and will be taken with, as they are rounded: exactly one where the maximum stays
+            // (fma(m, scale2, -shift) is the residue of a rounding there, which each tile that another row of the wave needs it for would leave in l and o: lse off by 6e-4 after 8000 keys, 1e-5 so)
+            const float fade = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * scale2 - shift);
             l *= fade;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= fade;

@@ -1,8 +1,9 @@
-"""Attention where numbers are unusual: rows without a key that hold NaN."""
+"""Attention where numbers are unusual: rows without a key that hold NaN, long rows whose maximum stays while others' rises."""
 import pytest
 import torch
 
-from test_gpu_graph_attention import DTYPES, Batch
+from paper_2412_12218_amd import binding as B
+from test_gpu_graph_attention import DTYPES, Batch, offsets
 from test_gpu_graph_attention_whole import Whole
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +49,32 @@ def test_rows_that_hold_nan_and_see_a_key(kind, dtype, lens, qlens):
     keep = torch.arange(b.n_q, device="cuda") != 1
     assert torch.equal(got["out"][keep], clean["out"][keep]) and torch.equal(got["lse"][keep], clean["lse"][keep])
     assert bool(got["out"][1].isnan().all()) and bool(got["lse"][1].isnan().all())
+
+
+def test_long_rows_beside_rows_whose_maximum_rises():
+    """Every 32nd query finds a larger score in every tile of keys; the largest of the others is that of the first key, 40 to 60, which has about half of
+    their weight, and the other 8191 share the rest.  Weights that the first key has must not change with the tiles that follow: out in
+    column 0 is p_0 - (1 - p_0).
+
+    lse is a sum with roundings of half a step of 16 to 128 each (score 1.9e-6, in base two 2.6e-6, result 1.9e-6) and of the sum itself, 4096 additions
+    in a lane, half a step of 0.5 to 1 each with random signs: 64 / sqrt(3) 2^-25, five times that 5.5e-6: 1.2e-5; out the same in p_0 (1 - p_0) twice, and
+    8192 additions into a sum of up to 1: five times 90 / sqrt(3) 2^-25, 8e-6: 1.4e-5.  Both are given twice that."""
+    n_q, n, D = 33_024, 8192, 16   # enough queries that the keys stay in one part
+    gen = torch.Generator().manual_seed(5)
+    Q, K, V = torch.zeros((n_q, D)), torch.zeros((n, D)), torch.randn((n, D), generator=gen)
+    Q[:, 1] = 160 + 80 * torch.rand(n_q, generator=gen)
+    Q[::32] = 0
+    Q[::32, 0] = 200.0
+    K[:, 0] = torch.arange(n) / n
+    K[:, 1] = 1 - 36 / 200 * (1 + 0.2 * (torch.rand(n, generator=gen) - 0.5))
+    K[0, 1] = 1
+    V[:, 0], V[0, 0] = -1, 1
+    out, lse = torch.empty((n_q, D), device="cuda"), torch.empty((n_q, 1), device="cuda")
+    B.ftc_graph_attention(Q.cuda(), K.cuda(), V.cuda(), offsets([n_q]), offsets([n]), heads=1, scale=0.25, out=out, lse=lse)
+    for some in (slice(0, 128), slice(16_384, 16_512), slice(n_q - 128, n_q)):
+        s = Q[some].double() @ K.double().t() * 0.25
+        want = torch.softmax(s, 1) @ V.double()
+        off_lse = (lse[some, 0].cpu().double() - torch.logsumexp(s, 1)).abs().max().item()
+        off = (out[some, 0].cpu().double() - want[:, 0]).abs().max().item()
+        print(f"lse {off_lse:.2e}, out {off:.2e}", flush=True)
+        assert off_lse <= 2.4e-5 and off <= 2.8e-5
