@@ -39,15 +39,15 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : 2) void a
     split_row(a, there ? r : 0, query, head);
     query += q0;
     head += here.share * a.group;
-    // scale has the sign of +: the maximum of the products is then that of the scores
-    const float scale2 = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);
+    // scale has the sign of + (turn_query): the maximum of the products is then that of the scores
+    const float scale2 = size_of_scale(a);
     const char *q_row = head_of<T>(a.Q, query, a.ldq, head * a.D);
     Frag<T> q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
         const int c = 16 * s + 8 * half;
         q[s] = operand_at<T, WHOLE>(q_row, c, a.D, there);
-        if (a.scale < 0.f) frag_negate<T>(q[s]);
+        if (a.scale <= 0.f) turn_query<T>(q[s], a.scale);
     }
     float m = -INFINITY, l = 0.f;  // maximum of the products, sum of the exponentials (a half's keys)
     f32x16 o[DT];

@@ -1,4 +1,4 @@
-"""Attention where numbers are unusual: rows without a key that hold NaN, long rows whose maximum stays while others' rises."""
+"""Attention where numbers are unusual: rows without a key that hold NaN, long rows whose maximum stays while others' rises, scales next to zero."""
 import pytest
 import torch
 
@@ -78,3 +78,24 @@ def test_long_rows_beside_rows_whose_maximum_rises():
         off = (out[some, 0].cpu().double() - want[:, 0]).abs().max().item()
         print(f"lse {off_lse:.2e}, out {off:.2e}", flush=True)
         assert off_lse <= 2.4e-5 and off <= 2.8e-5
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-36, -1e-36])
+def test_scales_next_to_zero(dtype, scale):
+    """Products of 1e31 and more: a scale of zero leaves nothing of them, 1e-36 only 1e-4."""
+    for kind, lens in ((Batch, [90, 5, 33]), (Whole, [90, 5, 33]), (Whole, [300, 170])):
+        b = kind(lens, 4, 2, 32, dtype, masked=0.3, seed=13)
+        b.Q.mul_(1e15), b.K.mul_(1e15)
+        b.scale = scale
+        got = b.run(False)
+        at = 0
+        for n in lens:
+            seen = b.mask[at:at + n] != 0
+            s = scale * b.Q[at:at + n, :32].double() @ b.K[at:at + n, :32][seen].double().t()
+            want = torch.softmax(s, 1) @ b.V[at:at + n, :32][seen].double()
+            u = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
+            bound = (2 * u + 2 * (n + 60) * 2.0 ** -24) * b.V.double().abs().max()   # p and out are rounded, sums of n and of 32 products
+            off = (got["out"][at:at + n, :32].double() - want).abs().max()
+            assert off <= bound, (lens, float(off), float(bound))
+            at += n
