@@ -437,7 +437,7 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
  * and the rows kv_ptr[g] .. kv_ptr[g+1] of K and V (device int32, n_graphs + 1 entries, non-decreasing; the same
  * array where every node attends to every node; one query a graph: a readout).  Head h has columns h D .. of Q and
  * out, and columns (h / (heads / kv_heads)) D .. of K and V: kv_heads divides heads.  Q, K, V may be column ranges of one matrix.
- *   s_ij = scale <q_i, k_j>,  p = softmax over the keys j of the graph with kv_mask[j] != 0,  out_i = sum_j p_ij v_j.
+ *   s_ij = scale <q_i, k_j> (scale: any finite number),  p = softmax over the keys j of the graph with kv_mask[j] != 0,  out_i = sum_j p_ij v_j.
  * kv_mask (n_kv bytes) may be NULL: all keys; K and V of masked keys are not read.  A query without a key gives
  * zeros.  Rows in front of the first and behind the last graph are neither read nor written.  lse (n_q x heads floats, may be NULL)
  * receives log sum_j exp(s_ij) (-inf without a key), what the backward pass needs.  All matrices are of `dtype`; D <= 128,

@@ -1,5 +1,6 @@
 // C ABI of libftc: host-side argument validation and dispatch.  See include/ftc.h for the
 // contract of every entry point.
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <mutex>
@@ -953,6 +954,7 @@ static int32_t check_attention(const char *who, const AttnShape &p)
     if (p.heads < 1 || p.kv_heads < 1 || p.heads % p.kv_heads != 0)
         return fail(FTC_EINVAL, "%s: heads must be a multiple of kv_heads, both at least 1", who);
     if (p.D < 1) return fail(FTC_EINVAL, "%s: need D >= 1", who);
+    if (!std::isfinite(p.scale)) return fail(FTC_EINVAL, "%s: scale is not finite", who);
     if (!attention_sizes_ok(p.n_q, p.n_kv, p.graphs, p.heads, p.kv_heads, p.D))
         return fail(FTC_EUNSUPPORTED, "%s: D is at most 128, kv_heads 65535, n_q * heads and n_kv * kv_heads 2^30", who);
     if (!attention_size(p.n_q, p.n_kv, p.graphs, p.heads, p.kv_heads, p.D).fits())
