@@ -240,7 +240,8 @@ class TrainPath:
 class GraphTransformerPath:
     """Forward + backward of a graph transformer on a packed batch of graphs: node features looked up by id, layers of attention
     between all nodes of a graph and of a feed-forward block (GELU), each with a residual connection around it, and a linear
-    head on every node.  graph_ptr: device int32, the graphs' first nodes and the end (n); heads share kv_heads K/V heads.
+    head on every node.  graph_ptr: device int32, the graphs' first nodes and the end, which is n (nodes that fill a batch up are a graph of their
+    own, masked); heads share kv_heads K/V heads.
 
     Weights are a dict: "table" (vocab x d), "head" and "head_bias", and "layers", a list of dicts "qkv" (d x (heads + 2 kv_heads) d / heads),
     "out" (d x d), "up" (d x hidden), "down" (hidden x d) with a bias each ("qkv_bias", ...).  Gradients come in the same shape, in fp32.
@@ -278,8 +279,13 @@ class GraphTransformerPath:
         q, k, v = (self.qkv[layer][:, c] for c in self.columns)
         return (q, k, v, self.graph_ptr, self.graph_ptr), dict(heads=self.heads, kv_heads=self.kv_heads, kv_mask=mask, ws=self.ws)
 
+    def _check_layers(self, weights):
+        if len(weights["layers"]) != self.layers:
+            raise ValueError(f"weights of {len(weights['layers'])} layers for a path of {self.layers} layers")
+
     def forward(self, ids, weights, mask=None):
-        """Logits (n x n_out).  mask: nodes with 0 are attended to by no node."""
+        """Logits (n x n_out), in the path's buffer.  mask: nodes with 0 are attended to by no node."""
+        self._check_layers(weights)
         B.ftc_embedding(ids, weights["table"], scale=self.scale, out=self.h[0])
         for i, w in enumerate(weights["layers"]):
             B.ftc_linear(self.h[i], w["qkv"], bias=w["qkv_bias"], out=self.qkv[i], ws=self.ws)
@@ -291,7 +297,8 @@ class GraphTransformerPath:
         return B.ftc_linear(self.h[-1], weights["head"], bias=weights["head_bias"], out=self.logits, ws=self.ws)
 
     def backward(self, ids, weights, d_out, mask=None):
-        """d_out = dL/d(logits), in the activation type; gradients of the weights that forward() was given."""
+        """d_out = dL/d(logits), in the activation type; gradients of the weights that forward() was given, with the mask that it was given."""
+        self._check_layers(weights)
         grads, back = dict(layers=[{} for _ in weights["layers"]]), B.ftc_linear_backward
         _, grads["head"], grads["head_bias"] = back(self.h[-1], weights["head"], d_out, dX=self.d_h, ws=self.ws)
         for i in reversed(range(self.layers)):
