@@ -18,6 +18,7 @@
 // with SiLU, its slope and a residual (124 MB at 2.3 TB/s; tiles of 64, 128 and 256 are level; the residual's rows are asked for before the activation).
 // Unaligned: 30 001 x 333 -> 777 61 us, 255 TFLOP/s.  fp32 runs six products of bf16 pieces: 1032 x 3696 -> 2920 197 us, 113 TFLOP/s of fp32.
 #pragma once
+#include "bf16_split.hpp"
 #include "dense_plan.hpp"
 #include "matrix_frag.hpp"
 
@@ -237,9 +238,9 @@ struct Operand {
     }
 };
 
-// A wave's blocks of an fp32 product once more, from memory and on the fp32 instruction, for the sums that the pieces left not finite.
+// A wave's blocks of an fp32 product from memory and on the fp32 instruction: the sums that the pieces left not finite, or (all) every one.
 template <bool AX, bool BX, int WM, int WN>
-__device__ __forceinline__ void dense_again(const DenseArgs &a, int row0, int col0, int k_begin, int k_end, f32x16 (&c)[WM][WN])
+__device__ __forceinline__ void dense_again(const DenseArgs &a, int row0, int col0, int k_begin, int k_end, bool all, f32x16 (&c)[WM][WN])
 {
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const float *A = static_cast<const float *>(a.A), *B = static_cast<const float *>(a.B);
@@ -256,7 +257,7 @@ __device__ __forceinline__ void dense_again(const DenseArgs &a, int row0, int co
                 sum = __builtin_amdgcn_mfma_f32_32x32x2f32(y, x, sum, 0, 0, 0);
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) c[i][j][e] = fabsf(c[i][j][e]) < INFINITY ? c[i][j][e] : sum[e];
+            for (int e = 0; e < 16; ++e) c[i][j][e] = !all && fabsf(c[i][j][e]) < INFINITY ? c[i][j][e] : sum[e];
         }
 }
 
@@ -325,7 +326,9 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
     };
     OA oa;
     OB ob;
-    if constexpr (FAST) {
+    const bool few = T::BYTES == 4 && a.K <= SPLIT_FROM;  // uniform: sums that pieces would be further off in (bf16_split.hpp)
+    if (few) {
+    } else if constexpr (FAST) {
         const int64_t da = (AX ? STEP * a.lda : STEP) * T::BYTES, db = (BX ? STEP * a.ldb : STEP) * T::BYTES;
         const int whole = (k_end - k_begin) / STEP, left = (k_end - k_begin) % STEP;
         oa.aim(a.A, a.lda, m0, a.M, k_begin);
@@ -395,7 +398,7 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
             for (int j = 0; j < WN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) finite = finite && fabsf(c[i][j][e]) < INFINITY;
-        if (__builtin_amdgcn_ballot_w64(!finite)) dense_again<AX, BX, WM, WN>(a, m0 + wm, n0 + wn, k_begin, k_end, c);
+        if (few || __builtin_amdgcn_ballot_w64(!finite)) dense_again<AX, BX, WM, WN>(a, m0 + wm, n0 + wn, k_begin, k_end, few, c);
     }
     // A wave's 32 rows through LDS, where no other wave looks any more: neighbouring lanes then have neighbouring columns.
     constexpr int WIDTH = 32 * WN, PITCH = WIDTH * 4 + 16, EIGHTS = WIDTH / 8;
