@@ -1,4 +1,4 @@
-"""The dense layer in fp32: short contractions."""
+"""The dense layer in fp32: short contractions, numbers next to the smallest."""
 import numpy as np
 import pytest
 import torch
@@ -30,3 +30,24 @@ def test_sums_of_up_to_four_products(few, rows, cols):
         compare("dX", B.ftc_linear_backward(randn(rows, cols_, 5), W, G, want_dW=False, want_db=False)[0], G, W.t())
         X, G = randn(few, rows, 6), randn(few, cols_, 7)
         compare("dW", B.ftc_linear_backward(X, randn(rows, cols_, 8), G, want_dX=False, want_db=False)[1], X.t(), G)
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(70, 64, 128), (300, 33, 65), (2900, 72, 1028), (2561, 35, 1537), (5, 5000, 70)])
+def test_small_numbers(n, d_in, d_out):
+    """Numbers below 2^-110 against others of 2^100: held to 2^-134, half a step of the smallest bf16 numbers, in every row or in some of them.  Those of
+    2^-108 are held in 24 bits."""
+    def sized(n, d, seed):
+        t = randn(n, d, seed)
+        return torch.sign(t) * (t.abs() % 1.0 + 0.5)    # no number far below the others
+    for least, every in ((-118, 1), (-118, 37), (-124, 1), (-108, 1)):
+        X, W, G = sized(n, d_in, 1), sized(d_in, d_out, 2) * 2.0 ** 100, sized(n, d_out, 3)
+        small = torch.where(torch.arange(n, device="cuda") % every == 0, 2.0 ** least, 2.0 ** -100)[:, None]
+        X, G = X * small, G * small
+        dX = B.ftc_linear_backward(X, W, G, want_dW=False, want_db=False)[0]
+        dW = B.ftc_linear_backward(X * 2.0 ** 100 * 2.0 ** 100, W, G, want_dX=False, want_db=False)[1]
+        x, w, g = f64(X), f64(W), f64(G)
+        for name, got, a, b in (("Z", B.ftc_linear(X, W), x, w), ("dX", dX, g, w.T), ("dW", dW, x.T * 2.0 ** 200, g)):
+            held = 2.0 ** -134 * (np.abs(a) < 2.0 ** -109) if name != "dW" else np.zeros_like(a)
+            other = 2.0 ** -134 * (np.abs(b) < 2.0 ** -109) if name == "dW" else np.zeros_like(b)
+            bound = np.abs(a) @ np.abs(b) * (a.shape[1] + 8) * S + held @ np.abs(b) + np.abs(a) @ other
+            check(f"{name} {n} {d_in} {d_out} 2^{least} every {every}", got, a @ b, bound)
