@@ -1,4 +1,6 @@
-"""The dense layer in fp32: short contractions, numbers next to the smallest."""
+"""The dense layer in fp32: short contractions, numbers next to the smallest, and GELU."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -51,3 +53,23 @@ def test_small_numbers(n, d_in, d_out):
             other = 2.0 ** -134 * (np.abs(b) < 2.0 ** -109) if name == "dW" else np.zeros_like(b)
             bound = np.abs(a) @ np.abs(b) * (a.shape[1] + 8) * S + held @ np.abs(b) + np.abs(a) @ other
             check(f"{name} {n} {d_in} {d_out} 2^{least} every {every}", got, a @ b, bound)
+
+
+def test_gelu():
+    """GELU and its slope at numbers between -9 and 9 in fp32.  z = p Phi(p): Phi(-a) = erfc(a / sqrt 2) / 2 is off by some steps (given eight) and by
+    that of its argument, whose rounding (half a step, twice) moves it by a^2 half steps; Phi(a) = 1 - Phi(-a).  The slope adds p phi(p), off by a few steps and, by its
+    exponent's rounding, by p^2 / 2."""
+    p = torch.linspace(-9, 9, 65_536 + 7)
+    n, few = 5, p.numel()
+    X, W, slope = torch.zeros((n, 3), device="cuda"), torch.zeros((3, few), device="cuda"), torch.empty((n, few), device="cuda")
+    out = B.ftc_linear(X, W, bias=p.cuda(), act=B.FTC_ACT_GELU, slope=slope)
+    one = B.ftc_linear(X[:1], W, bias=p.cuda(), act=B.FTC_ACT_GELU)
+    q = p.double()
+    cdf, pdf = 0.5 * torch.erfc(-q / math.sqrt(2)), torch.exp(-0.5 * q * q) / math.sqrt(2 * math.pi)
+    small = 0.5 * torch.erfc(q.abs() / math.sqrt(2))
+    off_cdf = (8 + 2 * q * q) * S * small + torch.where(q > 0, 2 * S, 0.0)
+    bound = q.abs() * off_cdf + 4 * S * (q * cdf).abs() + 2.0 ** -140
+    for got in (out, one):
+        check("GELU", got, (q * cdf).expand(got.shape).numpy(), bound.expand(got.shape).numpy())
+    steep = off_cdf + q.abs() * pdf * (8 + 2 * q * q) * S + 4 * S * (cdf + q * pdf).abs() + 2.0 ** -140
+    check("slope", slope, (cdf + q * pdf).expand(slope.shape).numpy(), steep.expand(slope.shape).numpy())
