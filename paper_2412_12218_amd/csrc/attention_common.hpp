@@ -203,18 +203,18 @@ __device__ __forceinline__ Frag<T> operand_at(const char *row, int c, int D, boo
 }
 
 // A query for a scale that is not positive: the kernels multiply by its size, so that -infinity stays what hides a key.  Zero leaves nothing of a product but NaN.
-template <class T>
-__device__ __forceinline__ void turn_query(Frag<T> &q, float scale)
+template <class T, int N>
+__device__ __forceinline__ void turn_query(Frag<T> (&q)[N], float scale)
 {
-    if (scale < 0.f) {
-        frag_negate<T>(q);
-        return;
-    }
-    float x[8];
-    frag_numbers<T>(q, x);
+    if (scale > 0.f) return;  // uniform
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= scale;
-    q = frag_of<T>(x);
+    for (int s = 0; s < N; ++s) {
+        float x[8];
+        frag_numbers<T>(q[s], x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = scale < 0.f ? -x[j] : x[j] * 0.f;
+        q[s] = frag_of<T>(x);
+    }
 }
 // For exponentials in base two; a normal number, so that -infinity times it is one.
 __device__ __forceinline__ float size_of_scale(const AttnArgs &a) { return fmaxf(fabsf(a.scale) * LOG2E, 0x1p-126f); }

@@ -49,9 +49,9 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
     for (int s = 0; s < KS; ++s) {
         const int c = 16 * s + 8 * half;
         q[s] = operand_at<T, WHOLE>(q_row, c, a.D, there);
-        if (a.scale <= 0.f) turn_query<T>(q[s], a.scale);
         g[s] = operand_at<T, WHOLE>(g_row, c, a.D, there);
     }
+    turn_query<T>(q, a.scale);
     // scale has the sign of + (turn_query), which the -infinity of hidden keys keeps
     const float scale2 = size_of_scale(a);
     const int64_t at = static_cast<int64_t>(query) * a.heads + head;
