@@ -31,6 +31,7 @@ struct AttnArgs {
     float *delta;     // n_q x heads
     float *part;      // parts of split sums
     float *part_ml;   // their maxima and sums
+    float *part_mean, *part_rest;  // dQ in parts, D up to 32 in 16 bits: of p k, and of ds
     const int *q_ptr, *kv_ptr;
     const uint8_t *mask;
     int64_t ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv;
@@ -325,6 +326,7 @@ __device__ __forceinline__ Frag<T> rest_of(const f32x16 &c, int step, const Frag
 // of one tile, whose few sums do not average it (three nodes, D = 37, bf16: 1.69 times), and which are bound by latency.
 template <class T, int DP>
 constexpr bool ds_in_two() { return T::BYTES == 2 && DP == 32; }
+constexpr bool delta_settled(int D) { return D <= 32; }  // by the dQ kernel, in 16 bits
 
 // Probabilities are 2^p_bits() times as large in fp16: one key of a hundred thousand has 1e-5, which fp16 holds with 8 bits, and 2^15 p with 11; the
 // largest is 2^15.  Sums of them are taken back in fp32.

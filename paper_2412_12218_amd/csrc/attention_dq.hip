@@ -3,7 +3,7 @@
 // delta' = <dO, out> carries the rounding of a 16-bit out, which in dQ shows beside that of ds (D = 8, graphs of 65 to 140 nodes: 1.62 times
 // the error of a result that is only rounded; 1.5 without it).  What is wrong with it is the sum of ds, which should be zero:
 // delta = delta' + sum_j ds'_j, which the dK / dV kernel finds in its place, and dQ = scale (sum_j ds'_j k_j - (sum_j ds'_j) sum_j p_j k_j), for which
-// the kernels with D up to 32 add up p k in one more product (D = 64, 48 x 400 nodes: 1.46 times the error without and 1.43 with it, but
+// the kernels with D up to 32 add up p k in one more product (keys in parts: attention_settle_kernel puts the sums together; D = 64, 48 x 400 nodes: 1.46 times the error without and 1.43 with it, but
 // 75 and 93 us).  Where one tile holds all keys delta is the sum of
 // p <dO, v> from the start: one key gives ds = 0 exactly.
 //
@@ -177,7 +177,9 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
 #pragma unroll
         for (int d = 0; d < DT; ++d) dq[d] -= rest * mean[MEAN ? d : 0];
     }
+    if (MEAN && a.splits > 1) rest = both_halves_sum(rest);
     if (!there) return;
+    const int64_t part = static_cast<int64_t>(here.part) * a.n_q * a.heads + at;
     const bool none = lse == -INFINITY;  // without a key dq is zero, and not what hidden ones, zeros in LDS, make of a query of NaN or infinities
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -187,9 +189,17 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
             float x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = none ? 0.f : dq[d][4 * b + i] * a.scale;
-            if (a.splits > 1) store_four<F32>(a.part, (static_cast<int64_t>(here.part) * a.n_q * a.heads + at) * a.D + c, a.D - c, x);
+            if (a.splits > 1) store_four<F32>(a.part, part * a.D + c, a.D - c, x);
             else store_four<T>(a.dQ, query * a.lddq + head * a.D + c, a.D - c, x);
+            if constexpr (MEAN) {
+                if (a.splits > 1) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = none ? 0.f : mean[d][4 * b + i] * a.scale;
+                    store_four<F32>(a.part_mean, part * a.D + c, a.D - c, x);
+                }
+            }
         }
+    if (MEAN && a.splits > 1 && half == 0) a.part_rest[part] = none || tiles == 1 ? 0.f : rest;
 }
 
 template <class T, int DP, int NW>

@@ -106,6 +106,26 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(const float *__restr
     store_elem(out, row * ld + c, DT, x);
 }
 
+// dQ of parts with their sums of ds, and delta with them (attention_dq.hip).
+template <class T>
+__global__ __launch_bounds__(256) void attention_settle_kernel(AttnArgs a)
+{
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, rows = static_cast<int64_t>(a.n_q) * a.heads;
+    const int64_t row = id / a.D;
+    const int c = static_cast<int>(id % a.D), query = static_cast<int>(row / a.heads), head = static_cast<int>(row % a.heads);
+    if (row >= rows || !in_a_graph(a.q_ptr, a.graphs, a.n_q, query)) return;
+    float x = 0.f, mean = 0.f, rest = 0.f;
+#pragma unroll 8
+    for (int z = 0; z < a.splits; ++z) {
+        x += a.part[z * rows * a.D + id];
+        mean += a.part_mean[z * rows * a.D + id];
+        rest += a.part_rest[z * rows + row];
+    }
+    constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
+    store_elem(a.dQ, query * a.lddq + head * a.D + c, DT, fmaf(-rest, mean, x));
+    if (c == 0) a.delta[row] += rest;
+}
+
 // ---- launches ----------------------------------------------------------------------------------------------------
 // Waves of a workgroup: one for short graphs, whose rows would not fill four, else four, which share the other side's tiles.  us of the forward and
 // backward passes with one and four, 50 000 nodes, 8 heads: bf16, D = 64, graphs of 80 nodes 49 / 59 and 197 / 220, of 100 57 / 52 and 223 / 198,
@@ -156,7 +176,7 @@ size_t attention_backward_ws(int n_q, int n_kv, int graphs, int heads, int kv_he
 {
     const int64_t rows = static_cast<int64_t>(n_q) * heads, group = heads / kv_heads;
     const int sq = attn_splits(n_q * group, n_kv, graphs, kv_heads, D), sk = attn_splits(n_kv, n_q * group, graphs, kv_heads, D);
-    const size_t parts_q = sq > 1 ? static_cast<size_t>(sq) * rows * D * sizeof(float) : 0;
+    const size_t parts_q = sq > 1 ? static_cast<size_t>(sq) * rows * (delta_settled(D) ? 2 * D + 1 : D) * sizeof(float) : 0;
     const size_t parts_k = sk > 1 ? static_cast<size_t>(sk) * 2 * n_kv * kv_heads * D * sizeof(float) : 0;
     return align_up(static_cast<size_t>(rows) * sizeof(float), 256) + align_up(parts_q > parts_k ? parts_q : parts_k, 256);
 }
@@ -208,11 +228,19 @@ static void backward(AttnArgs a, int dtype, void *ws, hipStream_t s)
         FTC_ATTN_TYPED(attention_delta_kernel, (rows + 15) / 16 < DELTA_GROUPS ? (rows + 15) / 16 : DELTA_GROUPS, a);
         const int nw = attn_waves(virt, a.n_kv, a.graphs, a.D);
         a.splits = attn_splits(virt, a.n_kv, a.graphs, a.kv_heads, a.D);
+        a.part_mean = a.part + a.splits * rows * a.D;
+        a.part_rest = a.part_mean + a.splits * rows * a.D;
         const unsigned grid = attn_grid(a, virt, nw);
         launch_attention_dq(a, dtype, nw, whole, grid, s);
         const int width = a.heads * a.D;
         const int64_t count = static_cast<int64_t>(a.n_q) * width;
-        if (a.splits > 1) FTC_ATTN_TYPED(attention_sum_kernel, (count + 255) / 256, a.part, count, a.splits, a.q_ptr, a.graphs, a.n_q, width, a.dQ, a.lddq);
+        const dim3 elements(static_cast<unsigned>((count + 255) / 256));
+        if (a.splits > 1 && dtype != FTC_F32 && delta_settled(a.D)) {
+            if (dtype == FTC_F16) hipLaunchKernelGGL(attention_settle_kernel<F16>, elements, dim3(256), 0, s, a);
+            else hipLaunchKernelGGL(attention_settle_kernel<BF16>, elements, dim3(256), 0, s, a);
+        } else if (a.splits > 1) {
+            FTC_ATTN_TYPED(attention_sum_kernel, elements.x, a.part, count, a.splits, a.q_ptr, a.graphs, a.n_q, width, a.dQ, a.lddq);
+        }
     }
     if (a.n_kv > 0) {
         const int nw = attn_waves(a.n_kv, virt, a.graphs, a.D);
