@@ -390,9 +390,10 @@ int32_t launch_order_by_key(int n, const int *keys_in, int *perm, int *inv, int 
 // ---- positions by id -------------------------------------------------------------------------------
 // The radix sort above with what ids allow: the first pass takes them where they are (an id outside the table as `vocab`, the last key), a workgroup
 // scans the tiles of one digit, and the scatter kernel adds up the digits before its own itself: three launches a pass instead of four and one before all.
-// Up to ID_RANK ids one launch does: a place is the number of ids that are smaller, or equal and before, which eight threads count
-// for each of the 32 ids of a workgroup.
-constexpr int ID_RANK = 4096, ID_RANK_EACH = 32;
+// Few ids take one launch: a place is the number of ids that are smaller, or equal and before, which eight threads count for each of the 32 ids of a
+// workgroup.  Up to ID_RANK_PASS ids for each pass of the sort that this stands for, ID_RANK in all (LDS).  us of a gradient of 64 columns, counted / sorted:
+// 118 rows (one pass) 100 ids 12 / 19, 1000 17 / 19, 2000 21 / 20, 4000 31 / 20, 8000 52 / 21; 30 000 rows (two) 100 ids 14 / 29, 2000 24 / 30, 4000 33 / 32, 8000 53 / 32.
+constexpr int ID_RANK = 4096, ID_RANK_PASS = 1536, ID_RANK_EACH = 32;
 
 __device__ __forceinline__ uint32_t id_key(int id, int vocab) { return static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab); }
 
@@ -542,7 +543,6 @@ static size_t id_array_bytes(int n) { return align_up(static_cast<size_t>(n) * s
 
 size_t id_sort_ws(int n)
 {
-    if (n <= ID_RANK) return 2 * id_array_bytes(n);
     return 4 * id_array_bytes(n) + 512 * sizeof(int) + align_up(static_cast<size_t>(512 * radix_tiles(n, radix_rounds(n))) * sizeof(int), 256);
 }
 
@@ -555,13 +555,13 @@ int32_t launch_sort_ids(int n, const int *ids, int vocab, const uint32_t **keys,
     *keys = k[0];
     *order = v[0];
     if (n == 0) return FTC_OK;
-    if (n <= ID_RANK) {
+    // digits of nine bits where they save a pass (vocab 65 536 to 262 143: two for three)
+    const int rounds = radix_rounds(n), bits = bit_length(static_cast<uint32_t>(vocab)), passes = bits > 9 ? (bits + 8) / 9 : 1;
+    if (n <= ID_RANK && n <= ID_RANK_PASS * passes) {
         hipLaunchKernelGGL(id_rank_kernel, dim3(ceil_div(n, ID_RANK_EACH)), dim3(256), 0, s, n, ids, vocab, k[0], v[0]);
         return launch_status("id sort");
     }
     int *totals = reinterpret_cast<int *>(p + 4 * arr), *table = totals + 512;
-    // digits of nine bits where they save a pass (vocab 65 536 to 262 143: two for three)
-    const int rounds = radix_rounds(n), bits = bit_length(static_cast<uint32_t>(vocab)), passes = bits > 9 ? (bits + 8) / 9 : 1;
     const int digit = bits <= 8 * passes ? 8 : 9;
     const int64_t n_tiles = radix_tiles(n, rounds);
     const dim3 grid(static_cast<unsigned>((n_tiles + 3) / 4));
