@@ -39,8 +39,7 @@ struct DenseArgs {
 template <bool AX, bool BX>
 void launch_dense(const DenseArgs &a, int dtype, int tile, hipStream_t s);
 
-// linear_rows.hip: a few rows of A, B across the contraction or along it
-constexpr int dense_few_rows(bool across) { return across ? 2 : 4; }
+// linear_rows.hip: a few rows of A (dense_few_rows in dense_plan.hpp), B across the contraction or along it
 void launch_dense_rows(const DenseArgs &a, int dtype, bool across, hipStream_t s);
 
 // Rows of whole 16-byte pieces at 16-byte alignment, 256 of them within 2^32 bytes.

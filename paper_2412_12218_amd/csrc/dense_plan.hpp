@@ -1,4 +1,4 @@
-// Which tile and how many parts of the contraction a product of the dense layer takes (linear.hip).  Plain C++, so that a host program can ask.
+// Which kernel, tile and how many parts of the contraction a product of the dense layer takes (linear.hip).  Plain C++, so that a host program can ask.
 #pragma once
 #include <math.h>
 #include <stdint.h>
@@ -54,6 +54,27 @@ inline DensePlan dense_plan(int M, int N, int K, bool f32, bool fast)
         }
     }
     return best;
+}
+
+// Whether M rows take the kernels of linear_rows.hip, which read B once on the vector units (two rows at most where its rows lie across the contraction, four
+// where they lie along it).  A workgroup has the whole contraction there, so long ones take tiles, whose contraction comes in parts; and where B is large what
+// counts is the rate, which tiles of 16-bit numbers have more of.  us of these kernels / of tiles, from Python:
+//   across, bf16, one row   1024 -> 4096 8.1 / 10.9  1024 -> 16 384 8.0 / 8.9  1024 -> 32 768 14.3 / 11.8  2048 -> 8192 14.5 / 11.0  4096 -> 1024 9.3 / 11.0
+//                           4096 -> 2048 13.3 / 11.0  4096 -> 14 336 41.5 / 23.3  16 384 -> 512 37.9 / 11.5;  two rows 2048 -> 2048 9.0 / 11.0  4096 -> 1024 12.8 / 11.1
+//   across, fp32, one row   4096 -> 2048 15.1 / 15.0  4096 -> 8192 26 / 39  8192 -> 1024 26 / 19  8192 -> 4096 31 / 39;  two rows 4096 -> 1024 13.8 / 13.2
+//   along, bf16, one row    4096 <- 4096 9.8 / 12.5  4096 <- 8192 19.7 / 14.5  2048 <- 8192 9.8 / 12.8  1024 <- 16 384 15.8 / 12.9  16 384 <- 2048 16.8 / 15.3
+//                four rows  4096 <- 4096 11.2 / 12.4  2048 <- 4096 10.7 / 12.5  2048 <- 8192 16.4 / 12.5  1024 <- 8192 15.3 / 12.8
+//   1024 -> 4096, bf16, more rows: across four 10.4 / 10.7, eight 17.1 / 10.7, along eight 15.7 / 13.9
+//   along, fp32, two rows   1024 <- 32 768 46 / 47;  four rows 1024 <- 8192 18.3 / 18.9  1024 <- 16 384 34 / 31  2048 <- 16 384 38 / 43  8192 <- 8192 51 / 73
+inline bool dense_few_rows(int M, int N, int K, bool f32, bool across)
+{
+    const int64_t numbers = static_cast<int64_t>(N) * K;
+    if (across) {
+        if (M > 2) return false;
+        return static_cast<int64_t>(K) * M <= 4096 ? f32 || numbers <= (1ll << 34) / K : f32 && N >= 4096;
+    }
+    if (M > 4) return false;
+    return f32 ? M <= 2 || K <= 8192 || K <= 8ll * N : numbers <= 1ll << 24 && K <= (M <= 2 ? 8192 : 4096);
 }
 
 }  // namespace ftc

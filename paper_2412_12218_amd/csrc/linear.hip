@@ -154,7 +154,7 @@ static size_t dense_ws(int M, int N, int K)
 template <bool AX, bool BX>
 static void dense(DenseArgs a, int dtype, void *ws, hipStream_t s)
 {
-    if (!AX && a.M <= dense_few_rows(BX)) {
+    if (!AX && dense_few_rows(a.M, a.N, a.K, dtype == FTC_F32, BX)) {
         launch_dense_rows(a, dtype, BX, s);
         return;
     }
@@ -165,7 +165,8 @@ static void dense(DenseArgs a, int dtype, void *ws, hipStream_t s)
     a.part = static_cast<float *>(ws);
     launch_dense<AX, BX>(a, dtype, p.tile, s);
     if (p.splits > 1) {
-        // a lane a result where there are many, eight for a few results of many parts
+        // a lane a result where there are many, eight for a few results of many parts.  us with one / eight, bf16: 300 x 2000 -> 300 in eight parts
+        // 13.6 / 11.3, 1000 x 3000 -> 100 in twelve 16.7 / 13.3, 512 x 4096 -> 1024 in four 15.9 / 17.8, 768 x 20 000 -> 768 in twelve 50.5 / 51.5
         const int64_t results = static_cast<int64_t>(a.M) * ceil_div(a.N, 8);
         const bool many = results >= (1 << 15) || p.splits < 8;
         const dim3 grid(static_cast<unsigned>(((many ? results : 8 * results) + 255) / 256));

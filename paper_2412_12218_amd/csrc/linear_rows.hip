@@ -1,7 +1,6 @@
 // Products of a few rows: Z = X W (W across the contraction) and dX = dP W^T (W along it).  What they cost is reading W once, and one
-// launch, so the whole contraction of a result stays in one workgroup (wave) on the vector units.  From Python, us, tiles of 64 rows with the
-// contraction in parts and a second kernel / here, bf16 1024 -> 4096: one row Z 11.4 / 7.7, dX 12.8 / 8.9; Z of four rows 10.7 / 10.4 and of eight 10.7 / 17.1, dX
-// of four 13.9 / 9.9 and of eight 13.9 / 15.7: two rows (four for dX) at most.
+// launch, so the whole contraction of a result stays in one workgroup (wave) on the vector units.  dense_few_rows() (dense_plan.hpp) says which
+// products come here, with the times of both sides; tiles of 64 rows there have the contraction in parts and a second kernel.
 #include "dense_kernel.hpp"
 
 namespace ftc {
