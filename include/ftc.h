@@ -441,7 +441,7 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
  *   s_ij = scale <q_i, k_j> (scale: any finite number),  p = softmax over the keys j of the graph with kv_mask[j] != 0,  out_i = sum_j p_ij v_j.
  * kv_mask (n_kv bytes) may be NULL: all keys; K and V of masked keys are not read.  A query without a key gives
  * zeros.  Rows in front of the first and behind the last graph are neither read nor written.  lse (n_q x heads floats, may be NULL)
- * receives log sum_j exp(s_ij) (-inf without a key), what the backward pass needs.  All matrices are of `dtype`; D <= 128,
+ * receives log sum_j exp(s_ij) (-inf without a key), what the backward pass needs.  All matrices are of `dtype`; D <= 128, kv_heads <= 65535,
  * n_q * heads and n_kv * kv_heads at most 2^30.  Offsets outside [0, n_q] ([0, n_kv]) are taken as the nearest end.
  * In 16 bits the probabilities are rounded to `dtype` before they multiply V (fp16: 2^15 times them).
  */
@@ -459,8 +459,12 @@ int32_t ftc_graph_attention(int32_t n_q, const int32_t *q_ptr, int32_t n_kv, con
  *   dV_j = sum_i p_ij dOut_i,  ds_ij = p_ij (<dOut_i, v_j> - <dOut_i, out_i>),
  *   dQ_i = scale sum_j ds_ij k_j,  dK_j = scale sum_i ds_ij q_i   (sums over the heads that share a K/V head).
  * All matrices are of `dtype`; rows of dK and dV of masked keys are zeros.  dQ, dK, dV must not overlap an input.  In 16 bits
- * p (fp16: 2^15 p) and ds are rounded to `dtype` for their products; ds below 2^-14 has fewer bits in fp16, as every gradient of
- * that size: scale the loss.
+ * p (fp16: 2^15 p) and ds are rounded to `dtype` for their products (ds for D up to 32, and in graphs of one tile, to two numbers).  In fp16 a ds
+ * below 2^-14 is held in steps of 2^-24, and sums of many such, dQ and dK, keep what they lost: scale the loss so that p times a gradient is well
+ * above that.
+ * With D above 32 in 16 bits <dOut_i, out_i> is that of `out` as it was rounded: where V has a mean of once (ten times) its spread, dQ is
+ * 2 to 3 (11 to 24) and dK 2 (11 to 14) times as far off as results that are only rounded, without a mean 1.5 times.  (A row that all of V
+ * have in common adds itself to out and nothing to dQ and dK: it can be taken off before.)
  */
 size_t ftc_graph_attention_backward_workspace_bytes(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads,
                                                     int32_t kv_heads, int32_t D);

@@ -939,7 +939,7 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
 }
 
 static constexpr int64_t ATTENTION_MOST_ROWS = 1 << 30;  // rows and heads of a matrix together, counted in int32
-static constexpr int32_t ATTENTION_MOST_HEADS = 65535;   // K/V heads are a dimension of the grid
+static constexpr int32_t ATTENTION_MOST_HEADS = 65535;   // of K and V: far more than any model has; what fits a launch is attention_size()'s to say
 
 static bool attention_sizes_ok(int32_t n_q, int32_t n_kv, int32_t n_graphs, int32_t heads, int32_t kv_heads, int32_t D)
 {

@@ -2,8 +2,8 @@
 // tiles in LDS that can be read along their rows or along their columns.
 //
 // A step of a product contracts 16 indices: lane l holds, of row (column) l % 32 of its operand, the eight indices of half
-// l / 32.  In 16 bits that is one v_mfma_f32_32x32x16, in fp32 eight v_mfma_f32_32x32x2 with one index of each half, so kernels
-// are written once for the three types.  Which eight indices a half has is free as long as both operands agree; the result
+// l / 32.  In 16 bits that is one v_mfma_f32_32x32x16; in fp32 eight v_mfma_f32_32x32x2 with one index of each half (attention), or six
+// v_mfma_f32_32x32x16 of bf16 pieces (dense layer), so kernels are written once for the three types.  Which eight indices a half has is free as long as both operands agree; the result
 // of a product (lane l: column l % 32, rows 8 b + 4 (l / 32) + i in element 4 b + i) is itself an operand of a next product
 // over its rows with the order {4 h + i, 8 + 4 h + i} of each 16, which the reads along columns can give.
 #pragma once
@@ -29,29 +29,6 @@ template <>
 struct Frag<F32> {
     float f[8];
 };
-
-template <class T>
-__device__ __forceinline__ void frag_zero(Frag<T> &a)
-{
-    if constexpr (T::BYTES == 4) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) a.f[j] = 0.f;
-    } else {
-        a.w = ftc_u32x4{0u, 0u, 0u, 0u};
-    }
-}
-
-template <class T>
-__device__ __forceinline__ void frag_negate(Frag<T> &a)
-{
-    if constexpr (T::BYTES == 4) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) a.f[j] = -a.f[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) a.w[j] ^= 0x80008000u;
-    }
-}
 
 // Eight fp32 numbers as an operand, rounded to nearest even where it has 16 bits.
 template <class T>
