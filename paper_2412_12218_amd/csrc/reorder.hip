@@ -393,7 +393,7 @@ int32_t launch_order_by_key(int n, const int *keys_in, int *perm, int *inv, int 
 // Few ids take one launch: a place is the number of ids that are smaller, or equal and before, which eight threads count for each of the 32 ids of a
 // workgroup.  Up to ID_RANK_PASS ids for each pass of the sort that this stands for, ID_RANK in all (LDS).  us of a gradient of 64 columns, counted / sorted:
 // 118 rows (one pass) 100 ids 12 / 19, 1000 17 / 19, 2000 21 / 20, 4000 31 / 20, 8000 52 / 21; 30 000 rows (two) 100 ids 14 / 29, 2000 24 / 30, 4000 33 / 32, 8000 53 / 32.
-constexpr int ID_RANK = 4096, ID_RANK_PASS = 1536, ID_RANK_EACH = 32;
+constexpr int ID_RANK = 4096, ID_RANK_PASS = 1500, ID_RANK_EACH = 32;
 
 __device__ __forceinline__ uint32_t id_key(int id, int vocab) { return static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab); }
 

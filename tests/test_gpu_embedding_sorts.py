@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("vocab", [1, 255, 511, 512, 65_535, 262_143, 262_144, 300_000])
-@pytest.mark.parametrize("n", [1, 1535, 1536, 1537, 3072, 3073, 4095, 4096, 4097])
+@pytest.mark.parametrize("n", [1, 1499, 1500, 1501, 3000, 3001, 4095, 4096, 4097])
 def test_gradient_next_to_the_limits(n, vocab):
     """Ids of the table's first and last rows and outside it among them; a workspace of what the query says, with anything in it."""
     ids, g = power_law_ids(n, vocab, n), rows(n, 4, 4, torch.float32, n)
