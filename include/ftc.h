@@ -407,8 +407,8 @@ typedef enum {
  * Dense layer: Z = act(X * W + bias) + residual, X n x d_in and W d_in x d_out (contiguous) of `dtype`,
  * bias (d_out numbers, may be NULL) and residual (n x d_out, may be NULL) of the same, Z n x d_out of z_dtype
  * (fp32 or `dtype`); sums, activation and residual in fp32, one rounding at the end.  Z may be the residual itself
- * (in place: same pointer, leading dimension and type).  Of more than two rows (four for dX) and four terms, products of fp32 numbers count an operand
- * below 2^-110 with an error of up to 2^-134; larger ones, infinities and NaN are as in fp32.
+ * (in place: same pointer, leading dimension and type).  fp32 products of more than four terms may
+ * count an operand below 2^-110 with an error of up to 2^-134; larger ones, infinities and NaN are as in fp32.
  * slope (n x d_out, may be NULL) receives act'(X * W + bias), which is all the backward pass needs of the
  * activation: float for fp32 inputs, int16 for 16-bit ones (fixed point, 2^14 is 1; -2^15 is NaN).
  * ftc_linear differs from ftc_update_gemm in the epilogue, and in its kernels, which are for layers of any

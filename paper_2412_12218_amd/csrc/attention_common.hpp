@@ -207,7 +207,7 @@ __device__ __forceinline__ Frag<T> operand_at(const char *row, int c, int D, boo
 template <class T, int N>
 __device__ __forceinline__ void turn_query(Frag<T> (&q)[N], float scale)
 {
-    if (scale > 0.f) return;  // uniform
+    if (__builtin_expect(scale > 0.f, 1)) return;  // uniform
 #pragma unroll
     for (int s = 0; s < N; ++s) {
         float x[8];

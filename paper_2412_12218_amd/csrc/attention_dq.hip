@@ -51,7 +51,6 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
         q[s] = operand_at<T, WHOLE>(q_row, c, a.D, there);
         g[s] = operand_at<T, WHOLE>(g_row, c, a.D, there);
     }
-    turn_query<T>(q, a.scale);
     // scale has the sign of + (turn_query), which the -infinity of hidden keys keeps
     const float scale2 = size_of_scale(a);
     const int64_t at = static_cast<int64_t>(query) * a.heads + head;
@@ -152,12 +151,17 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
     };
     for (int b = 0; b < BUFFERS; ++b) Tiles::clear(a, Ks[b], Vs[b]);
     if (WHOLE && a.D < DP) __syncthreads();
+    // the first tile is on its way before the query is waited for, except through the registers of a single wave
+    constexpr bool EARLY = WHOLE || BUFFERS == 2;
+    if constexpr (EARLY) get(first, Ks[0], Vs[0], biases[0]);
+    turn_query<T>(q, a.scale);
     if constexpr (BUFFERS == 1) {
         for (int t = first; t < last; ++t) {
-            get(t, Ks[0], Vs[0], biases[0]);
+            if constexpr (!EARLY) get(t, Ks[0], Vs[0], biases[0]);
             put(t, Ks[0], Vs[0], biases[0]);
             attend(Ks[0], Vs[0], biases[0]);
             __syncthreads();
+            if constexpr (EARLY) get(t + 1, Ks[0], Vs[0], biases[0]);
         }
     } else {
         // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
@@ -167,7 +171,6 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
             attend(K, V, bias);
             put(t + 1, Kn, Vn, bias_n);
         };
-        get(first, Ks[0], Vs[0], biases[0]);
         put(first, Ks[0], Vs[0], biases[0]);
         for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
     }

@@ -49,7 +49,6 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : T::BYTES 
         const int c = 16 * s + 8 * half;
         q[s] = operand_at<T, WHOLE>(q_row, c, a.D, there);
     }
-    turn_query<T>(q, a.scale);
     float m = -INFINITY, l = 0.f;  // maximum of the products, sum of the exponentials (a half's keys)
     f32x16 o[DT];
 #pragma unroll
@@ -103,12 +102,17 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : T::BYTES 
     };
     for (int b = 0; b < BUFFERS; ++b) Tiles::clear(a, Ks[b], Vs[b]);
     if (WHOLE && a.D < DP) __syncthreads();
+    // the first tile is on its way before the query is waited for, except through the registers of a single wave
+    constexpr bool EARLY = WHOLE || BUFFERS == 2;
+    if constexpr (EARLY) get(first, Ks[0], Vs[0], biases[0]);
+    turn_query<T>(q, a.scale);
     if constexpr (BUFFERS == 1) {
         for (int t = first; t < last; ++t) {
-            get(t, Ks[0], Vs[0], biases[0]);
+            if constexpr (!EARLY) get(t, Ks[0], Vs[0], biases[0]);
             put(t, Ks[0], Vs[0], biases[0]);
             attend(Ks[0], Vs[0], biases[0]);
             __syncthreads();
+            if constexpr (EARLY) get(t + 1, Ks[0], Vs[0], biases[0]);
         }
     } else {
         // one buffer is read while the next tile is on its way to the other (restrict: its arrival need not be waited for before)
@@ -118,14 +122,13 @@ __global__ __launch_bounds__(64 * NW, T::BYTES == 4 && DP == 128 ? 1 : T::BYTES 
             attend(K, V, bias);
             put(t + 1, Kn, Vn, bias_n);
         };
-        get(first, Ks[0], Vs[0], biases[0]);
         put(first, Ks[0], Vs[0], biases[0]);
         for (int t = first, b = 0; t < last; ++t, b ^= 1) turn(t, Ks[b], Vs[b], biases[b], Ks[b ^ 1], Vs[b ^ 1], biases[b ^ 1]);
     }
     l = both_halves_sum(l);
     // A query that holds NaN or an infinity makes NaN of hidden keys, which are zeros in LDS.  Where a key is seen the row is NaN anyway; where none is, as
     // in a graph of padding, the row has no weights.
-    if (__builtin_amdgcn_ballot_w64(l != l)) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(l != l) != 0, 0)) {
         bool sees = false;
         const int end = min(k1, k0 + last * TK);
         for (int j = k0 + first * TK + lane; j < end; j += 64) sees = sees || !a.mask || a.mask[j];
