@@ -167,6 +167,10 @@ struct Rows {
     }
 };
 
+// This wave's loads to LDS have arrived.  The barrier of several waves comes with that; a single wave has none, and the compiler does not see from one turn
+// of a loop to the next that what a load writes is read.
+__device__ __forceinline__ void wait_for_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // The first element of a row of a head, and an operand of it: elements c .. c + 7, zeros if the row is not `there`.
 template <class T>
 __device__ __forceinline__ const char *head_of(const void *p, int64_t row, int64_t ld, int col)

@@ -92,6 +92,7 @@ __global__ __launch_bounds__(64 * NW * (wave_sets<T, DP, NW>()), DP == 128 && (w
                 row_delta[threadIdx.x] = my_delta;
             }
         }
+        if constexpr (WHOLE) wait_for_lds_loads();
         __syncthreads();
     };
     for (int b = 0; b < BUFFERS; ++b) {

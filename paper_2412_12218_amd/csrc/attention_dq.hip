@@ -147,6 +147,7 @@ __global__ __launch_bounds__(64 * NW, DP == 128 && (T::BYTES == 4 || NW == 1) ? 
     };
     auto put = [&](int t, char *K, char *V, float *bias) {
         if (t < last) next.put(a, K, V, bias);
+        if constexpr (WHOLE) wait_for_lds_loads();
         __syncthreads();
     };
     for (int b = 0; b < BUFFERS; ++b) Tiles::clear(a, Ks[b], Vs[b]);
