@@ -434,6 +434,54 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
                             void *db, int32_t dw_dtype, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * The norms before and after a block of a network (attention, a feed-forward block), its gate and its residual connection, over the n rows
+ * of d numbers of the residual stream X and of the block's output F:
+ *   p = Npost(F),  h = x_scale X + gate p,  u = Npre(h),
+ *   N(t) = (t - mean(t)) / sqrt(mean((t - mean(t))^2) + eps) w + b  by rows; FTC_NORM_RMS: without mean(t); FTC_NORM_NONE: N(t) = t.
+ * F may be NULL: h = x_scale X.  Weights and biases (d numbers each) may be NULL: ones and zeros.  gate may be NULL (ones), d numbers (ldg 0) or
+ * n x d (ldg >= d); gate, post_w and post_b are of F, post_w and post_b of a norm, and refused without.  All matrices and vectors are of `dtype`;
+ * everything in between is fp32, and u is that of the unrounded h.  1 <= d <= 16384, eps > 0.  With distances from the mean above 1e19, whose squares fp32 does not
+ * hold, rows are normalised as in exact arithmetic all the same.
+ */
+typedef enum {
+    FTC_NORM_NONE = 0,
+    FTC_NORM_RMS = 1,
+    FTC_NORM_LAYER = 2
+} ftc_norm;
+
+typedef struct {
+    int32_t n, d, dtype;
+    int32_t post, pre; /* ftc_norm */
+    float eps, x_scale;
+    const void *X, *F, *gate, *post_w, *post_b, *pre_w, *pre_b;
+    int32_t ldx, ldf, ldg;
+} ftc_block;
+
+/*
+ * H (n x d, may be NULL) receives h, U (n x d, may be NULL; needs `pre`) u; one of them is given.  H may be X itself (in place: same pointer
+ * and leading dimension).  stats (n x 4 floats, 16-byte aligned, may be NULL) receives each row's mean and factor 1 / sqrt(..) of both norms, which
+ * the backward pass needs.
+ */
+int32_t ftc_block_norm(const ftc_block *b, void *H, int32_t ldh, void *U, int32_t ldu, float *stats, void *stream);
+
+/* What ftc_block_norm_backward computes: each may be NULL.  dX, dF and, for a gate of n x d, dgate are of the block's type; the others, d numbers each, of
+ * dw_dtype (fp32 or the block's type). */
+typedef struct {
+    void *dX, *dF, *dgate, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
+    int32_t lddx, lddf, lddg, dw_dtype;
+} ftc_block_grads;
+
+/*
+ * Gradients of ftc_block_norm for dL/dh = dH (what reaches h on other ways than u; NULL: nothing) and dL/du = dU (NULL: nothing; needs `pre`), the
+ * block as the forward call was given it (X not overwritten) and stats as it wrote them; these may be NULL where there is no norm.  The gradient of a gate, a weight or a
+ * bias is of one that the block has, but for biases of a norm, whose values the gradients do not need: dpre_b and dpost_b need the norm only.
+ * dX may be dH itself (same pointer and leading dimension).  Sums over the rows are added in a fixed order.
+ */
+size_t ftc_block_norm_backward_workspace_bytes(int32_t n, int32_t d);
+int32_t ftc_block_norm_backward(const ftc_block *b, const float *stats, const void *dH, int32_t lddh, const void *dU,
+                                int32_t lddu, const ftc_block_grads *g, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * Attention inside every graph of a packed batch.  Graph g has the query rows q_ptr[g] .. q_ptr[g+1] of Q and out,
  * and the rows kv_ptr[g] .. kv_ptr[g+1] of K and V (device int32, n_graphs + 1 entries, non-decreasing; the same
  * array where every node attends to every node; one query a graph: a readout).  Head h has columns h D .. of Q and

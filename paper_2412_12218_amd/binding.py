@@ -6,6 +6,7 @@ allocated with torch.empty and handed to the library as raw pointers.  All work 
 enqueued on torch's current stream.  There is no CPU or PyTorch fallback: if the shared
 library is missing, lib() raises.
 """
+import collections
 import ctypes as C
 import os
 
@@ -65,6 +66,9 @@ _SIGNATURES = {
     "ftc_linear": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _Z, _P]),
     "ftc_linear_backward_workspace_bytes": (_Z, [_I, _I, _I]),
     "ftc_linear_backward": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _P, _Z, _P]),
+    "ftc_block_norm": (_I, [_P, _P, _I, _P, _I, _P, _P]),
+    "ftc_block_norm_backward_workspace_bytes": (_Z, [_I, _I]),
+    "ftc_block_norm_backward": (_I, [_P, _P, _P, _I, _P, _I, _P, _P, _Z, _P]),
     "ftc_graph_attention_workspace_bytes": (_Z, [_I, _I, _I, _I, _I, _I]),
     "ftc_graph_attention": (_I, [_I, _P, _I, _P, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _F, _P, _I, _P, _P, _Z, _P]),
     "ftc_graph_attention_backward_workspace_bytes": (_Z, [_I, _I, _I, _I, _I, _I]),
@@ -561,6 +565,95 @@ def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_d
                                      _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
                                      _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), stream))
     return dX, dW, db
+
+
+FTC_NORM_NONE, FTC_NORM_RMS, FTC_NORM_LAYER = 0, 1, 2
+
+
+class ftc_block(C.Structure):
+    _fields_ = [("n", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32), ("eps", C.c_float),
+                ("x_scale", C.c_float), ("X", C.c_void_p), ("F", C.c_void_p), ("gate", C.c_void_p), ("post_w", C.c_void_p),
+                ("post_b", C.c_void_p), ("pre_w", C.c_void_p), ("pre_b", C.c_void_p), ("ldx", C.c_int32), ("ldf", C.c_int32),
+                ("ldg", C.c_int32)]
+
+
+class ftc_block_grads(C.Structure):
+    _fields_ = [("dX", C.c_void_p), ("dF", C.c_void_p), ("dgate", C.c_void_p), ("dpost_w", C.c_void_p), ("dpost_b", C.c_void_p),
+                ("dpre_w", C.c_void_p), ("dpre_b", C.c_void_p), ("lddx", C.c_int32), ("lddf", C.c_int32), ("lddg", C.c_int32),
+                ("dw_dtype", C.c_int32)]
+
+
+BlockGrads = collections.namedtuple("BlockGrads", "dX dF dgate dpost_w dpost_b dpre_w dpre_b")
+
+
+def _block(X, F, x_scale, post, post_w, post_b, gate, pre, pre_w, pre_b, eps):
+    n, d = X.shape
+    dt, ldg = X.dtype, 0
+    for v in (post_w, post_b, pre_w, pre_b):
+        if v is not None:
+            _vector(v, d, (dt,))
+    if gate is not None:
+        if gate.dim() == 1:
+            _vector(gate, d, (dt,))
+        else:
+            ldg = _ld(gate, n, d, dt)
+    return ftc_block(n, d, _dt(X), post, pre, eps, x_scale, _ptr(X), _ptr(F), _ptr(gate), _ptr(post_w), _ptr(post_b), _ptr(pre_w),
+                     _ptr(pre_b), _ld(X, n, d), _ld(F, n, d, dt) if F is not None else 0, ldg)
+
+
+def _stats(stats, n):
+    if stats.dtype != torch.float32 or stats.shape != (n, 4) or not stats.is_contiguous():
+        raise ValueError("stats is a contiguous n x 4 fp32 tensor")
+
+
+def ftc_block_norm(X, F=None, x_scale=1.0, post=FTC_NORM_NONE, post_w=None, post_b=None, gate=None, pre=FTC_NORM_RMS, pre_w=None,
+                   pre_b=None, eps=1e-5, H=None, U=None, stats=None):
+    """(H, U): h = x_scale X + gate Npost(F) and Npre(h), in X's type.  gate: d numbers, or n x d.  H is None without F unless it is given, U without
+    a norm `pre`.  stats: n x 4 fp32, for the backward pass."""
+    n, d = X.shape
+    if H is None and (F is not None or pre == FTC_NORM_NONE):
+        H = torch.empty((n, d), dtype=X.dtype, device=X.device)
+    if U is None and pre != FTC_NORM_NONE:
+        U = torch.empty((n, d), dtype=X.dtype, device=X.device)
+    if stats is not None:
+        _stats(stats, n)
+    stream = _here(X, F, post_w, post_b, gate, pre_w, pre_b, H, U, stats)
+    b = _block(X, F, x_scale, post, post_w, post_b, gate, pre, pre_w, pre_b, eps)
+    _check(lib().ftc_block_norm(C.byref(b), _ptr(H), _ld(H, n, d, X.dtype) if H is not None else 0, _ptr(U),
+                                _ld(U, n, d, X.dtype) if U is not None else 0, _ptr(stats), stream))
+    return H, U
+
+
+def ftc_block_norm_backward(X, stats, dH=None, dU=None, F=None, x_scale=1.0, post=FTC_NORM_NONE, post_w=None, post_b=None, gate=None,
+                            pre=FTC_NORM_RMS, pre_w=None, pre_b=None, eps=1e-5, dX=None, dF=None, dgate=None, dpost_w=None, dpost_b=None,
+                            dpre_w=None, dpre_b=None, want=("dX", "dF", "dgate", "dpost_w", "dpost_b", "dpre_w", "dpre_b"),
+                            dw_dtype=torch.float32, ws=None):
+    """BlockGrads, the block as ftc_block_norm was given it.  Of the names in `want` those come back that the block has, the others as None; dX, dF and
+    the gradient of an n x d gate in X's type, the other ones in dw_dtype unless one of them is given, whose type is that of all."""
+    n, d = X.shape
+    dt, rows = X.dtype, gate is not None and gate.dim() != 1
+    vectors = [t for t in ((None if rows else dgate), dpost_w, dpost_b, dpre_w, dpre_b) if t is not None]
+    wdt = vectors[0].dtype if vectors else dw_dtype
+    for v in vectors:
+        _vector(v, d, (wdt,))
+
+    def out(t, name, there, shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=X.device) if t is None and there and name in want else t
+    dX, dF = out(dX, "dX", True, (n, d), dt), out(dF, "dF", F is not None, (n, d), dt)
+    dgate = out(dgate, "dgate", gate is not None, (n, d) if rows else d, dt if rows else wdt)
+    dpost_w, dpost_b = out(dpost_w, "dpost_w", post_w is not None, d, wdt), out(dpost_b, "dpost_b", post_b is not None, d, wdt)
+    dpre_w, dpre_b = out(dpre_w, "dpre_w", pre_w is not None, d, wdt), out(dpre_b, "dpre_b", pre_b is not None, d, wdt)
+    if ws is None:
+        ws = _workspace(lib().ftc_block_norm_backward_workspace_bytes(n, d), X.device)
+    if stats is not None:
+        _stats(stats, n)
+    stream = _here(X, F, post_w, post_b, gate, pre_w, pre_b, stats, dH, dU, dX, dF, dgate, dpost_w, dpost_b, dpre_w, dpre_b, ws)
+    b = _block(X, F, x_scale, post, post_w, post_b, gate, pre, pre_w, pre_b, eps)
+    ld = lambda t: _ld(t, n, d, dt) if t is not None else 0
+    g = ftc_block_grads(_ptr(dX), _ptr(dF), _ptr(dgate), _ptr(dpost_w), _ptr(dpost_b), _ptr(dpre_w), _ptr(dpre_b), ld(dX), ld(dF),
+                        ld(dgate) if rows else 0, _DTYPES[wdt])
+    _check(lib().ftc_block_norm_backward(C.byref(b), _ptr(stats), _ptr(dH), ld(dH), _ptr(dU), ld(dU), C.byref(g), _ptr(ws), ws.numel(), stream))
+    return BlockGrads(dX, dF, dgate, dpost_w, dpost_b, dpre_w, dpre_b)
 
 
 def _attention_sizes(Q, K, V, q_ptr, kv_ptr, heads, kv_heads, kv_mask):

@@ -938,6 +938,97 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
     return launch_linear_backward(p, g, ws, static_cast<hipStream_t>(stream));
 }
 
+static int32_t check_block(const char *who, const ftc_block *b)
+{
+    if (!b) return fail(FTC_EINVAL, "%s: block is NULL", who);
+    if (b->n < 0 || b->d < 1) return fail(FTC_EINVAL, "%s: negative n, or d below 1", who);
+    if (!valid_dtype(b->dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype", who);
+    if (b->post < FTC_NORM_NONE || b->post > FTC_NORM_LAYER || b->pre < FTC_NORM_NONE || b->pre > FTC_NORM_LAYER)
+        return fail(FTC_EINVAL, "%s: unknown norm", who);
+    if (b->d > BLOCK_NORM_WIDEST || b->n > MOST_ROWS) return fail(FTC_EUNSUPPORTED, "%s: d is at most %d, n 2^30", who, BLOCK_NORM_WIDEST);
+    if (!(b->eps > 0.f) || !std::isfinite(b->eps)) return fail(FTC_EINVAL, "%s: eps is not a positive number", who);
+    if (!std::isfinite(b->x_scale)) return fail(FTC_EINVAL, "%s: x_scale is not finite", who);
+    if (b->n > 0 && !b->F && (b->post != FTC_NORM_NONE || b->gate)) return fail(FTC_EINVAL, "%s: a norm or gate of F without F", who);
+    if (b->post == FTC_NORM_NONE && (b->post_w || b->post_b)) return fail(FTC_EINVAL, "%s: post_w or post_b without a norm", who);
+    if (b->pre == FTC_NORM_NONE && (b->pre_w || b->pre_b)) return fail(FTC_EINVAL, "%s: pre_w or pre_b without a norm", who);
+    if (b->n > 0) {
+        FTC_TRY(check_dense(b->X, b->ldx, b->dtype, b->d, who, "X"));
+        if (b->F) FTC_TRY(check_dense(b->F, b->ldf, b->dtype, b->d, who, "F"));
+    }
+    if (b->gate) FTC_TRY(check_dense(b->gate, b->ldg == 0 ? b->d : b->ldg, b->dtype, b->d, who, "gate"));
+    const void *const vectors[4] = {b->post_w, b->post_b, b->pre_w, b->pre_b};
+    for (const void *v : vectors)
+        if (v) FTC_TRY(check_dense(v, b->d, b->dtype, b->d, who, "a weight or bias"));
+    return FTC_OK;
+}
+
+// Whether `out` is one of the block's inputs, X aside.
+static bool block_has(const ftc_block &b, const void *out)
+{
+    return out == b.F || out == b.gate || out == b.post_w || out == b.post_b || out == b.pre_w || out == b.pre_b;
+}
+
+int32_t ftc_block_norm(const ftc_block *b, void *H, int32_t ldh, void *U, int32_t ldu, float *stats, void *stream)
+{
+    const char *who = "ftc_block_norm";
+    FTC_TRY(check_block(who, b));
+    if (b->n == 0) return FTC_OK;
+    if (!H && !U) return fail(FTC_EINVAL, "%s: neither H nor U is given", who);
+    if (U && b->pre == FTC_NORM_NONE) return fail(FTC_EINVAL, "%s: U without a norm", who);
+    if (H) FTC_TRY(check_dense(H, ldh, b->dtype, b->d, who, "H"));
+    if (U) FTC_TRY(check_dense(U, ldu, b->dtype, b->d, who, "U"));
+    if ((H && block_has(*b, H)) || (U && (U == b->X || U == H || block_has(*b, U))) || (stats && (stats == b->X || stats == H || stats == U || block_has(*b, stats))))
+        return fail(FTC_EINVAL, "%s: an output aliases an input or another output", who);
+    if (H == b->X && ldh != b->ldx) return fail(FTC_EINVAL, "%s: H on top of X needs its leading dimension", who);
+    if (!aligned16(stats)) return fail(FTC_EALIGN, "%s: stats must be 16-byte aligned", who);
+    return launch_block_norm(*b, H, ldh, U, ldu, stats, static_cast<hipStream_t>(stream));
+}
+
+size_t ftc_block_norm_backward_workspace_bytes(int32_t n, int32_t d)
+{
+    if (n < 0 || d < 1 || d > BLOCK_NORM_WIDEST || n > MOST_ROWS) return 0;
+    return block_norm_backward_ws(n, d);
+}
+
+int32_t ftc_block_norm_backward(const ftc_block *b, const float *stats, const void *dH, int32_t lddh, const void *dU, int32_t lddu,
+                                const ftc_block_grads *g, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_block_norm_backward";
+    FTC_TRY(check_block(who, b));
+    if (!g) return fail(FTC_EINVAL, "%s: grads is NULL", who);
+    if (dU && b->pre == FTC_NORM_NONE) return fail(FTC_EINVAL, "%s: dU without a norm", who);
+    if ((b->n > 0 && g->dF && !b->F) || (g->dgate && !b->gate) || (g->dpost_w && !b->post_w) || (g->dpre_w && !b->pre_w) || (g->dpost_b && b->post == FTC_NORM_NONE) ||
+        (g->dpre_b && b->pre == FTC_NORM_NONE))
+        return fail(FTC_EINVAL, "%s: a gradient of what the block does not have", who);
+    const bool gates = b->gate && b->ldg != 0;  // one a row
+    if (b->n > 0) {
+        if ((b->pre != FTC_NORM_NONE || b->post != FTC_NORM_NONE) && !stats) return fail(FTC_EINVAL, "%s: stats is NULL", who);
+        if (!aligned16(stats)) return fail(FTC_EALIGN, "%s: stats must be 16-byte aligned", who);
+        if (dH) FTC_TRY(check_dense(dH, lddh, b->dtype, b->d, who, "dH"));
+        if (dU) FTC_TRY(check_dense(dU, lddu, b->dtype, b->d, who, "dU"));
+        if (g->dX) FTC_TRY(check_dense(g->dX, g->lddx, b->dtype, b->d, who, "dX"));
+        if (g->dF) FTC_TRY(check_dense(g->dF, g->lddf, b->dtype, b->d, who, "dF"));
+        if (g->dgate && gates) FTC_TRY(check_dense(g->dgate, g->lddg, b->dtype, b->d, who, "dgate"));
+    }
+    const void *sums[5] = {gates ? nullptr : g->dgate, g->dpost_w, g->dpost_b, g->dpre_w, g->dpre_b};
+    for (const void *v : sums)
+        if (v) {
+            FTC_TRY(check_dense(v, b->d, g->dw_dtype, b->d, who, "the gradient of a weight or bias"));
+            FTC_TRY(check_out_type(who, "the gradient of a weight or bias", b->dtype, g->dw_dtype));
+        }
+    const void *outs[7] = {g->dX, g->dF, g->dgate, g->dpost_w, g->dpost_b, g->dpre_w, g->dpre_b};
+    for (int i = 0; i < 7; ++i) {
+        if (!outs[i]) continue;
+        if (outs[i] == b->X || block_has(*b, outs[i]) || outs[i] == stats || outs[i] == dU || (i > 0 && outs[i] == dH))
+            return fail(FTC_EINVAL, "%s: an output aliases an input", who);
+        for (int j = 0; j < i; ++j)
+            if (outs[i] == outs[j]) return fail(FTC_EINVAL, "%s: two outputs are the same", who);
+    }
+    if (g->dX && g->dX == dH && g->lddx != lddh) return fail(FTC_EINVAL, "%s: dX on top of dH needs its leading dimension", who);
+    FTC_TRY(check_ws(who, block_norm_backward_ws(b->n, b->d), ws, ws_bytes));
+    return launch_block_norm_backward(*b, stats, dH, lddh, dU, lddu, *g, ws, static_cast<hipStream_t>(stream));
+}
+
 static constexpr int64_t ATTENTION_MOST_ROWS = 1 << 30;  // rows and heads of a matrix together, counted in int32
 static constexpr int32_t ATTENTION_MOST_HEADS = 65535;   // of K and V: far more than any model has; what fits a launch is attention_size()'s to say
 

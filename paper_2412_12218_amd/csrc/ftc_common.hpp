@@ -217,6 +217,12 @@ size_t linear_ws(int n, int d_in, int d_out);
 int32_t launch_linear(const LinearShape &p, void *ws, hipStream_t s);
 size_t linear_backward_ws(int n, int d_in, int d_out);
 int32_t launch_linear_backward(const LinearShape &p, const LinearGrads &g, void *ws, hipStream_t s);
+// block_norm.hip, block_norm_backward.hip
+constexpr int BLOCK_NORM_WIDEST = 16384;
+int32_t launch_block_norm(const ftc_block &b, void *H, int ldh, void *U, int ldu, float *stats, hipStream_t s);
+size_t block_norm_backward_ws(int n, int d);
+int32_t launch_block_norm_backward(const ftc_block &b, const float *stats, const void *dH, int lddh, const void *dU, int lddu,
+                                   const ftc_block_grads &g, void *ws, hipStream_t s);
 // graph_attention.hip
 struct AttnShape {
     int n_q, n_kv, graphs, heads, kv_heads, D, dtype;
