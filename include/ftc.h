@@ -434,6 +434,29 @@ int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype
                             void *db, int32_t dw_dtype, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * Dense layer with weights of their own for every group of rows (the types of nodes, experts): group g has the rows group_ptr[g] .. group_ptr[g+1] of X and Z
+ * (device int32, n_groups + 1 entries, non-decreasing; a group may have no row), W[g] (W: n_groups x d_in x d_out, contiguous) and bias[g] (n_groups x d_out, contiguous, may
+ * be NULL).  Otherwise as ftc_linear, for each group; rows in front of the first and behind the last group are neither read nor written, and
+ * W of groups without a row is not read.  Offsets outside [0, n] are taken as the nearest end; d_in, d_out and n_groups at most 2^20.
+ */
+size_t ftc_grouped_linear_workspace_bytes(int32_t n, int32_t n_groups, int32_t d_in, int32_t d_out);
+int32_t ftc_grouped_linear(int32_t n, const int32_t *group_ptr, int32_t n_groups, const void *X, int32_t ldx,
+                           int32_t dtype, int32_t d_in, const void *W, int32_t d_out, const void *bias, int32_t act,
+                           const void *residual, int32_t ldr, void *slope, int32_t lds, void *Z, int32_t ldz,
+                           int32_t z_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Backward of ftc_grouped_linear, as ftc_linear_backward for each group: dW (n_groups x d_in x d_out, contiguous) and db (n_groups x d_out,
+ * contiguous) of groups without a row are zeros.  Sums over the rows are added in a fixed order.
+ */
+size_t ftc_grouped_linear_backward_workspace_bytes(int32_t n, int32_t n_groups, int32_t d_in, int32_t d_out);
+int32_t ftc_grouped_linear_backward(int32_t n, const int32_t *group_ptr, int32_t n_groups, const void *X, int32_t ldx,
+                                    int32_t dtype, int32_t d_in, const void *W, int32_t d_out, const void *slope,
+                                    int32_t lds, const void *dZ, int32_t lddz, const void *dX_add, int32_t ldda,
+                                    void *dX, int32_t lddx, int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype,
+                                    void *ws, size_t ws_bytes, void *stream);
+
+/*
  * The norms before and after a block of a network (attention, a feed-forward block), its gate and its residual connection, over the n rows
  * of d numbers of the residual stream X and of the block's output F:
  *   p = Npost(F),  h = x_scale X + gate p,  u = Npre(h),

@@ -66,6 +66,10 @@ _SIGNATURES = {
     "ftc_linear": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _Z, _P]),
     "ftc_linear_backward_workspace_bytes": (_Z, [_I, _I, _I]),
     "ftc_linear_backward": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _P, _Z, _P]),
+    "ftc_grouped_linear_workspace_bytes": (_Z, [_I, _I, _I, _I]),
+    "ftc_grouped_linear": (_I, [_I, _P, _I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _Z, _P]),
+    "ftc_grouped_linear_backward_workspace_bytes": (_Z, [_I, _I, _I, _I]),
+    "ftc_grouped_linear_backward": (_I, [_I, _P, _I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _P, _Z, _P]),
     "ftc_block_norm": (_I, [_P, _P, _I, _P, _I, _P, _P]),
     "ftc_block_norm_backward_workspace_bytes": (_Z, [_I, _I]),
     "ftc_block_norm_backward": (_I, [_P, _P, _P, _I, _P, _I, _P, _P, _Z, _P]),
@@ -564,6 +568,61 @@ def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_d
                                      _ptr(dX_add), _ld(dX_add, n, d_in, X.dtype) if dX_add is not None else 0, _ptr(dX),
                                      _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
                                      _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), stream))
+    return dX, dW, db
+
+
+def _contiguous(t, shape, dtype):
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {shape} tensor of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+
+
+def ftc_grouped_linear(X, W, group_ptr, bias=None, act=FTC_ACT_NONE, residual=None, out=None, out_dtype=None, slope=None, ws=None):
+    """act(X W[g] + bias[g]) + residual for the rows group_ptr[g] .. group_ptr[g+1] of every group g; W groups x d_in x d_out, bias groups x d_out, group_ptr
+    int32.  out in X's type unless given; rows of no group keep what out has there.  slope: see slope_like."""
+    (n, d_in), (groups, _, d_out) = X.shape, W.shape
+    if out is None:
+        out = torch.empty((n, d_out), dtype=out_dtype or X.dtype, device=X.device)
+    if ws is None:
+        ws = _workspace(lib().ftc_grouped_linear_workspace_bytes(n, groups, d_in, d_out), X.device)
+    stream = _here(X, W, group_ptr, bias, residual, out, slope, ws)
+    _vector(group_ptr, groups + 1, (torch.int32,))
+    _contiguous(W, (groups, d_in, d_out), X.dtype)
+    if bias is not None:
+        _contiguous(bias, (groups, d_out), X.dtype)
+    sdt = torch.float32 if X.dtype == torch.float32 else torch.int16
+    _check(lib().ftc_grouped_linear(n, _ptr(group_ptr), groups, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(bias), act, _ptr(residual),
+                                    _ld(residual, n, d_out, X.dtype) if residual is not None else 0, _ptr(slope),
+                                    _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(out), _ld(out, n, d_out), _dt(out), _ptr(ws),
+                                    ws.numel(), stream))
+    return out
+
+
+def ftc_grouped_linear_backward(X, W, group_ptr, dZ, slope=None, want_dX=True, want_dW=True, want_db=True, dX=None, dx_dtype=None, dW=None, db=None,
+                                dw_dtype=torch.float32, dX_add=None, ws=None):
+    """(dX, dW, db) of ftc_grouped_linear, with the types that ftc_linear_backward has; rows of no group keep what dX has there."""
+    (n, d_in), (groups, _, d_out) = X.shape, W.shape
+    if dX is None and want_dX:
+        dX = torch.empty((n, d_in), dtype=dx_dtype or X.dtype, device=X.device)
+    wdt = dW.dtype if dW is not None else db.dtype if db is not None else dw_dtype
+    if dW is None and want_dW:
+        dW = torch.empty((groups, d_in, d_out), dtype=wdt, device=X.device)
+    if db is None and want_db:
+        db = torch.empty((groups, d_out), dtype=wdt, device=X.device)
+    if ws is None:
+        ws = _workspace(lib().ftc_grouped_linear_backward_workspace_bytes(n, groups, d_in, d_out), X.device)
+    stream = _here(X, W, group_ptr, dZ, slope, dX_add, dX, dW, db, ws)
+    _vector(group_ptr, groups + 1, (torch.int32,))
+    _contiguous(W, (groups, d_in, d_out), X.dtype)
+    if dW is not None:
+        _contiguous(dW, (groups, d_in, d_out), wdt)
+    if db is not None:
+        _contiguous(db, (groups, d_out), wdt)
+    sdt = torch.float32 if X.dtype == torch.float32 else torch.int16
+    _check(lib().ftc_grouped_linear_backward(n, _ptr(group_ptr), groups, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(slope),
+                                             _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(dZ), _ld(dZ, n, d_out, X.dtype),
+                                             _ptr(dX_add), _ld(dX_add, n, d_in, X.dtype) if dX_add is not None else 0, _ptr(dX),
+                                             _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
+                                             _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), stream))
     return dX, dW, db
 
 

@@ -862,6 +862,27 @@ size_t ftc_linear_workspace_bytes(int32_t n, int32_t d_in, int32_t d_out)
     return linear_ws(n, d_in, d_out);
 }
 
+static int32_t check_linear(const char *who, const LinearShape &p)
+{
+    FTC_TRY(check_dense(p.X, p.ldx, p.dtype, p.d_in, who, "X"));
+    FTC_TRY(check_dense(p.W, p.d_out, p.dtype, p.d_out, who, "W"));
+    FTC_TRY(check_dense(p.Z, p.ldz, p.z_dtype, p.d_out, who, "Z"));
+    FTC_TRY(check_out_type(who, "Z", p.dtype, p.z_dtype));
+    if (p.bias) FTC_TRY(check_dense(p.bias, p.d_out, p.dtype, p.d_out, who, "bias"));
+    if (p.residual) FTC_TRY(check_dense(p.residual, p.ldr, p.dtype, p.d_out, who, "residual"));
+    if (p.slope) {
+        if (p.lds < p.d_out) return fail(FTC_EINVAL, "%s: need ld >= D for slope", who);
+        if (reinterpret_cast<uintptr_t>(p.slope) % elem_size(p.dtype) != 0)
+            return fail(FTC_EALIGN, "%s: slope is not aligned to its element size", who);
+    }
+    if (p.Z == p.X || p.Z == p.W || p.Z == p.bias || p.Z == p.slope ||
+        (p.slope && (p.slope == p.X || p.slope == p.W || p.slope == p.bias || p.slope == p.residual)))
+        return fail(FTC_EINVAL, "%s: an output aliases an input or the other output", who);
+    if (p.Z == p.residual && (p.ldz != p.ldr || p.z_dtype != p.dtype))
+        return fail(FTC_EINVAL, "%s: Z on top of the residual needs its leading dimension and type", who);
+    return FTC_OK;
+}
+
 int32_t ftc_linear(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W, int32_t d_out,
                    const void *bias, int32_t act, const void *residual, int32_t ldr, void *slope, int32_t lds, void *Z,
                    int32_t ldz, int32_t z_dtype, void *ws, size_t ws_bytes, void *stream)
@@ -870,24 +891,10 @@ int32_t ftc_linear(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t
     if (n < 0) return fail(FTC_EINVAL, "%s: negative n", who);
     if (act < FTC_ACT_NONE || act > FTC_ACT_SILU) return fail(FTC_EINVAL, "%s: unknown activation %d", who, act);
     if (n == 0) return FTC_OK;
-    FTC_TRY(check_dense(X, ldx, dtype, d_in, who, "X"));
-    FTC_TRY(check_dense(W, d_out, dtype, d_out, who, "W"));
-    FTC_TRY(check_dense(Z, ldz, z_dtype, d_out, who, "Z"));
-    FTC_TRY(check_out_type(who, "Z", dtype, z_dtype));
-    if (bias) FTC_TRY(check_dense(bias, d_out, dtype, d_out, who, "bias"));
-    if (residual) FTC_TRY(check_dense(residual, ldr, dtype, d_out, who, "residual"));
-    if (slope) {
-        if (lds < d_out) return fail(FTC_EINVAL, "%s: need ld >= D for slope", who);
-        if (reinterpret_cast<uintptr_t>(slope) % elem_size(dtype) != 0)
-            return fail(FTC_EALIGN, "%s: slope is not aligned to its element size", who);
-    }
-    if (Z == X || Z == W || Z == bias || Z == slope || (slope && (slope == X || slope == W || slope == bias || slope == residual)))
-        return fail(FTC_EINVAL, "%s: an output aliases an input or the other output", who);
-    if (Z == residual && (ldz != ldr || z_dtype != dtype))
-        return fail(FTC_EINVAL, "%s: Z on top of the residual needs its leading dimension and type", who);
+    const LinearShape p = {n, d_in, d_out, dtype, X, W, bias, residual, slope, Z, ldx, ldr, lds, ldz, act, z_dtype};
+    FTC_TRY(check_linear(who, p));
     FTC_TRY(check_sizes(who, n, d_in, d_out, linear_size));
     FTC_TRY(check_ws(who, linear_ws(n, d_in, d_out), ws, ws_bytes));
-    const LinearShape p = {n, d_in, d_out, dtype, X, W, bias, residual, slope, Z, ldx, ldr, lds, ldz, act, z_dtype};
     return launch_linear(p, ws, static_cast<hipStream_t>(stream));
 }
 
@@ -897,45 +904,107 @@ size_t ftc_linear_backward_workspace_bytes(int32_t n, int32_t d_in, int32_t d_ou
     return linear_backward_ws(n, d_in, d_out);
 }
 
-int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W, int32_t d_out,
-                            const void *slope, int32_t lds, const void *dZ, int32_t lddz, const void *dX_add, int32_t ldda, void *dX,
-                            int32_t lddx, int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws, size_t ws_bytes,
-                            void *stream)
+static int32_t check_linear_backward(const char *who, const LinearShape &p, const LinearGrads &g)
 {
-    const char *who = "ftc_linear_backward";
-    if (n < 0 || d_in < 1 || d_out < 1) return fail(FTC_EINVAL, "%s: negative n, or a width below 1", who);
-    if (!valid_dtype(dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for X", who);
-    if (n > 0) {
-        if (dW) FTC_TRY(check_dense(X, ldx, dtype, d_in, who, "X"));
-        if (dX) FTC_TRY(check_dense(W, d_out, dtype, d_out, who, "W"));
-        FTC_TRY(check_dense(dZ, lddz, dtype, d_out, who, "dZ"));
-        if (slope && lds < d_out) return fail(FTC_EINVAL, "%s: need ld >= D for slope", who);
-        if (reinterpret_cast<uintptr_t>(slope) % elem_size(dtype) != 0)
+    if (p.n < 0 || p.d_in < 1 || p.d_out < 1) return fail(FTC_EINVAL, "%s: negative n, or a width below 1", who);
+    if (!valid_dtype(p.dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for X", who);
+    if (p.n > 0) {
+        if (g.dW) FTC_TRY(check_dense(p.X, p.ldx, p.dtype, p.d_in, who, "X"));
+        if (g.dX) FTC_TRY(check_dense(p.W, p.d_out, p.dtype, p.d_out, who, "W"));
+        FTC_TRY(check_dense(g.dZ, g.lddz, p.dtype, p.d_out, who, "dZ"));
+        if (p.slope && p.lds < p.d_out) return fail(FTC_EINVAL, "%s: need ld >= D for slope", who);
+        if (reinterpret_cast<uintptr_t>(p.slope) % elem_size(p.dtype) != 0)
             return fail(FTC_EALIGN, "%s: slope is not aligned to its element size", who);
-        if (dX) {
-            FTC_TRY(check_dense(dX, lddx, dx_dtype, d_in, who, "dX"));
-            FTC_TRY(check_out_type(who, "dX", dtype, dx_dtype));
-            if (dX_add) FTC_TRY(check_dense(dX_add, ldda, dtype, d_in, who, "dX_add"));
-            if (dX_add == dX && (ldda != lddx || dx_dtype != dtype))
+        if (g.dX) {
+            FTC_TRY(check_dense(g.dX, g.lddx, g.dx_dtype, p.d_in, who, "dX"));
+            FTC_TRY(check_out_type(who, "dX", p.dtype, g.dx_dtype));
+            if (g.dX_add) FTC_TRY(check_dense(g.dX_add, g.ldda, p.dtype, p.d_in, who, "dX_add"));
+            if (g.dX_add == g.dX && (g.ldda != g.lddx || g.dx_dtype != p.dtype))
                 return fail(FTC_EINVAL, "%s: dX on top of dX_add needs its leading dimension and type", who);
         }
     }
-    if (dW) FTC_TRY(check_dense(dW, d_out, dw_dtype, d_out, who, "dW"));
-    if (db) FTC_TRY(check_dense(db, d_out, dw_dtype, d_out, who, "db"));
-    if (dW || db) FTC_TRY(check_out_type(who, "dW", dtype, dw_dtype));
-    const void *outs[3] = {dX, dW, db}, *ins[4] = {X, W, slope, dZ};
+    if (g.dW) FTC_TRY(check_dense(g.dW, p.d_out, g.dw_dtype, p.d_out, who, "dW"));
+    if (g.db) FTC_TRY(check_dense(g.db, p.d_out, g.dw_dtype, p.d_out, who, "db"));
+    if (g.dW || g.db) FTC_TRY(check_out_type(who, "dW", p.dtype, g.dw_dtype));
+    const void *outs[3] = {g.dX, g.dW, g.db}, *ins[4] = {p.X, p.W, p.slope, g.dZ};
     for (int i = 0; i < 3; ++i) {
         for (int j = 0; j < 4; ++j)
             if (outs[i] && outs[i] == ins[j]) return fail(FTC_EINVAL, "%s: an output aliases an input", who);
         for (int j = 0; j < i; ++j)
             if (outs[i] && outs[i] == outs[j]) return fail(FTC_EINVAL, "%s: two outputs are the same", who);
     }
+    if (g.dX_add && (g.dX_add == g.dW || g.dX_add == g.db)) return fail(FTC_EINVAL, "%s: an output aliases an input", who);
+    return FTC_OK;
+}
+
+int32_t ftc_linear_backward(int32_t n, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W, int32_t d_out,
+                            const void *slope, int32_t lds, const void *dZ, int32_t lddz, const void *dX_add, int32_t ldda, void *dX,
+                            int32_t lddx, int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws, size_t ws_bytes,
+                            void *stream)
+{
+    const char *who = "ftc_linear_backward";
+    const LinearShape p = {n, d_in, d_out, dtype, X, W, nullptr, nullptr, const_cast<void *>(slope), nullptr, ldx, 0, lds, 0, FTC_ACT_NONE, dtype};
+    const LinearGrads g = {dZ, dX_add, dX, dW, db, lddz, ldda, lddx, dx_dtype, dw_dtype};
+    FTC_TRY(check_linear_backward(who, p, g));
     FTC_TRY(check_sizes(who, n, d_in, d_out, linear_backward_size));
     FTC_TRY(check_ws(who, linear_backward_ws(n, d_in, d_out), ws, ws_bytes));
-    const LinearShape p = {n, d_in, d_out, dtype, X, W, nullptr, nullptr, const_cast<void *>(slope), nullptr, ldx, 0, lds, 0, FTC_ACT_NONE, dtype};
-    if (dX_add && (dX_add == dW || dX_add == db)) return fail(FTC_EINVAL, "%s: an output aliases an input", who);
-    const LinearGrads g = {dZ, dX_add, dX, dW, db, lddz, ldda, lddx, dx_dtype, dw_dtype};
     return launch_linear_backward(p, g, ws, static_cast<hipStream_t>(stream));
+}
+
+// ---- dense layers with weights for each group of rows
+static constexpr int32_t GROUPED_MOST = 1 << 20;  // of groups and of each width
+static bool grouped_sizes_ok(int32_t n, int32_t n_groups, int32_t d_in, int32_t d_out)
+{
+    return n >= 0 && n <= MOST_ROWS && n_groups >= 0 && n_groups <= GROUPED_MOST && d_in >= 1 && d_in <= GROUPED_MOST && d_out >= 1 && d_out <= GROUPED_MOST;
+}
+static int32_t check_groups(const char *who, int32_t n, const int32_t *group_ptr, int32_t n_groups, int32_t d_in, int32_t d_out)
+{
+    if (n < 0 || n_groups < 0) return fail(FTC_EINVAL, "%s: negative n or n_groups", who);
+    if (d_in < 1 || d_out < 1) return fail(FTC_EINVAL, "%s: a width below 1", who);
+    if (n_groups > 0 && !group_ptr) return fail(FTC_EINVAL, "%s: group_ptr is NULL", who);
+    if (reinterpret_cast<uintptr_t>(group_ptr) % sizeof(int32_t) != 0) return fail(FTC_EALIGN, "%s: group_ptr is not aligned to its element size", who);
+    if (!grouped_sizes_ok(n, n_groups, d_in, d_out)) return fail(FTC_EUNSUPPORTED, "%s: n is at most 2^30, n_groups and widths 2^20", who);
+    return FTC_OK;
+}
+
+size_t ftc_grouped_linear_workspace_bytes(int32_t n, int32_t n_groups, int32_t d_in, int32_t d_out)
+{
+    return grouped_sizes_ok(n, n_groups, d_in, d_out) ? grouped_linear_ws(n, n_groups, d_in, d_out) : 0;
+}
+
+int32_t ftc_grouped_linear(int32_t n, const int32_t *group_ptr, int32_t n_groups, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W,
+                           int32_t d_out, const void *bias, int32_t act, const void *residual, int32_t ldr, void *slope, int32_t lds, void *Z, int32_t ldz,
+                           int32_t z_dtype, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_grouped_linear";
+    FTC_TRY(check_groups(who, n, group_ptr, n_groups, d_in, d_out));
+    if (act < FTC_ACT_NONE || act > FTC_ACT_SILU) return fail(FTC_EINVAL, "%s: unknown activation %d", who, act);
+    if (n == 0 || n_groups == 0) return FTC_OK;
+    const LinearShape p = {n, d_in, d_out, dtype, X, W, bias, residual, slope, Z, ldx, ldr, lds, ldz, act, z_dtype};
+    FTC_TRY(check_linear(who, p));
+    if (!grouped_linear_size(n, n_groups, d_in, d_out).fits()) return fail(FTC_EUNSUPPORTED, "%s: too large for one launch", who);
+    FTC_TRY(check_ws(who, grouped_linear_ws(n, n_groups, d_in, d_out), ws, ws_bytes));
+    return launch_grouped_linear(p, group_ptr, n_groups, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t ftc_grouped_linear_backward_workspace_bytes(int32_t n, int32_t n_groups, int32_t d_in, int32_t d_out)
+{
+    return grouped_sizes_ok(n, n_groups, d_in, d_out) ? grouped_linear_backward_ws(n, n_groups, d_in, d_out) : 0;
+}
+
+int32_t ftc_grouped_linear_backward(int32_t n, const int32_t *group_ptr, int32_t n_groups, const void *X, int32_t ldx, int32_t dtype, int32_t d_in, const void *W,
+                                    int32_t d_out, const void *slope, int32_t lds, const void *dZ, int32_t lddz, const void *dX_add, int32_t ldda, void *dX,
+                                    int32_t lddx, int32_t dx_dtype, void *dW, void *db, int32_t dw_dtype, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_grouped_linear_backward";
+    FTC_TRY(check_groups(who, n, group_ptr, n_groups, d_in, d_out));
+    if (n_groups == 0) return FTC_OK;
+    const LinearShape p = {n, d_in, d_out, dtype, X, W, nullptr, nullptr, const_cast<void *>(slope), nullptr, ldx, 0, lds, 0, FTC_ACT_NONE, dtype};
+    const LinearGrads g = {dZ, dX_add, dX, dW, db, lddz, ldda, lddx, dx_dtype, dw_dtype};
+    FTC_TRY(check_linear_backward(who, p, g));
+    if (!grouped_linear_backward_size(n, n_groups, d_in, d_out).fits()) return fail(FTC_EUNSUPPORTED, "%s: too large for one launch", who);
+    FTC_TRY(check_ws(who, grouped_linear_backward_ws(n, n_groups, d_in, d_out), ws, ws_bytes));
+    return launch_grouped_linear_backward(p, g, group_ptr, n_groups, ws, static_cast<hipStream_t>(stream));
 }
 
 static int32_t check_block(const char *who, const ftc_block *b)

@@ -268,21 +268,26 @@ __device__ __forceinline__ void dense_again(const DenseArgs &a, int row0, int co
         }
 }
 
-// Which tile a workgroup has.  Workgroups go round the eight XCDs, each of which has an L2: every XCD gets a range of consecutive
-// tiles (the rest keep their place), in the order of bands of eight tile rows, column by column inside a band, so that the tiles at
-// work in an XCD share rows of A and columns of B.
-__device__ __forceinline__ void dense_tile(int id, int tiles_m, int tiles_n, int &m, int &n)
+// The tiles in the order of bands of eight tile rows, column by column inside a band.
+__device__ __forceinline__ void dense_band(int id, int tiles_m, int tiles_n, int &m, int &n)
 {
-    const int each = tiles_m * tiles_n / 8;
-    if (id < each * 8) id = (id % 8) * each + id / 8;
     constexpr int BAND = 8;
     const int band = id / (BAND * tiles_n), in = id % (BAND * tiles_n), rows = min(BAND, tiles_m - band * BAND);
     m = band * BAND + in % rows;
     n = in / rows;
 }
+// Which tile a workgroup has.  Workgroups go round the eight XCDs, each of which has an L2: every XCD gets a range of consecutive
+// tiles (the rest keep their place), so that the tiles at work in an XCD share rows of A and columns of B.
+__device__ __forceinline__ void dense_tile(int id, int tiles_m, int tiles_n, int &m, int &n)
+{
+    const int each = tiles_m * tiles_n / 8;
+    if (id < each * 8) id = (id % 8) * each + id / 8;
+    dense_band(id, tiles_m, tiles_n, m, n);
+}
 
+// The tile (tm, tn) of a product over the indices k_begin .. k_end - 1, with the epilogue, or without it to `part` (M x N).
 template <class T, bool AX, bool BX, bool FAST, int RW, int CW, int WM, int WN>
-__global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
+__device__ __forceinline__ void dense_product(const DenseArgs &a, int tm, int tn, int k_begin, int k_end, float *part)
 {
     constexpr int WAVES = RW * CW, TM = 32 * WM * RW, TN = 32 * WN * CW, STEP = 128 / T::BYTES, KS = STEP / 16;
     typedef Operand<T, TM, STEP, AX, WAVES> OA;
@@ -290,10 +295,7 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
     // arrays of their own: the compiler sees that reads of one buffer need not wait for the loads into the other
     __shared__ __align__(16) char A0[OA::BYTES], B0[OB::BYTES], A1[OA::BYTES], B1[OB::BYTES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int tm, tn;
-    dense_tile(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
     const int m0 = tm * TM, n0 = tn * TN, wm = wave / CW * 32 * WM, wn = wave % CW * 32 * WN;
-    const int k_begin = static_cast<int>(blockIdx.y) * a.k_each, k_end = min(a.K, k_begin + a.k_each);
     f32x16 c[WM][WN];
 #pragma unroll
     for (int i = 0; i < WM; ++i)
@@ -409,11 +411,13 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
     }
     // A wave's 32 rows through LDS, where no other wave looks any more: neighbouring lanes then have neighbouring columns.
     constexpr int WIDTH = 32 * WN, PITCH = WIDTH * 4 + 16, EIGHTS = WIDTH / 8;
-    static_assert((WAVES / 4) * 32 * PITCH <= OA::BYTES && (WAVES / 4) * 32 * PITCH <= OB::BYTES, "a place for every wave");
-    char *area = ((wave & 3) == 0 ? A0 : (wave & 3) == 1 ? B0 : (wave & 3) == 2 ? A1 : B1) + (wave >> 2) * 32 * PITCH;
+    constexpr bool EACH = (WAVES / 4) * 32 * PITCH <= OA::BYTES;  // all four have room for a fourth of the waves, else the two of B for half of them
+    static_assert((WAVES / (EACH ? 4 : 2)) * 32 * PITCH <= OB::BYTES, "a place for every wave");
+    char *area = EACH ? ((wave & 3) == 0 ? A0 : (wave & 3) == 1 ? B0 : (wave & 3) == 2 ? A1 : B1) + (wave >> 2) * 32 * PITCH
+                      : ((wave & 1) == 0 ? B0 : B1) + (wave >> 1) * 32 * PITCH;
     const int q = lane % EIGHTS, col = n0 + wn + 8 * q, left = a.N - col;
     float bias[8];
-    load_eight_numbers<T>(a.bias, col, a.bias && a.splits == 1 ? left : 0, bias);
+    load_eight_numbers<T>(a.bias, col, a.bias && !part ? left : 0, bias);
 #pragma unroll
     for (int i = 0; i < WM; ++i) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         constexpr int ROWS = 64 / EIGHTS, TURNS = 32 / ROWS;  // rows at a time
         const int r0 = lane / EIGHTS, row0 = m0 + wm + 32 * i;
-        const bool adds = a.residual && a.splits == 1;
+        const bool adds = a.residual && !part;
         Frag<T> add[TURNS];  // all on their way while the activation is computed
         if (adds) {
 #pragma unroll
@@ -442,8 +446,8 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
             float *at = reinterpret_cast<float *>(area + r * PITCH + 32 * q);
             const ftc_f32x4 u = *reinterpret_cast<const ftc_f32x4 *>(at), v = *reinterpret_cast<const ftc_f32x4 *>(at + 4);
             float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-            if (a.splits > 1) {
-                store_eight_numbers(a.part, (static_cast<int64_t>(blockIdx.y) * a.M + row) * a.N + col, FTC_F32, left, x);
+            if (part) {
+                store_eight_numbers(part, static_cast<int64_t>(row) * a.N + col, FTC_F32, left, x);
                 continue;
             }
             activate<T>(a, row, col, left, bias, x);
@@ -468,6 +472,17 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
             }
         }
     }
+}
+
+template <class T, bool AX, bool BX, bool FAST, int RW, int CW, int WM, int WN>
+__global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
+{
+    constexpr int TM = 32 * WM * RW, TN = 32 * WN * CW;
+    int tm, tn;
+    dense_tile(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
+    const int k_begin = static_cast<int>(blockIdx.y) * a.k_each, k_end = min(a.K, k_begin + a.k_each);
+    float *part = a.splits > 1 ? a.part + static_cast<int64_t>(blockIdx.y) * a.M * a.N : nullptr;
+    dense_product<T, AX, BX, FAST, RW, CW, WM, WN>(a, tm, tn, k_begin, k_end, part);
 }
 
 template <class T, bool AX, bool BX, bool FAST>

@@ -217,6 +217,13 @@ size_t linear_ws(int n, int d_in, int d_out);
 int32_t launch_linear(const LinearShape &p, void *ws, hipStream_t s);
 size_t linear_backward_ws(int n, int d_in, int d_out);
 int32_t launch_linear_backward(const LinearShape &p, const LinearGrads &g, void *ws, hipStream_t s);
+// grouped_linear.hip
+LaunchSize grouped_linear_size(int n, int groups, int d_in, int d_out);
+LaunchSize grouped_linear_backward_size(int n, int groups, int d_in, int d_out);
+size_t grouped_linear_ws(int n, int groups, int d_in, int d_out);
+int32_t launch_grouped_linear(const LinearShape &p, const int *group_ptr, int groups, void *ws, hipStream_t s);
+size_t grouped_linear_backward_ws(int n, int groups, int d_in, int d_out);
+int32_t launch_grouped_linear_backward(const LinearShape &p, const LinearGrads &g, const int *group_ptr, int groups, void *ws, hipStream_t s);
 // block_norm.hip, block_norm_backward.hip
 constexpr int BLOCK_NORM_WIDEST = 16384;
 int32_t launch_block_norm(const ftc_block &b, void *H, int ldh, void *U, int ldu, float *stats, hipStream_t s);

@@ -1,0 +1,18 @@
+// Grouped products with W along the contraction.  See grouped_kernel.hpp.
+#include "grouped_kernel.hpp"
+
+namespace ftc {
+
+template <class T, bool FAST>
+static void rows_t(const GroupedArgs &g, int tile, hipStream_t s) { launch_grouped_rows_t<T, false, FAST>(g, tile, s); }
+
+template <>
+void launch_grouped_rows<false>(const GroupedArgs &g, int dtype, int tile, hipStream_t s)
+{
+    const bool fast = grouped_rows_fast(g.a, false, dtype);
+    if (dtype == FTC_F32) FTC_GROUPED(rows_t, F32);
+    else if (dtype == FTC_F16) FTC_GROUPED(rows_t, F16);
+    else FTC_GROUPED(rows_t, BF16);
+}
+
+}  // namespace ftc

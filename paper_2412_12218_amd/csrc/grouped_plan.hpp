@@ -1,0 +1,60 @@
+// Which tile and how many parts of the contraction the products of a grouped dense layer take (grouped_linear.hip).  The host knows the rows and the groups, not
+// the rows of a group.  Plain C++, so that a host program can ask.
+#pragma once
+#include "dense_plan.hpp"
+
+namespace ftc {
+
+// Tiles of DENSE_64 .. DENSE_256, and one of 32 rows by 128 columns for groups of few rows.
+enum { GROUPED_THIN = 3 };
+constexpr int grouped_rows(int tile) { return tile == GROUPED_THIN ? 32 : dense_side(tile); }
+constexpr int grouped_columns(int tile) { return tile == GROUPED_THIN ? 128 : dense_side(tile); }
+constexpr int grouped_threads(int tile) { return tile == DENSE_256 ? 512 : 256; }
+
+// Groups begin anywhere, and tiles (or chunks, in the weight gradient) of `side` rows begin anew with each.  Group g, rows s .. e - 1, has the numbers from
+// s / side + g on: ceil((e - s) / side) <= e / side - s / side + 1, so the next one's are behind them, whatever the groups are, and n / side + groups numbers do for
+// all of them; some stand for nothing.
+inline int64_t grouped_numbers(int n, int groups, int side) { return static_cast<int64_t>(n / side) + groups; }
+
+// Z and dX: n rows in groups.
+inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fast)
+{
+    static constexpr DenseCost cost[2][4] = {{{0.45f, 0.22f, 5}, {0.79f, 0.53f, 2}, {1.74f, 1.74f, 1}, {0.45f, 0.22f, 4}},
+                                             {{0.75f, 0.49f, 4}, {1.55f, 1.46f, 2}, {0.f, 0.f, 0}, {0.75f, 0.49f, 4}}};
+    constexpr float JOIN_US = 5.f, PART_BYTES_US = 4e6f;
+    DensePlan best = {DENSE_64, 1, 64};
+    if (n < 1 || groups < 1 || N < 1 || K < 1) return best;
+    float least = INFINITY;
+    const int step = f32 ? 32 : 64;
+    for (int tile = DENSE_64; tile <= GROUPED_THIN; ++tile) {
+        if (tile == DENSE_256 && (!fast || f32)) continue;
+        const DenseCost &c = cost[f32][tile];
+        const float alone = fast ? c.alone : 1.5f * c.alone;
+        const int used = groups < n ? groups : n;  // a group's last tile is half full
+        const int64_t tiles = (n / grouped_rows(tile) + (used + 1) / 2) * dense_parts(N, grouped_columns(tile));
+        for (int want = 1; want <= 64; want = want < 8 ? want + 1 : want + want / 4) {
+            DensePlan p = {tile, 1, static_cast<int>(dense_parts(dense_parts(K, want), 64) * 64)};
+            p.splits = static_cast<int>(dense_parts(K, p.k_each));
+            if (p.splits != want) continue;
+            const int64_t blocks = tiles * p.splits, room = 256ll * c.most, full = blocks / room, rest = blocks % room;
+            const auto each = [&](int64_t k) { return k * c.shared > alone ? k * c.shared : alone; };
+            float us = dense_parts(p.k_each, step) * (full * each(c.most) + (rest ? each((rest + 255) / 256) : 0.f));
+            if (p.splits > 1) us += JOIN_US + 8.f * p.splits * n * N / PART_BYTES_US;
+            if (us < least) {
+                least = us;
+                best = p;
+            }
+            if (tiles * want >= 2048) break;
+        }
+    }
+    return best;
+}
+
+// dW: a group's contraction is over its rows, in chunks of at most k_each of them.  As the dense layer has it for all the rows in one group, which no
+// group has more of; where there are groups enough these have their chunks to themselves.
+inline DensePlan grouped_dw_plan(int n, int M, int N, bool f32, bool fast) { return dense_plan(M, N, n, f32, fast); }
+// Parts of a weight gradient: a group of several chunks, so of more than k_each rows, has those from 2 (s / k_each) on.  With q = e / k_each - s / k_each >= 1 it has at
+// most q + 1 <= 2 q chunks, so the next group's are behind them.
+inline int64_t grouped_dw_parts(int n, const DensePlan &p) { return p.k_each < n ? 2ll * (n / p.k_each) : 0; }
+
+}  // namespace ftc

@@ -100,3 +100,28 @@ def block(X, F, x_scale, post, post_w, post_b, gate, pre, pre_w, pre_b, dH=None,
             res["dpost_b"] = db
     res["dF"] = rounded(dh_, ddh)
     return res
+
+
+# ---- dense layers by group: the dense layer's values and bounds for each group's rows, NaN where there is no group --------------------------------
+def grouped(X, W, ptr, bias, act, residual, out_dtype):
+    """(Z, bound), (slope, bound), where the slope is sure."""
+    n, d_out = X.shape[0], W.shape[2]
+    z, dz, s, ds, sure = (np.full((n, d_out), np.nan) if i in (0, 2) else np.zeros((n, d_out)) for i in range(5))
+    for g, (a, b) in enumerate(zip(ptr, ptr[1:])):
+        if b > a:
+            at = slice(a, b)
+            z[at], dz[at], s[at], ds[at], dp, p = linear(X[at], W[g], None if bias is None else bias[g], act, None if residual is None else residual[at], out_dtype)
+            sure[at] = np.abs(p) > dp if act == "relu" else 1
+    return (z, dz), (s, ds), sure > 0
+
+
+def grouped_backward(X, W, ptr, dZ, slope, dx_dtype, dw_dtype):
+    """[(dX, bound), (dW, bound), (db, bound)] for the slopes as they are."""
+    (n, d_in), (groups, _, d_out) = X.shape, W.shape
+    dX, dW, db = (np.full((n, d_in), np.nan), np.zeros((n, d_in))), (np.zeros(W.shape), np.zeros(W.shape)), (np.zeros((groups, d_out)), np.zeros((groups, d_out)))
+    for g, (a, b) in enumerate(zip(ptr, ptr[1:])):
+        if b > a:
+            at = slice(a, b)
+            for to, where, (value, bound) in zip((dX, dW, db), (at, g, g), linear_backward(X[at], W[g], dZ[at], None if slope is None else slope[at], dx_dtype, dw_dtype)):
+                to[0][where], to[1][where] = value, bound
+    return [dX, dW, db]
