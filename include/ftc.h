@@ -505,6 +505,28 @@ int32_t ftc_block_norm_backward(const ftc_block *b, const float *stats, const vo
                                 int32_t lddu, const ftc_block_grads *g, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * The norm over all gradients of a model and their clipping, for scale * g as the gradients (scale: what a scaled loss is divided by again):
+ *   norm = |scale| sqrt(sum over all gradients of g^2),  out = scale min(1, max_norm / norm) g.
+ * `grads` is an array of `count` descriptors on the HOST, read during the call: a matrix `grad` of rows x cols (ld; one row for what is contiguous) of any ftc_dtype, each
+ * its own, and for ftc_clip_grad_norm `out` of the same type (ldo), which may be `grad` itself (same ld) and must not overlap anything else.  Tensors without a number are
+ * skipped.  norm (device float) receives the norm before clipping.  Squares are summed in 64 bits, in a fixed order.  A norm that is infinite makes zeros of what is finite, and one
+ * that is NaN makes everything NaN, as the formula has it; max_norm may be infinite (nothing is clipped but by scale) and is not negative.  At most 2^31 - 1 numbers in the rows of a
+ * matrix that is not contiguous and 2^38 in a tensor.
+ */
+typedef struct {
+    const void *grad;
+    void *out;
+    int64_t rows, cols, ld, ldo;
+    int32_t dtype;
+} ftc_grad;
+
+size_t ftc_grad_norm_workspace_bytes(int32_t count);
+int32_t ftc_grad_norm(const ftc_grad *grads, int32_t count, float scale, float *norm, void *ws, size_t ws_bytes,
+                      void *stream);
+int32_t ftc_clip_grad_norm(const ftc_grad *grads, int32_t count, float max_norm, float scale, float *norm, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/*
  * Attention inside every graph of a packed batch.  Graph g has the query rows q_ptr[g] .. q_ptr[g+1] of Q and out,
  * and the rows kv_ptr[g] .. kv_ptr[g+1] of K and V (device int32, n_graphs + 1 entries, non-decreasing; the same
  * array where every node attends to every node; one query a graph: a readout).  Head h has columns h D .. of Q and

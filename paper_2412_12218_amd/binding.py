@@ -66,6 +66,9 @@ _SIGNATURES = {
     "ftc_linear": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _Z, _P]),
     "ftc_linear_backward_workspace_bytes": (_Z, [_I, _I, _I]),
     "ftc_linear_backward": (_I, [_I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _P, _Z, _P]),
+    "ftc_grad_norm_workspace_bytes": (_Z, [_I]),
+    "ftc_grad_norm": (_I, [_P, _I, _F, _P, _P, _Z, _P]),
+    "ftc_clip_grad_norm": (_I, [_P, _I, _F, _F, _P, _P, _Z, _P]),
     "ftc_grouped_linear_workspace_bytes": (_Z, [_I, _I, _I, _I]),
     "ftc_grouped_linear": (_I, [_I, _P, _I, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _I, _P, _Z, _P]),
     "ftc_grouped_linear_backward_workspace_bytes": (_Z, [_I, _I, _I, _I]),
@@ -624,6 +627,100 @@ def ftc_grouped_linear_backward(X, W, group_ptr, dZ, slope=None, want_dX=True, w
                                              _ld(dX, n, d_in) if dX is not None else 0, _dt(dX) if dX is not None else 0, _ptr(dW),
                                              _ptr(db), _DTYPES[wdt], _ptr(ws), ws.numel(), stream))
     return dX, dW, db
+
+
+class ftc_grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("ldo", C.c_int64),
+                ("dtype", C.c_int32)]
+
+
+def _as_matrix(t):
+    """(rows, cols, ld) of a contiguous tensor of any shape, or of a matrix whose rows are contiguous."""
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() != 2 or t.stride(1) != 1 and t.shape[1] > 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"expected a contiguous tensor or a matrix with contiguous rows, got strides {t.stride()}")
+    return t.shape[0], t.shape[1], t.stride(0)
+
+
+def _overlap(a, b):
+    """Whether two tensors as (address, bytes of a number, rows, cols, ld) share memory; rows of one distance can lie beside each other."""
+    (pa, ea, ra, ca, la), (pb, eb, rb, cb, lb) = a, b
+    end = lambda p, e, r, c, ld: p + ((r - 1) * ld + c) * e
+    if end(*a) <= pb or end(*b) <= pa:
+        return False
+    if la * ea != lb * eb or ra == 1 or rb == 1:
+        return True
+    d = (pb - pa) % (la * ea)   # where a row of b begins in a row of a, and where a row of a begins in a row of b
+    return d < ca * ea or (la * ea - d) % (la * ea) < cb * eb
+
+
+class GradList:
+    """Gradients (and where the clipped ones go: `out`, in place unless given) and their descriptors for ftc_grad_norm and ftc_clip_grad_norm: for a program whose
+    gradients stay where they are.  The tensors share no memory, but that a gradient may be its own `out`."""
+
+    def __init__(self, grads, out=None):
+        self.grads, self.out = list(grads), list(grads if out is None else out)
+        if len(self.out) != len(self.grads):
+            raise ValueError(f"{len(self.out)} outputs for {len(self.grads)} gradients")
+        devices = {t.device for t in self.grads + self.out}
+        if len(devices) > 1:
+            raise ValueError(f"gradients and outputs on {len(devices)} devices")
+        self.first = self.grads[0] if self.grads else None   # stands for all of them
+        self.c = (ftc_grad * len(self.grads))()
+        spans = []
+        for i, (g, o) in enumerate(zip(self.grads, self.out)):
+            if o.shape != g.shape or o.dtype != g.dtype:
+                raise ValueError(f"gradient {i} is {tuple(g.shape)} of {g.dtype}, its output {tuple(o.shape)} of {o.dtype}")
+            if g.is_contiguous() and o.is_contiguous():
+                (rows, cols, ld), (_, _, ldo) = _as_matrix(g), _as_matrix(o)
+            else:
+                two = lambda t: (t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1]) if t.dim() == 2 and t.is_contiguous() else _as_matrix(t)
+                if g.dim() != 2:
+                    raise ValueError(f"gradient {i}: a tensor that is not a matrix, and its output, are contiguous")
+                (rows, cols, ld), (_, _, ldo) = two(g), two(o)
+            self.c[i] = ftc_grad(_ptr(g), _ptr(o), rows, cols, ld, ldo, _dt(g))
+            if g.numel():
+                e = g.element_size()
+                spans.append((g.data_ptr(), e, rows, cols, ld))
+                if o.data_ptr() != g.data_ptr() or ld != ldo:
+                    spans.append((o.data_ptr(), e, rows, cols, ldo))
+        spans.sort()
+        ends = []                    # those that reach beyond the next one's beginning
+        for s in spans:
+            ends = [t for t in ends if t[0] + ((t[2] - 1) * t[4] + t[3]) * t[1] > s[0]]
+            if any(_overlap(t, s) for t in ends):
+                raise ValueError("two of the gradients and outputs share memory")
+            ends.append(s)
+
+    def workspace_bytes(self):
+        return lib().ftc_grad_norm_workspace_bytes(len(self.grads))
+
+
+def _grad_call(grads, norm, ws):
+    if not isinstance(grads, GradList):
+        grads = GradList(grads)
+    dev = norm.device if norm is not None else grads.first.device if grads.grads else "cuda"
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    _vector(norm, 1, (torch.float32,))
+    if ws is None:
+        ws = _workspace(grads.workspace_bytes(), dev)
+    return grads, norm, ws, _here(norm, ws, grads.first)
+
+
+def ftc_grad_norm(grads, scale=1.0, norm=None, ws=None):
+    """|scale| times the norm over all gradients (a GradList, or tensors), one fp32 number on the device."""
+    grads, norm, ws, stream = _grad_call(grads, norm, ws)
+    _check(lib().ftc_grad_norm(grads.c, len(grads.grads), scale, _ptr(norm), _ptr(ws), ws.numel(), stream))
+    return norm
+
+
+def ftc_clip_grad_norm(grads, max_norm, scale=1.0, norm=None, ws=None):
+    """scale min(1, max_norm / norm) times every gradient (a GradList, or tensors: in place), norm as ftc_grad_norm has it, which is what comes back."""
+    grads, norm, ws, stream = _grad_call(grads, norm, ws)
+    _check(lib().ftc_clip_grad_norm(grads.c, len(grads.grads), max_norm, scale, _ptr(norm), _ptr(ws), ws.numel(), stream))
+    return norm
 
 
 FTC_NORM_NONE, FTC_NORM_RMS, FTC_NORM_LAYER = 0, 1, 2

@@ -1007,6 +1007,54 @@ int32_t ftc_grouped_linear_backward(int32_t n, const int32_t *group_ptr, int32_t
     return launch_grouped_linear_backward(p, g, group_ptr, n_groups, ws, static_cast<hipStream_t>(stream));
 }
 
+// ---- the norm over all gradients
+static constexpr int32_t GRAD_MOST = 1 << 20;  // gradients of a call
+static int32_t check_grads(const char *who, const ftc_grad *grads, int32_t count, float scale, const float *norm, bool out)
+{
+    if (count < 0) return fail(FTC_EINVAL, "%s: negative count", who);
+    if (count > 0 && !grads) return fail(FTC_EINVAL, "%s: grads is NULL", who);
+    if (count > GRAD_MOST) return fail(FTC_EUNSUPPORTED, "%s: at most 2^20 gradients", who);
+    if (!std::isfinite(scale)) return fail(FTC_EINVAL, "%s: scale is not finite", who);
+    if (!norm) return fail(FTC_EINVAL, "%s: norm is NULL", who);
+    if (reinterpret_cast<uintptr_t>(norm) % sizeof(float) != 0) return fail(FTC_EALIGN, "%s: norm is not aligned to its element size", who);
+    for (int32_t i = 0; i < count; ++i) {
+        const ftc_grad &g = grads[i];
+        if (g.rows < 0 || g.cols < 0) return fail(FTC_EINVAL, "%s: gradient %d has a negative size", who, i);
+        if (!valid_dtype(g.dtype)) return fail(FTC_EUNSUPPORTED, "%s: unknown dtype for gradient %d", who, i);
+        if (g.rows == 0 || g.cols == 0) continue;
+        if (g.rows > (1ll << 38) / g.cols) return fail(FTC_EUNSUPPORTED, "%s: gradient %d has more than 2^38 numbers", who, i);
+        if (!g.grad || (out && !g.out)) return fail(FTC_EINVAL, "%s: gradient %d is NULL", who, i);
+        const void *const both[2] = {g.grad, out ? g.out : nullptr};
+        for (const void *p : both)
+            if (reinterpret_cast<uintptr_t>(p) % elem_size(g.dtype) != 0) return fail(FTC_EALIGN, "%s: gradient %d is not aligned to its element size", who, i);
+        if (g.rows == 1) continue;
+        if (g.ld < g.cols || (out && g.ldo < g.cols)) return fail(FTC_EINVAL, "%s: need ld >= cols for gradient %d", who, i);
+        if (out && g.out == g.grad && g.ldo != g.ld) return fail(FTC_EINVAL, "%s: out on top of gradient %d needs its leading dimension", who, i);
+        if (!grad_whole(g, out) && (g.rows > INT32_MAX / g.cols || g.ld > INT32_MAX || (out && g.ldo > INT32_MAX)))
+            return fail(FTC_EUNSUPPORTED, "%s: gradient %d is not contiguous and has rows of more than 2^31 - 1 numbers", who, i);
+    }
+    return FTC_OK;
+}
+
+size_t ftc_grad_norm_workspace_bytes(int32_t count) { return count < 0 || count > GRAD_MOST ? 0 : grad_norm_ws(count); }
+
+int32_t ftc_grad_norm(const ftc_grad *grads, int32_t count, float scale, float *norm, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_grad_norm";
+    FTC_TRY(check_grads(who, grads, count, scale, norm, false));
+    FTC_TRY(check_ws(who, grad_norm_ws(count), ws, ws_bytes));
+    return launch_grad_norm(grads, count, scale, norm, ws, static_cast<hipStream_t>(stream));
+}
+
+int32_t ftc_clip_grad_norm(const ftc_grad *grads, int32_t count, float max_norm, float scale, float *norm, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ftc_clip_grad_norm";
+    FTC_TRY(check_grads(who, grads, count, scale, norm, true));
+    if (!(max_norm >= 0.f)) return fail(FTC_EINVAL, "%s: max_norm is negative or NaN", who);
+    FTC_TRY(check_ws(who, grad_norm_ws(count), ws, ws_bytes));
+    return launch_clip_grad_norm(grads, count, max_norm, scale, norm, ws, static_cast<hipStream_t>(stream));
+}
+
 static int32_t check_block(const char *who, const ftc_block *b)
 {
     if (!b) return fail(FTC_EINVAL, "%s: block is NULL", who);

@@ -217,6 +217,11 @@ size_t linear_ws(int n, int d_in, int d_out);
 int32_t launch_linear(const LinearShape &p, void *ws, hipStream_t s);
 size_t linear_backward_ws(int n, int d_in, int d_out);
 int32_t launch_linear_backward(const LinearShape &p, const LinearGrads &g, void *ws, hipStream_t s);
+// grad_norm.hip
+bool grad_whole(const ftc_grad &g, bool clip);
+size_t grad_norm_ws(int count);
+int32_t launch_grad_norm(const ftc_grad *grads, int count, float scale, float *norm, void *ws, hipStream_t s);
+int32_t launch_clip_grad_norm(const ftc_grad *grads, int count, float max_norm, float scale, float *norm, void *ws, hipStream_t s);
 // grouped_linear.hip
 LaunchSize grouped_linear_size(int n, int groups, int d_in, int d_out);
 LaunchSize grouped_linear_backward_size(int n, int groups, int d_in, int d_out);

@@ -1,0 +1,76 @@
+"""What the norm over all gradients and their clipping refuse, on the host, before anything is launched (the pointers are never followed).  CPU only."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2412_12218_amd import binding as B
+
+P = lambda i: 0x10000 * i
+INVALID, UNSUPPORTED, ALIGN, WORKSPACE = B.FTC_EINVAL, B.FTC_EUNSUPPORTED, B.FTC_EALIGN, B.FTC_EWORKSPACE
+GRAD = dict(grad=P(1), out=P(2), rows=3, cols=5, ld=8, ldo=6, dtype=0)
+
+
+def call(fn, k):
+    g = (B.ftc_grad * 2)(B.ftc_grad(P(8), P(8), 1, 7, 7, 7, 2), B.ftc_grad(*(GRAD | {x: v for x, v in k.items() if x in GRAD}).values()))
+    a = dict(grads=g, count=2) | ({} if fn == "ftc_grad_norm" else dict(max_norm=1.0)) | dict(scale=1.0, norm=P(9), ws=P(10), bytes=1 << 40)
+    a |= {x: v for x, v in k.items() if x in a}
+    return getattr(B.lib(), fn)(*a.values(), None)
+
+
+BOTH = [(dict(count=-1), INVALID), (dict(grads=None), INVALID), (dict(count=(1 << 20) + 1), UNSUPPORTED), (dict(scale=float("nan")), INVALID),
+        (dict(scale=float("inf")), INVALID), (dict(norm=None), INVALID), (dict(norm=P(9) + 2), ALIGN), (dict(rows=-1), INVALID), (dict(cols=-1), INVALID),
+        (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED), (dict(rows=1 << 20, cols=1 << 20), UNSUPPORTED), (dict(grad=None), INVALID),
+        (dict(grad=P(1) + 2), ALIGN), (dict(ld=4), INVALID), (dict(rows=1 << 16, cols=1 << 16, ld=(1 << 16) + 1, ldo=1 << 17), UNSUPPORTED),
+        (dict(ld=1 << 31, ldo=1 << 20), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(bytes=64), WORKSPACE), (dict(ws=P(10) + 16), ALIGN)]
+CASES = [(f, k, code) for f in ("ftc_grad_norm", "ftc_clip_grad_norm") for k, code in BOTH] + [
+    ("ftc_clip_grad_norm", dict(max_norm=-1.0), INVALID), ("ftc_clip_grad_norm", dict(max_norm=float("nan")), INVALID), ("ftc_clip_grad_norm", dict(out=None), INVALID),
+    ("ftc_clip_grad_norm", dict(out=P(2) + 1), ALIGN), ("ftc_clip_grad_norm", dict(ldo=4), INVALID), ("ftc_clip_grad_norm", dict(out=P(1)), INVALID)]
+
+
+@pytest.mark.parametrize("fn,args,code", CASES, ids=str)
+def test_refused(fn, args, code):
+    assert call(fn, args) == code, B.lib().ftc_last_error()
+    assert fn in B.lib().ftc_last_error().decode()
+
+
+def test_workspace():
+    f = B.lib().ftc_grad_norm_workspace_bytes
+    assert f(-1) == 0 and f((1 << 20) + 1) == 0 and f(0) == 0 and f(1) == f(64) < f(65)
+
+
+def test_lists():
+    t = torch.arange(200.0)
+    with pytest.raises(ValueError):
+        B.GradList([t[:10], t[5:15]])                               # share memory
+    with pytest.raises(ValueError):
+        B.GradList([t, t])
+    with pytest.raises(ValueError):
+        B.GradList([t[:10]], out=[t[5:15]])
+    with pytest.raises(ValueError):
+        B.GradList([t[:10]], out=[t[10:19]])                        # shapes
+    with pytest.raises(ValueError):
+        B.GradList([t[:10]], out=[torch.zeros(10).half()])          # types
+    with pytest.raises(ValueError):
+        B.GradList([t[:10]], out=[])
+    with pytest.raises(ValueError):
+        B.GradList([t[::2]])                                        # strides
+    with pytest.raises(ValueError):
+        B.GradList([t.view(10, 20).t()])
+    with pytest.raises(ValueError):
+        B.GradList([t.view(2, 10, 10)[:, :, :4]])
+    with pytest.raises(KeyError):
+        B.GradList([t.double()])
+    m = t.view(10, 20)
+    with pytest.raises(ValueError):
+        B.GradList([m[:, :8], m[:, 7:]])
+    with pytest.raises(ValueError):
+        B.GradList([m[:, 4:], m[1:, :5]])
+    with pytest.raises(ValueError):
+        B.GradList([m[:5, 4:], t[90:91]])
+    beside = B.GradList([m[:, :8], m[:, 8:], torch.zeros(3, 0)], out=[torch.zeros(10, 8), m[:, 8:], torch.zeros(3, 0)])
+    assert [(g.rows, g.cols, g.ld, g.ldo) for g in beside.c[:2]] == [(10, 8, 20, 8), (10, 12, 20, 20)]
+    whole = B.GradList([m, t.new_zeros(2, 3, 4)])
+    assert [(g.rows, g.cols) for g in whole.c] == [(1, 200), (1, 24)] and whole.c[0].out == whole.c[0].grad
+    many = torch.zeros(3000)
+    assert len(B.GradList([many[i:i + 1] for i in range(3000)]).c) == 3000
