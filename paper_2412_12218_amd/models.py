@@ -245,11 +245,21 @@ class GraphTransformerPath:
 
     Weights are a dict: "table" (vocab x d), "head" and "head_bias", and "layers", a list of dicts "qkv" (d x (heads + 2 kv_heads) d / heads),
     "out" (d x d), "up" (d x hidden), "down" (hidden x d) with a bias each ("qkv_bias", ...).  Gradients come in the same shape, in fp32.
-    Buffers are allocated here once; forward() keeps in them what backward() needs."""
+    Buffers are allocated here once; forward() keeps in them what backward() needs.
+
+    What a layer can have besides (each with weights of its own):
+      norm       a norm (B.FTC_NORM_RMS, B.FTC_NORM_LAYER) in front of both blocks and of the head: "attention_norm" and "feed_norm" of a layer, "head_norm"
+      post_norm  a norm of what a block gives: "attention_post" and "feed_post" of a layer; layer norms have biases ("feed_norm_bias", ...)
+      gates      learned factors of what a block adds, d of them: "attention_gate" and "feed_gate" of a layer
+      residual_scale  what the residual connections multiply their input by
+      types      the type of every node (device int32, from 0 on below n_types): "up" and "down" are of each type, n_types x d x hidden and
+                 n_types x hidden x d, their biases n_types x hidden and n_types x d
+    clip() is the clipping of all gradients by their norm."""
 
     LINEAR = ("qkv", "out", "up", "down")
 
-    def __init__(self, graph_ptr, n, vocab, d=64, heads=4, kv_heads=None, hidden=None, n_out=8, layers=2, act_dtype=torch.float16):
+    def __init__(self, graph_ptr, n, vocab, d=64, heads=4, kv_heads=None, hidden=None, n_out=8, layers=2, act_dtype=torch.float16,
+                 norm=B.FTC_NORM_NONE, post_norm=B.FTC_NORM_NONE, gates=False, residual_scale=1.0, types=None, n_types=0):
         dev, L = graph_ptr.device, B.lib()
         if d % heads:
             raise ValueError("d is a multiple of heads")
@@ -274,6 +284,139 @@ class GraphTransformerPath:
         self.ws = B._workspace(max([L.ftc_graph_attention_workspace_bytes(*sizes), L.ftc_graph_attention_backward_workspace_bytes(*sizes),
                                     L.ftc_embedding_backward_workspace_bytes(n, vocab, d)] +
                                    [f(n, *s) for f in (L.ftc_linear_workspace_bytes, L.ftc_linear_backward_workspace_bytes) for s in shapes]), dev)
+        self.norm, self.post_norm, self.gates, self.residual_scale, self.n_types = norm, post_norm, gates, residual_scale, n_types
+        self.blocks = bool(norm or post_norm or gates or types is not None or residual_scale != 1.0)
+        if not self.blocks:
+            return
+        self.group_ptr = None
+        if types is not None:
+            low, high = (int(x.item()) for x in types.aminmax()) if n else (0, -1)
+            if types.shape != (n,) or low < 0 or high >= n_types:
+                raise ValueError(f"types of {n} nodes, from 0 on below n_types")
+            self.perm, self.inv, _ = B.ftc_order_by_key(types)
+            self.group_ptr = torch.zeros(n_types + 1, dtype=torch.int32, device=dev)
+            self.group_ptr[1:] = torch.cumsum(torch.bincount(types, minlength=n_types), 0)
+            self.by_type, self.d_by_type = [act(d) for _ in range(layers)], act(d)     # inputs of the feed-forward block in the order of the types
+            self.unsorted = act(d)
+        # what is normed for a block or the head, what a block gives, the statistics of the norms behind it
+        self.normed = [act(d) for _ in range(2 * layers + 1)] if norm else None
+        self.given = [act(d) for _ in range(2 * layers)]
+        self.stats = [torch.empty((n, 4), dtype=torch.float32, device=dev) for _ in range(2 * layers + 1)]
+        self.d_given, self.d_normed = act(d), act(d)
+        self.ws = B._workspace(max([self.ws.numel(), L.ftc_block_norm_backward_workspace_bytes(n, d)] +
+                                   [f(n, n_types, *s) for f in (L.ftc_grouped_linear_workspace_bytes, L.ftc_grouped_linear_backward_workspace_bytes)
+                                    for s in shapes[2:4]]), dev)
+
+    def _join(self, weights, at):
+        """The arguments of the norms and the residual connection behind block `at` (0: in front of the first; 2 i + 1, 2 i + 2: behind attention and
+        feed-forward block of layer i) and the names and owners of their weights."""
+        layers, args, names = weights["layers"], dict(x_scale=self.residual_scale if at else 1.0, post=B.FTC_NORM_NONE, pre=self.norm), {}
+
+        def take(owner, name, arg):
+            args[arg], names["d" + arg] = owner[name], (owner, name)
+
+        def take_norm(owner, name, arg, kind):
+            take(owner, name, arg + "_w")
+            if kind == B.FTC_NORM_LAYER:
+                take(owner, name + "_bias", arg + "_b")
+        if at:
+            owner, block = layers[(at - 1) // 2], ("attention", "feed")[(at - 1) % 2]
+            args["F"], args["post"] = self.given[at - 1], self.post_norm
+            if self.post_norm:
+                take_norm(owner, block + "_post", "post", self.post_norm)
+            if self.gates:
+                take(owner, block + "_gate", "gate")
+        if self.norm:
+            take_norm(*((weights, "head_norm") if at == 2 * self.layers else (layers[at // 2], ("attention_norm", "feed_norm")[at % 2])), "pre", self.norm)
+        return args, names
+
+    def _streams(self):
+        """The residual stream in front of and behind every block."""
+        between = [self.h[0]]
+        for i in range(self.layers):
+            between += [self.middle[i], self.h[i + 1]]
+        return between
+
+    def _forward_blocks(self, weights, mask):
+        between, ws = self._streams(), self.ws
+
+        def join(at):
+            """What the next block (or the head) gets."""
+            if at == 0 and not self.norm:
+                return between[0]
+            args, _ = self._join(weights, at)
+            B.ftc_block_norm(between[max(at - 1, 0)], H=between[at] if at else None, U=self.normed[at] if self.norm else None, stats=self.stats[at], **args)
+            return self.normed[at] if self.norm else between[at]
+        x = join(0)
+        for i, w in enumerate(weights["layers"]):
+            B.ftc_linear(x, w["qkv"], bias=w["qkv_bias"], out=self.qkv[i], ws=ws)
+            args, kw = self._attention_args(i, mask)
+            B.ftc_graph_attention(*args, out=self.attended[i], lse=self.lse[i], **kw)
+            B.ftc_linear(self.attended[i], w["out"], bias=w["out_bias"], out=self.given[2 * i], ws=ws)
+            x = join(2 * i + 1)
+            if self.group_ptr is None:
+                B.ftc_linear(x, w["up"], bias=w["up_bias"], act=B.FTC_ACT_GELU, out=self.up[i], slope=self.slope[i], ws=ws)
+                B.ftc_linear(self.up[i], w["down"], bias=w["down_bias"], out=self.given[2 * i + 1], ws=ws)
+            else:
+                B.ftc_permute_rows(x, self.perm, out=self.by_type[i])
+                B.ftc_grouped_linear(self.by_type[i], w["up"], self.group_ptr, bias=w["up_bias"], act=B.FTC_ACT_GELU, out=self.up[i], slope=self.slope[i], ws=ws)
+                B.ftc_grouped_linear(self.up[i], w["down"], self.group_ptr, bias=w["down_bias"], out=self.unsorted, ws=ws)
+                B.ftc_permute_rows(self.unsorted, self.inv, out=self.given[2 * i + 1])
+            x = join(2 * i + 2)
+        return B.ftc_linear(x, weights["head"], bias=weights["head_bias"], out=self.logits, ws=ws)
+
+    def _backward_blocks(self, weights, grads, d_out, mask):
+        between, ws, back = self._streams(), self.ws, B.ftc_linear_backward
+        into = {id(o): g for o, g in [(weights, grads), *zip(weights["layers"], grads["layers"])]}
+
+        def join(at):
+            """Through the join: d_h is the gradient of the stream in front of it then, d_given that of the block's result.  What reaches the stream behind it on the
+            way of the next block's input is in d_normed, or has been added to d_h where there is no norm."""
+            if at == 0 and not self.norm:
+                return
+            args, names = self._join(weights, at)
+            last = at == 2 * self.layers       # nothing goes on behind the head's norm
+            got = B.ftc_block_norm_backward(between[max(at - 1, 0)], self.stats[at], dH=None if last and self.norm else self.d_h, dU=self.d_normed if self.norm else None,
+                                            dX=self.d_h, dF=self.d_given if at else None, ws=ws, **args)
+            for name, (owner, key) in names.items():
+                into[id(owner)][key] = getattr(got, name)
+
+        def block_input(at, **k):
+            """Where the gradient of what a block (or the head) got goes."""
+            if self.norm:
+                return dict(dX=self.d_normed, **k)
+            return dict(dX=self.d_h, **k) if at == 2 * self.layers else dict(dX=self.d_h, dX_add=self.d_h, **k)
+        put = lambda at: self.normed[at] if self.norm else between[at]
+        last = 2 * self.layers
+        _, grads["head"], grads["head_bias"] = back(put(last), weights["head"], d_out, ws=ws, **block_input(last))
+        for i in reversed(range(self.layers)):
+            w, g, at = weights["layers"][i], grads["layers"][i], 2 * i
+            join(at + 2)
+            if self.group_ptr is None:
+                _, g["down"], g["down_bias"] = back(self.up[i], w["down"], self.d_given, dX=self.d_up, ws=ws)
+                _, g["up"], g["up_bias"] = back(put(at + 1), w["up"], self.d_up, slope=self.slope[i], ws=ws, **block_input(at + 1))
+            else:
+                grouped = B.ftc_grouped_linear_backward
+                B.ftc_permute_rows(self.d_given, self.perm, out=self.unsorted)
+                _, g["down"], g["down_bias"] = grouped(self.up[i], w["down"], self.group_ptr, self.unsorted, dX=self.d_up, ws=ws)
+                _, g["up"], g["up_bias"] = grouped(self.by_type[i], w["up"], self.group_ptr, self.d_up, slope=self.slope[i], dX=self.d_by_type, ws=ws)
+                if self.norm:
+                    B.ftc_permute_rows(self.d_by_type, self.inv, out=self.d_normed)
+                else:
+                    B.ftc_permute_rows(self.d_by_type, self.inv, out=self.unsorted)
+                    B.ftc_block_norm(self.d_h, F=self.unsorted, pre=B.FTC_NORM_NONE, H=self.d_h)
+            join(at + 1)
+            _, g["out"], g["out_bias"] = back(self.attended[i], w["out"], self.d_given, dX=self.d_attended, ws=ws)
+            args, kw = self._attention_args(i, mask)
+            dq, dk, dv = (self.d_qkv[:, c] for c in self.columns)
+            B.ftc_graph_attention_backward(*args, self.attended[i], self.lse[i], self.d_attended, dQ=dq, dK=dk, dV=dv, **kw)
+            _, g["qkv"], g["qkv_bias"] = back(put(at), w["qkv"], self.d_qkv, ws=ws, **block_input(at))
+        join(0)
+
+    def clip(self, grads, max_norm, scale=1.0, norm=None):
+        """Clips the gradients of backward(), in place, all by their one norm, which is what comes back (before clipping); scale: what a scaled loss is divided by."""
+        flat = [t for k, t in sorted(grads.items()) if k != "layers"] + [t for g in grads["layers"] for _, t in sorted(g.items())]
+        return B.ftc_clip_grad_norm(flat, max_norm, scale=scale, norm=norm)
 
     def _attention_args(self, layer, mask):
         q, k, v = (self.qkv[layer][:, c] for c in self.columns)
@@ -287,6 +430,8 @@ class GraphTransformerPath:
         """Logits (n x n_out), in the path's buffer.  mask: nodes with 0 are attended to by no node."""
         self._check_layers(weights)
         B.ftc_embedding(ids, weights["table"], scale=self.scale, out=self.h[0])
+        if self.blocks:
+            return self._forward_blocks(weights, mask)
         for i, w in enumerate(weights["layers"]):
             B.ftc_linear(self.h[i], w["qkv"], bias=w["qkv_bias"], out=self.qkv[i], ws=self.ws)
             args, kw = self._attention_args(i, mask)
@@ -300,6 +445,10 @@ class GraphTransformerPath:
         """d_out = dL/d(logits), in the activation type; gradients of the weights that forward() was given, with the mask that it was given."""
         self._check_layers(weights)
         grads, back = dict(layers=[{} for _ in weights["layers"]]), B.ftc_linear_backward
+        if self.blocks:
+            self._backward_blocks(weights, grads, d_out, mask)
+            grads["table"] = B.ftc_embedding_backward(ids, self.d_h, self.vocab, scale=self.scale, ws=self.ws)
+            return grads
         _, grads["head"], grads["head_bias"] = back(self.h[-1], weights["head"], d_out, dX=self.d_h, ws=self.ws)
         for i in reversed(range(self.layers)):
             w, g = weights["layers"][i], grads["layers"][i]
