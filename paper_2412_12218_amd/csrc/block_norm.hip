@@ -5,89 +5,119 @@
 
 namespace ftc {
 
-template <class T, int L, int C, bool WHOLE>
+// BLOCK: with F
+template <class T, int L, int C, bool BLOCK, bool WHOLE, bool NT>
 __global__ __launch_bounds__(row_threads(L)) void block_norm_kernel(BlockArgs a, void *H, int64_t ldh, void *U, int64_t ldu, float *stats)
 {
     constexpr int GROUPS = row_threads(L) / L;
     __shared__ float area[32];
     int turn = 0;
-    const RowPieces<T, L, C, WHOLE> r = {a.d, static_cast<int>(threadIdx.x) % L};
-    const int sub = threadIdx.x / L;
-    // weights: from memory once, for all rows
-    Frag<T> post_w[C], post_b[C], pre_w[C], pre_b[C], gate[C];
-    r.load(a.post_w, 0, a.post_w != nullptr, post_w);
-    r.load(a.post_b, 0, a.post_b != nullptr, post_b);
-    r.load(a.pre_w, 0, a.pre_w != nullptr, pre_w);
-    r.load(a.pre_b, 0, a.pre_b != nullptr, pre_b);
-    r.load(a.gate, 0, a.gate && a.ldg == 0, gate);
-    auto scaled = [&](float (&x)[C][8], float mean, float rstd, const void *w, const Frag<T> (&wf)[C], const Frag<T> (&bf)[C]) {
+    const RowPieces<T, L, C, WHOLE, NT> r = {a.d, static_cast<int>(threadIdx.x) % L, L < 64 ? static_cast<int>(threadIdx.x) / L : __builtin_amdgcn_readfirstlane(threadIdx.x / L)};
+    auto scaled = [&](float (&x)[C][8], float mean, float rstd, const float (&w)[C][8], const float (&b)[C][8]) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[c][j] = fmaf((x[c][j] - mean) * rstd, w[c][j], b[c][j]);
+    };
+    // the next rows are on their way while these are worked on
+    const int64_t step = static_cast<int64_t>(gridDim.x) * GROUPS;
+    Frag<T> next_x[C], next_f[C], next_gate[C];
+    r.clear(next_x);
+    r.clear(next_f);
+    r.clear(next_gate);
+    auto fetch = [&](int64_t row0) {
+        const bool there = row0 + r.sub < a.n;
+        if (row0 + GROUPS > a.n) {  // uniform
+            r.clear(next_x);
+            r.clear(next_f);
+        }
+        r.load(a.X, a.ldx, row0, there, next_x);
+        if (BLOCK) r.load(a.F, a.ldf, row0, there, next_f);
+        if (BLOCK && a.ldg) r.load(a.gate, a.ldg, row0, there, next_gate);
+    };
+    fetch(static_cast<int64_t>(blockIdx.x) * GROUPS);
+    Frag<T> raw_post_w[C], raw_post_b[C], raw_pre_w[C], raw_pre_b[C], raw_gate[C];
+    r.fetch(a.post_w, raw_post_w);
+    r.fetch(a.post_b, raw_post_b);
+    r.fetch(a.pre_w, raw_pre_w);
+    r.fetch(a.pre_b, raw_pre_b);
+    r.fetch(a.ldg ? nullptr : a.gate, raw_gate);
+    float post_w[C][8], post_b[C][8], pre_w[C][8], pre_b[C][8], one_gate[C][8];
+    r.vector(a.post_w, raw_post_w, 1.f, post_w);
+    r.vector(a.post_b, raw_post_b, 0.f, post_b);
+    r.vector(a.pre_w, raw_pre_w, 1.f, pre_w);
+    r.vector(a.pre_b, raw_pre_b, 0.f, pre_b);
+    r.vector(a.ldg ? nullptr : a.gate, raw_gate, 1.f, one_gate);
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * GROUPS; row0 < a.n; row0 += step) {
+        const bool there = row0 + r.sub < a.n;
+        float h[C][8], p[C][8], gate[C][8], m[4] = {0.f, 1.f, 0.f, 1.f};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            float wn[8], bn[8];
-            frag_numbers<T>(wf[c], wn);
-            frag_numbers<T>(bf[c], bn);  // zeros where there are none
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[c][j] = fmaf((x[c][j] - mean) * rstd, w ? wn[j] : 1.f, bn[j]);
+            frag_numbers<T>(next_x[c], h[c]);
+            frag_numbers<T>(next_f[c], p[c]);
         }
-    };
-    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * GROUPS; row0 < a.n; row0 += static_cast<int64_t>(gridDim.x) * GROUPS) {
-        const int64_t row = row0 + sub;
-        const bool there = row < a.n;
-        Frag<T> x[C], f[C];
-        r.load(a.X, row * a.ldx, there, x);
-        r.load(a.F, row * a.ldf, there && a.F, f);
-        if (a.ldg) r.load(a.gate, row * a.ldg, there, gate);
-        float h[C][8], m[4] = {0.f, 1.f, 0.f, 1.f};
-        if (a.F) {
-            float p[C][8];
+        if (BLOCK && a.ldg) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) frag_numbers<T>(f[c], p[c]);
-            if (a.post != FTC_NORM_NONE) {
-                row_statistics(r, a.post, a.eps, p, area, turn, m[0], m[1]);
-                scaled(p, m[0], m[1], a.post_w, post_w, post_b);
-            }
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float xn[8], g[8];
-                frag_numbers<T>(x[c], xn);
-                frag_numbers<T>(gate[c], g);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[c][j] = r.has(c, j) ? fmaf(a.x_scale, xn[j], a.gate ? g[j] * p[c][j] : p[c][j]) : 0.f;
-            }
+            for (int c = 0; c < C; ++c) frag_numbers<T>(next_gate[c], gate[c]);
         } else {
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                frag_numbers<T>(x[c], h[c]);
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) gate[c][j] = one_gate[c][j];
+        }
+        if (row0 + step < a.n) fetch(row0 + step);
+        if constexpr (BLOCK) {
+            if (a.post != FTC_NORM_NONE) {
+                row_statistics(r, a.post, a.eps, p, area, turn, m[0], m[1]);
+                scaled(p, m[0], m[1], post_w, post_b);
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    h[c][j] = fmaf(a.x_scale, h[c][j], gate[c][j] * p[c][j]);
+                    if (!r.has(c, j)) h[c][j] = 0.f;
+                }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[c][j] *= a.x_scale;
-            }
         }
-        if (H) r.store(H, row * ldh, there, h);
+        if (H) r.store(H, ldh, row0, there, h);
         if (a.pre != FTC_NORM_NONE) {
             row_statistics(r, a.pre, a.eps, h, area, turn, m[2], m[3]);
             if (U) {
-                scaled(h, m[2], m[3], a.pre_w, pre_w, pre_b);
-                r.store(U, row * ldu, there, h);
+                scaled(h, m[2], m[3], pre_w, pre_b);
+                r.store(U, ldu, row0, there, h);
             }
         }
-        if (stats && there && r.lane == 0) *reinterpret_cast<ftc_f32x4 *>(stats + 4 * row) = ftc_f32x4{m[0], m[1], m[2], m[3]};
+        if (stats && there && r.lane == 0) *reinterpret_cast<ftc_f32x4 *>(stats + 4 * (row0 + r.sub)) = ftc_f32x4{m[0], m[1], m[2], m[3]};
     }
 }
 
-template <class T, int L, int C>
+template <class T, int L, int C, bool BLOCK>
 static void forward_t(const BlockArgs &a, void *H, int ldh, void *U, int ldu, float *stats, hipStream_t s)
 {
-    constexpr int THREADS = row_threads(L), GROUPS = THREADS / L, MOST = 256 * 2048 / THREADS;
-    const int64_t groups = (static_cast<int64_t>(a.n) + GROUPS - 1) / GROUPS;
-    const dim3 grid(static_cast<unsigned>(groups < MOST ? groups : MOST));
-    if (a.d % 8 == 0) hipLaunchKernelGGL((block_norm_kernel<T, L, C, true>), grid, dim3(THREADS), 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
-    else hipLaunchKernelGGL((block_norm_kernel<T, L, C, false>), grid, dim3(THREADS), 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
+    const dim3 grid(row_groups(a.n, L, BLOCK ? 1024 : 2048)), threads(row_threads(L));
+    const bool whole = whole_rows<T>(a.d, a.ldx) && whole_rows<T>(a.d, a.ldf) && whole_rows<T>(a.d, a.ldg) && whole_rows<T>(a.d, ldh) && whole_rows<T>(a.d, ldu);
+    const int arrays = 1 + (a.F != nullptr) + (a.ldg != 0) + (H != nullptr) + (U != nullptr);
+    if (whole && row_stream(static_cast<int64_t>(a.n) * a.d * T::BYTES * arrays))
+        hipLaunchKernelGGL((block_norm_kernel<T, L, C, BLOCK, true, true>), grid, threads, 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
+    else if (whole)
+        hipLaunchKernelGGL((block_norm_kernel<T, L, C, BLOCK, true, false>), grid, threads, 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
+    else
+        hipLaunchKernelGGL((block_norm_kernel<T, L, C, BLOCK, false, false>), grid, threads, 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
 }
 
 int32_t launch_block_norm(const ftc_block &b, void *H, int ldh, void *U, int ldu, float *stats, hipStream_t s)
 {
     const BlockArgs a = {b.n, b.d, b.F ? b.post : FTC_NORM_NONE, b.pre, b.eps, b.x_scale, b.X, b.F, b.gate, b.post_w, b.post_b, b.pre_w, b.pre_b, b.ldx, b.ldf, b.ldg};
-#define FTC_ROWS(T, L, C) forward_t<T, L, C>(a, H, ldh, U, ldu, stats, s)
+#define FTC_ROWS(T, L, C)                                                     \
+    do {                                                                      \
+        if (a.F) forward_t<T, L, C, true>(a, H, ldh, U, ldu, stats, s);       \
+        else forward_t<T, L, C, false>(a, H, ldh, U, ldu, stats, s);          \
+    } while (0)
 #define FTC_WIDTHS(T)                                \
     do {                                             \
         if (b.d <= 32) FTC_ROWS(T, 4, 1);            \

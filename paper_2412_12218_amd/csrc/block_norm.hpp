@@ -3,11 +3,22 @@
 // A row is in the registers of L lanes, C pieces of eight numbers each, lane l having the pieces l, l + L, ...; it is read once whatever is computed
 // of it.  Up to 64 lanes are lanes of one wave and their sums stay in registers; more are waves of one workgroup, whose sums meet in LDS.
 #pragma once
-#include "matrix_frag.hpp"
+#include "stream_piece.hpp"
 
 namespace ftc {
 
 constexpr int row_threads(int lanes) { return lanes > 64 ? lanes : 256; }  // of a workgroup
+
+// Workgroups of a launch: at most as many as the compute units hold at once, and as many turns for each of them.
+inline int row_groups(int n, int lanes, int threads_a_unit)
+{
+    const int threads = row_threads(lanes), groups = ceil_div(n, threads / lanes), most = 256 * (threads_a_unit / threads > 0 ? threads_a_unit / threads : 1);
+    return groups <= most ? groups : ceil_div(groups, ceil_div(groups, most));
+}
+// Whether a pass over so many bytes takes the non-temporal hint (stream_piece.hpp): more than a third of the last-level cache of 256 MB, of which the kernels before and behind have
+// theirs.  us with / without: 74 MB (46 000 x 200 in fp32, normed) 14.9 / 13.1; 123 MB (20 000 x 768 in bf16, a block's join) 32 / 42, its gradients (184 MB) 46 / 54; 256 MB (200 000 x 128) 47 / 50;
+// 410 MB (50 000 x 1024) 75 / 80.
+inline bool row_stream(int64_t bytes) { return bytes > 85ll << 20; }
 
 struct BlockArgs {
     int n, d, post, pre;
@@ -47,71 +58,142 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float *area, int &turn)
     }
 }
 
-// A lane's C pieces of rows of d numbers.  WHOLE: d is a multiple of eight, so a piece is there or it is not.
-template <class T, int L, int C, bool WHOLE>
+// A lane's C pieces of rows of d numbers.  Loads and stores are of 16 bytes, those of neighbouring lanes beside each other: in fp32 a piece is two of
+// them, 4 L numbers apart.  WHOLE: rows are whole 16 bytes, which are there or not, and the rows of a workgroup lie within 2^31 bytes, so that what a lane adds to the
+// address of the workgroup's first row is 32 bits and the same for every turn.
+template <class T, int L, int C, bool WHOLE, bool NT>
 struct RowPieces {
-    int d, lane;
-    __device__ __forceinline__ int col(int c) const { return 8 * (c * L + lane); }
-    __device__ __forceinline__ int left(int c) const { return d - col(c); }
-    __device__ __forceinline__ bool has(int c, int j) const { return WHOLE ? left(c) > 0 : j < left(c); }
-    // there: whether there is such a row
-    __device__ __forceinline__ void load(const void *base, int64_t at, bool there, Frag<T> (&f)[C]) const
+    static constexpr int V = T::VEC, UNITS = 8 / V, DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
+    int d, lane, sub;  // sub: which of the workgroup's rows
+    __device__ __forceinline__ int col(int c, int u) const { return V * ((c * UNITS + u) * L + lane); }
+    __device__ __forceinline__ bool has(int c, int j) const { return WHOLE ? col(c, j / V) < d : col(c, j / V) + j % V < d; }
+    __device__ __forceinline__ int64_t at(int64_t row0, int64_t ld, int c, int u) const { return (row0 + sub) * ld + col(c, u); }
+    __device__ __forceinline__ int64_t byte(int64_t row0, int64_t ld, int c, int u) const
     {
+        return row0 * ld * T::BYTES + (static_cast<uint32_t>(sub) * static_cast<uint32_t>(ld) + static_cast<uint32_t>(col(c, u))) * static_cast<uint32_t>(T::BYTES);
+    }
+    static __device__ __forceinline__ ftc_u32x4 whole_piece(const void *base, int64_t at) { return NT ? load_piece_nt<T>(base, at) : load_piece<T>(base, at, V); }
+    static __device__ __forceinline__ void store_whole(void *base, int64_t at, const float (&y)[V])
+    {
+        if constexpr (NT) store_piece_nt<T>(base, at, y);
+        else store_vec_any<V>(base, at, DT, y);
+    }
+    static __device__ __forceinline__ void put(Frag<T> &f, int u, ftc_u32x4 w)
+    {
+        if constexpr (T::BYTES == 4) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if constexpr (WHOLE) f[c] = load_frag<T>(base, at + col(c), there && left(c) > 0 ? 8 : 0);
-            else f[c] = load_frag<T>(base, at + col(c), there ? left(c) : 0);
+            for (int j = 0; j < 4; ++j) f.f[4 * u + j] = __uint_as_float(w[j]);
+        } else {
+            f.w = w;
         }
     }
-    __device__ __forceinline__ void store(void *base, int64_t at, bool there, const float (&x)[C][8]) const
+    static __device__ __forceinline__ void clear(Frag<T> (&f)[C])
     {
-        constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) put(f[c], u, ftc_u32x4{0u, 0u, 0u, 0u});
+    }
+    // What this lane has of a row of the workgroup's, row0 the first of them; there: whether there is this lane's.  What is not there keeps what it was.
+    __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row0, bool there, Frag<T> (&f)[C]) const
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const int left = there ? d - col(c, u) : 0;
+                if (WHOLE ? left > 0 : left >= V) put(f[c], u, whole_piece(WHOLE ? static_cast<const char *>(base) + byte(row0, ld, c, u) : base, WHOLE ? 0 : at(row0, ld, c, u)));
+                else if (!WHOLE && left > 0) put(f[c], u, load_piece<T>(base, at(row0, ld, c, u), left));
+            }
+    }
+    __device__ __forceinline__ void store(void *base, int64_t ld, int64_t row0, bool there, const float (&x)[C][8]) const
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const int left = there ? d - col(c, u) : 0;
+                float y[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) y[j] = x[c][u * V + j];
+                if constexpr (WHOLE) {
+                    if (left > 0) store_whole(static_cast<char *>(base) + byte(row0, ld, c, u), 0, y);
+                } else if (left >= V) {
+                    store_whole(base, at(row0, ld, c, u), y);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V - 1; ++j)
+                        if (j < left) store_elem(base, at(row0, ld, c, u) + j, DT, y[j]);
+                }
+            }
+    }
+    // A vector of d numbers; all vectors are loaded before the first is looked at.  NULL: `none` each
+    __device__ __forceinline__ void fetch(const void *base, Frag<T> (&f)[C]) const
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) put(f[c], u, load_piece<T>(base, col(c, u), base ? d - col(c, u) : 0));
+    }
+    __device__ __forceinline__ void vector(const void *base, const Frag<T> (&f)[C], float none, float (&x)[C][8]) const
+    {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if constexpr (WHOLE) {
-                if (there && left(c) > 0) store_eight_numbers(base, at + col(c), DT, 8, x[c]);
-            } else {
-                if (there) store_eight_numbers(base, at + col(c), DT, left(c), x[c]);
-            }
+            frag_numbers<T>(f[c], x[c]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[c][j] = base ? x[c][j] : none;
         }
     }
 };
 
+// Whether rows at `ld` can be taken as WHOLE.
+template <class T>
+inline bool whole_rows(int d, int64_t ld) { return d % T::VEC == 0 && 64 * ld * T::BYTES < (1ll << 31); }
+
 // Mean (0 for FTC_NORM_RMS) of a row and what its distance from there is multiplied by.  The squares are those of the distances, from registers, so
 // a mean that is large beside the spread costs nothing.  Distances from 1e19 on, whose squares are infinite in fp32, once more times 2^-96.
-template <class T, int L, int C, bool WHOLE>
-__device__ __forceinline__ void row_statistics(const RowPieces<T, L, C, WHOLE> &r, int kind, float eps, const float (&x)[C][8], float *area, int &turn, float &mean, float &rstd)
+template <class T, int L, int C, bool WHOLE, bool NT>
+__device__ __forceinline__ void row_statistics(const RowPieces<T, L, C, WHOLE, NT> &r, int kind, float eps, const float (&x)[C][8], float *area, int &turn, float &mean, float &rstd)
 {
     const float each = 1.f / static_cast<float>(r.d);
+    float s[1] = {0.f};
     mean = 0.f;
     if (kind == FTC_NORM_LAYER) {  // uniform
-        float s[1] = {0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[0] = fmaf(x[c][j], each, s[0]);  // zeros behind the row; no sum beyond the largest number
         row_sums<L, 1>(s, area, turn);
         mean = s[0];
-    }
-    auto squares = [&](float scale) {
-        float s[1] = {0.f};
+        s[0] = 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float v = r.has(c, j) ? (x[c][j] - mean) * scale : 0.f;
+                const float v = r.has(c, j) ? x[c][j] - mean : 0.f;
+                s[0] = fmaf(v, v, s[0]);
+            }
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[0] = fmaf(x[c][j], x[c][j], s[0]);
+    }
+    row_sums<L, 1>(s, area, turn);
+    rstd = 1.f / sqrtf(fmaf(s[0], each, eps));
+    // lanes that meet in row_sums go the same way: those of a wave, or of a workgroup, which has one row then
+    const bool wide = s[0] == INFINITY;
+    if (L > 64 ? wide : __builtin_amdgcn_ballot_w64(wide) != 0) {
+        s[0] = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = r.has(c, j) ? (x[c][j] - mean) * 0x1p-96f : 0.f;
                 s[0] = fmaf(v, v, s[0]);
             }
         row_sums<L, 1>(s, area, turn);
-        return s[0] * each;
-    };
-    const float s = squares(1.f);
-    rstd = 1.f / sqrtf(s + eps);
-    // lanes that meet in row_sums go the same way: those of a wave, or of a workgroup, which has one row then
-    const bool wide = s == INFINITY;
-    if (L > 64 ? wide : __builtin_amdgcn_ballot_w64(wide) != 0) {
-        const float t = squares(0x1p-96f);
-        if (wide) rstd = 0x1p-96f / sqrtf(t);
+        if (wide) rstd = 0x1p-96f / sqrtf(s[0] * each);
     }
 }
 

@@ -18,88 +18,135 @@ struct BlockGradArgs {
     float *part[SUMS];  // gridDim.x rows of d each, or NULL
 };
 
-template <class T, int L, int C, bool WHOLE>
+// BLOCK: with F
+template <class T, int L, int C, bool BLOCK, bool WHOLE, bool NT>
 __global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(BlockArgs a, BlockGradArgs g)
 {
     constexpr int THREADS = row_threads(L), GROUPS = THREADS / L;
     __shared__ float area[64];
     __shared__ __align__(16) float joined[GROUPS > 1 ? THREADS * C * 8 : 1];
     int turn = 0;
-    const RowPieces<T, L, C, WHOLE> r = {a.d, static_cast<int>(threadIdx.x) % L};
-    const int sub = threadIdx.x / L;
+    const RowPieces<T, L, C, WHOLE, NT> r = {a.d, static_cast<int>(threadIdx.x) % L, L < 64 ? static_cast<int>(threadIdx.x) / L : __builtin_amdgcn_readfirstlane(threadIdx.x / L)};
+    const int sub = r.sub;
     const float each = 1.f / static_cast<float>(a.d);
-    Frag<T> post_w[C], post_b[C], pre_w[C], gate[C];
-    r.load(a.post_w, 0, a.post_w != nullptr, post_w);
-    r.load(a.post_b, 0, a.post_b != nullptr, post_b);
-    r.load(a.pre_w, 0, a.pre_w != nullptr, pre_w);
-    r.load(a.gate, 0, a.gate && a.ldg == 0, gate);
-    float sum[SUMS][C][8];
+    float post_w[C][8], post_b[C][8], pre_w[C][8], one_gate[C][8], sum[SUMS][C][8];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k)
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[k][c][j] = 0.f;
-    // N'(gr) for the weights wf, its sums on the way; gr is replaced
-    auto back = [&](int kind, const float (&xh)[C][8], float rstd, const void *w, const Frag<T> (&wf)[C], float (&sw)[C][8], float (&sb)[C][8], float (&gr)[C][8]) {
+    // N'(gr), its sums on the way; gr is replaced.  Numbers behind a row's end are zeros all the way
+    auto back = [&](int kind, const float (&xh)[C][8], float rstd, const float (&w)[C][8], float (&sw)[C][8], float (&sb)[C][8], float (&gr)[C][8]) {
         float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            float wn[8];
-            frag_numbers<T>(wf[c], wn);
+        for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 sw[c][j] = fmaf(gr[c][j], xh[c][j], sw[c][j]);
                 sb[c][j] += gr[c][j];
-                if (w) gr[c][j] *= wn[j];
+                gr[c][j] *= w[c][j];
                 s[0] = fmaf(gr[c][j], xh[c][j], s[0]);
                 s[1] += gr[c][j];
             }
-        }
         row_sums<L, 2>(s, area, turn);
         s[0] *= each;
         s[1] = kind == FTC_NORM_LAYER ? s[1] * each : 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) gr[c][j] = r.has(c, j) ? rstd * (gr[c][j] - fmaf(xh[c][j], s[0], s[1])) : 0.f;
+            for (int j = 0; j < 8; ++j) gr[c][j] = (r.has(c, j) ? rstd : 0.f) * (gr[c][j] - fmaf(xh[c][j], s[0], s[1]));
     };
-    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * GROUPS; row0 < a.n; row0 += static_cast<int64_t>(gridDim.x) * GROUPS) {
-        const int64_t row = row0 + sub;
-        const bool there = row < a.n;
-        Frag<T> x[C], f[C], dh[C], du[C];
-        r.load(a.X, row * a.ldx, there, x);
-        r.load(a.F, row * a.ldf, there && a.F, f);
-        r.load(g.dH, row * g.lddh, there && g.dH, dh);
-        r.load(g.dU, row * g.lddu, there && g.dU, du);
-        if (a.ldg) r.load(a.gate, row * a.ldg, there, gate);
-        ftc_f32x4 m = {0.f, 0.f, 0.f, 0.f};
-        if (there && g.stats) m = *reinterpret_cast<const ftc_f32x4 *>(g.stats + 4 * row);
-        // numbers behind a row's end are zeros all the way: normalised ones are made so
-        float fh[C][8], p[C][8], hh[C][8], gr[C][8];
+    // the next rows are on their way while these are worked on
+    const int64_t step = static_cast<int64_t>(gridDim.x) * GROUPS;
+    Frag<T> next_x[C], next_f[C], next_dh[C], next_du[C], next_gate[C];
+    ftc_f32x4 next_m = {0.f, 0.f, 0.f, 0.f};
+    r.clear(next_x);
+    r.clear(next_f);
+    r.clear(next_dh);
+    r.clear(next_du);
+    r.clear(next_gate);
+    auto fetch = [&](int64_t row0) {
+        const bool there = row0 + sub < a.n;
+        if (row0 + GROUPS > a.n) {  // uniform: rows that are not there add nothing
+            r.clear(next_x);
+            r.clear(next_f);
+            r.clear(next_dh);
+            r.clear(next_du);
+            next_m = ftc_f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        r.load(a.X, a.ldx, row0, there, next_x);
+        if (BLOCK) r.load(a.F, a.ldf, row0, there, next_f);
+        if (g.dH) r.load(g.dH, g.lddh, row0, there, next_dh);
+        if (g.dU) r.load(g.dU, g.lddu, row0, there, next_du);
+        if (BLOCK && a.ldg) r.load(a.gate, a.ldg, row0, there, next_gate);
+        if (there && g.stats) next_m = *reinterpret_cast<const ftc_f32x4 *>(g.stats + 4 * (row0 + sub));
+    };
+    fetch(static_cast<int64_t>(blockIdx.x) * GROUPS);
+    Frag<T> raw_post_w[C], raw_post_b[C], raw_pre_w[C], raw_gate[C];
+    r.fetch(a.post_w, raw_post_w);
+    r.fetch(a.post_b, raw_post_b);
+    r.fetch(a.pre_w, raw_pre_w);
+    r.fetch(a.ldg ? nullptr : a.gate, raw_gate);
+    r.vector(a.post_w, raw_post_w, 1.f, post_w);
+    r.vector(a.post_b, raw_post_b, 0.f, post_b);
+    r.vector(a.pre_w, raw_pre_w, 1.f, pre_w);
+    r.vector(a.ldg ? nullptr : a.gate, raw_gate, 1.f, one_gate);
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * GROUPS; row0 < a.n; row0 += step) {
+        const bool there = row0 + sub < a.n;
+        const ftc_f32x4 m = next_m;
+        float fh[C][8], p[C][8], hh[C][8], gr[C][8], gate[C][8];
+        Frag<T> dh[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            float xn[8], gn[8], w[8], b[8];
-            frag_numbers<T>(x[c], xn);
-            frag_numbers<T>(f[c], fh[c]);
-            frag_numbers<T>(gate[c], gn);
-            frag_numbers<T>(post_w[c], w);
-            frag_numbers<T>(post_b[c], b);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (a.post != FTC_NORM_NONE) {
-                    fh[c][j] = r.has(c, j) ? (fh[c][j] - m[0]) * m[1] : 0.f;
-                    p[c][j] = fmaf(fh[c][j], a.post_w ? w[j] : 1.f, b[j]);
-                } else {
-                    p[c][j] = fh[c][j];
-                }
-                float h = a.x_scale * xn[j];
-                if (a.F) h = fmaf(a.x_scale, xn[j], a.gate ? gn[j] * p[c][j] : p[c][j]);
-                hh[c][j] = r.has(c, j) ? (h - m[2]) * m[3] : 0.f;
-            }
-            frag_numbers<T>(du[c], gr[c]);
+            frag_numbers<T>(next_x[c], hh[c]);
+            frag_numbers<T>(next_f[c], fh[c]);
+            frag_numbers<T>(next_du[c], gr[c]);
+            dh[c] = next_dh[c];
         }
-        if (a.pre != FTC_NORM_NONE) back(a.pre, hh, m[3], a.pre_w, pre_w, sum[SUM_PRE_W], sum[SUM_PRE_B], gr);
+        if (BLOCK && a.ldg) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) frag_numbers<T>(next_gate[c], gate[c]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) gate[c][j] = one_gate[c][j];
+        }
+        if (row0 + step < a.n) fetch(row0 + step);
+        if (BLOCK && a.post != FTC_NORM_NONE) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    fh[c][j] = (fh[c][j] - m[0]) * (r.has(c, j) ? m[1] : 0.f);
+                    p[c][j] = fmaf(fh[c][j], post_w[c][j], post_b[c][j]);
+                }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[c][j] = fh[c][j];
+        }
+        if (a.pre != FTC_NORM_NONE) {
+            // as the forward pass has h
+            if constexpr (BLOCK) {
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) hh[c][j] = fmaf(a.x_scale, hh[c][j], gate[c][j] * p[c][j]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) hh[c][j] *= a.x_scale;
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) hh[c][j] = (hh[c][j] - m[2]) * (r.has(c, j) ? m[3] : 0.f);
+            back(a.pre, hh, m[3], pre_w, sum[SUM_PRE_W], sum[SUM_PRE_B], gr);
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float v[8];
@@ -113,25 +160,22 @@ __global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(Blo
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[c][j] = a.x_scale * gr[c][j];
-            r.store(g.dX, row * g.lddx, there, v);
+            r.store(g.dX, g.lddx, row0, there, v);
         }
-        if (!a.F) continue;
+        if constexpr (!BLOCK) continue;
         if (a.gate) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float gn[8];
-                frag_numbers<T>(gate[c], gn);
+            for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     p[c][j] *= gr[c][j];  // dgate
                     sum[SUM_GATE][c][j] += p[c][j];
-                    gr[c][j] *= gn[j];
+                    gr[c][j] *= gate[c][j];
                 }
-            }
-            if (g.dgate) r.store(g.dgate, row * g.lddg, there, p);
+            if (g.dgate) r.store(g.dgate, g.lddg, row0, there, p);
         }
-        if (a.post != FTC_NORM_NONE) back(a.post, fh, m[1], a.post_w, post_w, sum[SUM_POST_W], sum[SUM_POST_B], gr);
-        if (g.dF) r.store(g.dF, row * g.lddf, there, gr);
+        if (a.post != FTC_NORM_NONE) back(a.post, fh, m[1], post_w, sum[SUM_POST_W], sum[SUM_POST_B], gr);
+        if (g.dF) r.store(g.dF, g.lddf, row0, there, gr);
     }
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) {
@@ -139,7 +183,10 @@ __global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(Blo
         float *to = g.part[k] + static_cast<int64_t>(blockIdx.x) * a.d;
         if constexpr (GROUPS == 1) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) store_eight_numbers(to, r.col(c), FTC_F32, r.left(c), sum[k][c]);
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (r.has(c, j)) to[r.col(c, j / T::VEC) + j % T::VEC] = sum[k][c][j];
         } else {
             constexpr int COLS = L * C * 8;
             __syncthreads();
@@ -147,7 +194,7 @@ __global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(Blo
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; j += 4)
-                    *reinterpret_cast<ftc_f32x4 *>(joined + sub * COLS + r.col(c) + j) = ftc_f32x4{sum[k][c][j], sum[k][c][j + 1], sum[k][c][j + 2], sum[k][c][j + 3]};
+                    *reinterpret_cast<ftc_f32x4 *>(joined + sub * COLS + r.col(c, j / T::VEC) + j % T::VEC) = ftc_f32x4{sum[k][c][j], sum[k][c][j + 1], sum[k][c][j + 2], sum[k][c][j + 3]};
             __syncthreads();
             for (int i = threadIdx.x; i < COLS && i < a.d; i += THREADS) {
                 float v = 0.f;
@@ -195,12 +242,6 @@ __global__ __launch_bounds__(SUM_THREADS) void block_norm_sums_kernel(int parts,
     }
 }
 
-// Workgroups of a launch, which are the rows of the sums' parts.
-static int backward_groups(int n, int lanes)
-{
-    const int threads = row_threads(lanes), most = 256 * 512 / threads, groups = ceil_div(n, threads / lanes);
-    return groups < most ? groups : most;
-}
 static int lanes_of(int d)
 {
     int lanes = 4;
@@ -208,17 +249,26 @@ static int lanes_of(int d)
     return d > 8192 ? 1024 : lanes;
 }
 
+// Workgroups of a launch, which are the rows of the sums' parts.
+static int backward_groups(int n, int d) { return row_groups(n, lanes_of(d), 512); }
+
 size_t block_norm_backward_ws(int n, int d)
 {
-    return align_up(static_cast<size_t>(SUMS) * backward_groups(n, lanes_of(d)) * d * sizeof(float), 256);
+    return align_up(static_cast<size_t>(SUMS) * backward_groups(n, d) * d * sizeof(float), 256);
 }
 
-template <class T, int L, int C>
+template <class T, int L, int C, bool BLOCK>
 static void backward_t(const BlockArgs &a, const BlockGradArgs &g, int groups, hipStream_t s)
 {
-    constexpr int THREADS = row_threads(L);
-    if (a.d % 8 == 0) hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, true>), dim3(groups), dim3(THREADS), 0, s, a, g);
-    else hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, false>), dim3(groups), dim3(THREADS), 0, s, a, g);
+    const int64_t lds[8] = {a.ldx, a.ldf, a.ldg, g.lddh, g.lddu, g.lddx, g.lddf, g.lddg};
+    const void *const arrays[8] = {a.X, a.F, a.ldg ? a.gate : nullptr, g.dH, g.dU, g.dX, g.dF, g.dgate};
+    bool whole = true;
+    int64_t bytes = 0;
+    for (int64_t ld : lds) whole = whole && whole_rows<T>(a.d, ld);
+    for (const void *p : arrays) bytes += p ? static_cast<int64_t>(a.n) * a.d * T::BYTES : 0;
+    if (whole && row_stream(bytes)) hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, BLOCK, true, true>), dim3(groups), dim3(row_threads(L)), 0, s, a, g);
+    else if (whole) hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, BLOCK, true, false>), dim3(groups), dim3(row_threads(L)), 0, s, a, g);
+    else hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, BLOCK, false, false>), dim3(groups), dim3(row_threads(L)), 0, s, a, g);
 }
 
 int32_t launch_block_norm_backward(const ftc_block &b, const float *stats, const void *dH, int lddh, const void *dU, int lddu,
@@ -226,7 +276,7 @@ int32_t launch_block_norm_backward(const ftc_block &b, const float *stats, const
 {
     const BlockArgs a = {b.n, b.d, b.F ? b.post : FTC_NORM_NONE, b.pre, b.eps, b.x_scale, b.X, b.F, b.gate, b.post_w, b.post_b, b.pre_w, b.pre_b, b.ldx, b.ldf, b.ldg};
     const bool rows = b.gate && b.ldg != 0;
-    const int groups = backward_groups(b.n, lanes_of(b.d));
+    const int groups = backward_groups(b.n, b.d);
     BlockGradArgs k = {stats, dH, dU, g.dX, g.dF, rows ? g.dgate : nullptr, lddh, lddu, g.lddx, g.lddf, g.lddg, {}};
     BlockSums sums = {};
     void *const outs[SUMS] = {rows ? nullptr : g.dgate, g.dpost_w, g.dpost_b, g.dpre_w, g.dpre_b};
@@ -238,7 +288,11 @@ int32_t launch_block_norm_backward(const ftc_block &b, const float *stats, const
         sums.part[i] = k.part[i] = static_cast<float *>(ws) + static_cast<size_t>(i) * groups * b.d;
     }
     if (b.n > 0) {
-#define FTC_ROWS(T, L, C) backward_t<T, L, C>(a, k, groups, s)
+#define FTC_ROWS(T, L, C)                                       \
+    do {                                                        \
+        if (a.F) backward_t<T, L, C, true>(a, k, groups, s);    \
+        else backward_t<T, L, C, false>(a, k, groups, s);       \
+    } while (0)
 #define FTC_WIDTHS(T)                                \
     do {                                             \
         if (b.d <= 32) FTC_ROWS(T, 4, 1);            \
