@@ -3,11 +3,16 @@
 
 namespace ftc {
 
+int64_t grouped_dw_groups(int n, int groups, int k_each, int64_t tiles)
+{
+    const int64_t turn = 8 * dw_unit(static_cast<int>(tiles < DW_EIGHT ? tiles : DW_EIGHT));
+    return (grouped_most(n, groups, k_each) * tiles + turn - 1) / turn * turn;
+}
+
 template <class T, bool FAST>
 static void dw_t(const GroupedArgs &g, int tile, hipStream_t s)
 {
-    const int64_t chunks = (grouped_numbers(g.a.K, g.groups, g.a.k_each) + 7) / 8 * 8;
-    const dim3 grid(static_cast<unsigned>(chunks * dense_tiles(g.a.M, g.a.N, tile)));
+    const dim3 grid(static_cast<unsigned>(grouped_dw_groups(g.a.K, g.groups, g.a.k_each, dense_tiles(g.a.M, g.a.N, tile))));
     if (tile == DENSE_64) {
         hipLaunchKernelGGL((grouped_dw_kernel<T, FAST, 2, 2, 1, 1>), grid, dim3(256), 0, s, g);
     } else if (tile == DENSE_128) {

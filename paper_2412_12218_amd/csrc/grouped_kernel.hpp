@@ -1,7 +1,7 @@
 // The product kernels of the grouped dense layer (grouped_linear.hip): the dense layer's tiles, each of one group.
 //
-// The groups' rows are known on the device only, so a launch has as many workgroups as groups could ever need (grouped_plan.hpp) and each looks up what it is
-// for: a wave looks at 64 offsets at once, one step for up to 64 groups, two up to 4096.
+// The groups' rows are known on the device only, so a launch has as many workgroups as groups could ever need (grouped_plan.hpp), and each of them looks up which tile of
+// which group it is for, or that it is not needed.
 #pragma once
 #include "dense_kernel.hpp"
 #include "grouped_plan.hpp"
@@ -29,29 +29,69 @@ inline bool grouped_dw_fast(const DenseArgs &a, int dtype)
     return dense_whole_pieces(a.A, a.lda, a.M, dtype) && dense_whole_pieces(a.B, a.ldb, a.N, dtype);
 }
 
+// Workgroups of a weight gradient's launch.
+int64_t grouped_dw_groups(int n, int groups, int k_each, int64_t tiles);
+
 #if defined(__HIPCC__)
 
+// What a workgroup is for: tile (chunk) `at` of the rows start .. start + len - 1 of a group, of the tiles of all groups; group -1: nothing.
 struct GroupSpan {
-    int group, start, len, at;  // at: which of the group's tiles
+    int group, start, len, at, tiles;
 };
 __device__ __forceinline__ int group_offset(const int *ptr, int i, int n) { return min(max(ptr[i], 0), n); }
+// Tiles of a group; EMPTY: one of a group without rows, too.
+template <bool EMPTY>
+__device__ __forceinline__ int group_tiles(int start, int end, int side)
+{
+    const int len = max(end - start, 0);
+    return EMPTY && len == 0 ? 1 : len / side + (len % side != 0);
+}
 
-// What number `id` stands for (grouped_numbers); group -1: nothing.
-__device__ __forceinline__ GroupSpan group_span(const int *ptr, int groups, int n, int side, int id)
+// The tile `number` of the tiles of all groups, counted in their order; number(tiles): it, from how many there are.  Every wave counts for itself, lane l the groups from
+// l each on, `each` = ceil(groups / 64): one load for up to 64 groups, and a scan over the lanes.  Beyond GROUPS_COUNTED groups nothing is counted: a group's
+// tiles have the numbers of grouped_plan.hpp, some of which stand for nothing, and the group is found by looking at 64 offsets at a time.
+constexpr int GROUPS_COUNTED = 512;
+template <bool EMPTY, class Number>
+__device__ __forceinline__ GroupSpan group_span(const int *ptr, int groups, int n, int side, const Number &number)
 {
     const int lane = threadIdx.x & 63;
-    int lo = 0, hi = groups;  // the last group whose numbers begin at or before id is in lo .. hi - 1
-    do {
-        const int stride = (hi - lo + 63) / 64, i = lo + lane * stride;
-        const bool before = i < hi && group_offset(ptr, i, n) / side + i <= id;
-        const int count = __popcll(__builtin_amdgcn_ballot_w64(before));
-        if (count == 0) return {-1, 0, 0, 0};  // in front of the first group
-        lo += (count - 1) * stride;
-        hi = min(lo + stride, hi);
-    } while (hi - lo > 1);
-    const int start = __builtin_amdgcn_readfirstlane(group_offset(ptr, lo, n)), end = __builtin_amdgcn_readfirstlane(group_offset(ptr, lo + 1, n));
-    const int at = id - start / side - lo;
-    return {at < 0 ? -1 : lo, start, max(end - start, 0), at};  // below 0: offsets that decrease
+    if (groups > GROUPS_COUNTED) {
+        const int tiles = n / side + groups, wanted = number(tiles);
+        if (wanted < 0 || wanted >= tiles) return {-1, 0, 0, 0, tiles};
+        int lo = 0, hi = groups;  // the last group whose numbers begin at or before it is in lo .. hi - 1
+        do {
+            const int stride = (hi - lo + 63) / 64, i = lo + lane * stride;
+            const bool before = i < hi && group_offset(ptr, i, n) / side + i <= wanted;
+            const int count = __popcll(__builtin_amdgcn_ballot_w64(before));
+            if (count == 0) return {-1, 0, 0, 0, tiles};  // in front of the first group
+            lo += (count - 1) * stride;
+            hi = min(lo + stride, hi);
+        } while (hi - lo > 1);
+        const int s = __builtin_amdgcn_readfirstlane(group_offset(ptr, lo, n)), e = __builtin_amdgcn_readfirstlane(group_offset(ptr, lo + 1, n)), at = wanted - s / side - lo;
+        return {at >= 0 && at < group_tiles<EMPTY>(s, e, side) ? lo : -1, s, max(e - s, 0), at, tiles};
+    }
+    const int each = (groups + 63) / 64, from = min(lane * each, groups), to = min(from + each, groups);
+    int own = 0, start = group_offset(ptr, from, n), last = start;
+#pragma unroll 4
+    for (int g = from; g < to; ++g) {
+        const int end = group_offset(ptr, g + 1, n);
+        own += group_tiles<EMPTY>(last, end, side);
+        last = end;
+    }
+    const int upto = wave_inclusive_scan(own), tiles = __builtin_amdgcn_readlane(upto, 63), wanted = number(tiles);
+    if (wanted < 0 || wanted >= tiles) return {-1, 0, 0, 0, tiles};
+    const int at_lane = __popcll(__builtin_amdgcn_ballot_w64(upto <= wanted));  // the first lane that has more
+    int g = min(at_lane * each, groups - 1), at = wanted - __builtin_amdgcn_readlane(upto - own, at_lane);
+    int s = __builtin_amdgcn_readlane(start, at_lane), e = each == 1 ? __builtin_amdgcn_readlane(last, at_lane) : group_offset(ptr, g + 1, n);
+    for (int k = 1; k < each; ++k) {  // uniform
+        const int there = group_tiles<EMPTY>(s, e, side);
+        if (at < there) break;
+        at -= there;
+        s = e;
+        g = min(g + 1, groups - 1);
+        e = group_offset(ptr, g + 1, n);
+    }
+    return {at >= 0 && at < group_tiles<EMPTY>(s, e, side) ? g : -1, s, max(e - s, 0), at, tiles};  // else: offsets that decrease
 }
 
 __device__ __forceinline__ const void *moved(const void *p, int64_t bytes) { return p ? static_cast<const char *>(p) + bytes : nullptr; }
@@ -63,10 +103,20 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void grouped_rows_kernel(GroupedAr
 {
     constexpr int TM = 32 * WM * RW, TN = 32 * WN * CW;
     DenseArgs a = g.a;
-    int id, tn;
-    dense_tile(blockIdx.x, a.M / TM + g.groups, (a.N + TN - 1) / TN, id, tn);
-    const GroupSpan span = group_span(g.group_ptr, g.groups, a.M, TM, id);
-    if (span.group < 0 || static_cast<int64_t>(span.at) * TM >= span.len) return;
+    const int tiles_n = (a.N + TN - 1) / TN;
+    int tn = 0;
+    // groups of few rows are bound by reading their weights, which no two tiles share: those of a group go round the XCDs
+    const GroupSpan span = group_span<false>(g.group_ptr, g.groups, a.M, TM, [&](int tiles) {
+        int tm = -1;
+        if (TM == 32) {
+            tm = blockIdx.x / tiles_n;
+            tn = blockIdx.x % tiles_n;
+        } else if (blockIdx.x < static_cast<unsigned>(tiles * tiles_n)) {
+            dense_tile(blockIdx.x, tiles, tiles_n, tm, tn);
+        }
+        return tm;
+    });
+    if (span.group < 0) return;
     const int64_t first = span.start;
     const int k_begin = static_cast<int>(blockIdx.y) * a.k_each, k_end = min(a.K, k_begin + a.k_each);
     float *part = a.splits > 1 ? a.part + (static_cast<int64_t>(blockIdx.y) * a.M + first) * a.N : nullptr;
@@ -80,18 +130,21 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void grouped_rows_kernel(GroupedAr
     dense_product<T, false, BX, FAST, RW, CW, WM, WN>(a, span.at, tn, k_begin, k_end, part);
 }
 
-// Chunks go round the XCDs; all the tiles of a chunk, which share its rows, are of one.
+// Eight tiles of a chunk (a band's column, dense_band: they share the rows of both operands) are of one XCD, the eights go round the XCDs.
+constexpr int DW_EIGHT = 8;
+inline __host__ __device__ int dw_unit(int tiles) { return tiles < DW_EIGHT ? tiles : DW_EIGHT; }
 template <class T, bool FAST, int RW, int CW, int WM, int WN>
 __global__ __launch_bounds__(64 * RW * CW, 2) void grouped_dw_kernel(GroupedArgs g)
 {
     constexpr int TM = 32 * WM * RW, TN = 32 * WN * CW;
     DenseArgs a = g.a;
-    const int tiles_m = (a.M + TM - 1) / TM, tiles_n = (a.N + TN - 1) / TN, tiles = tiles_m * tiles_n, k = blockIdx.x / 8;
+    const int tiles_m = (a.M + TM - 1) / TM, tiles_n = (a.N + TN - 1) / TN, tiles = tiles_m * tiles_n, unit = dw_unit(tiles), k = blockIdx.x / 8;
+    const int item = (k / unit * 8 + static_cast<int>(blockIdx.x) % 8) * unit + k % unit;
     int tm, tn;
-    dense_band(k % tiles, tiles_m, tiles_n, tm, tn);
-    const GroupSpan span = group_span(g.group_ptr, g.groups, a.K, a.k_each, k / tiles * 8 + static_cast<int>(blockIdx.x) % 8);
-    const int chunks = span.len > a.k_each ? (span.len + a.k_each - 1) / a.k_each : 1;  // a group without rows has zeros to write
-    if (span.group < 0 || span.at >= chunks) return;
+    dense_band(item % tiles, tiles_m, tiles_n, tm, tn);
+    const GroupSpan span = group_span<true>(g.group_ptr, g.groups, a.K, a.k_each, [&](int) { return item / tiles; });
+    if (span.group < 0) return;
+    const int chunks = group_tiles<true>(span.start, span.start + span.len, a.k_each);  // a group without rows has zeros to write
     const int64_t first = span.start + static_cast<int64_t>(span.at) * a.k_each;
     float *part = chunks > 1 ? a.part + (2ll * (span.start / a.k_each) + span.at) * a.M * a.N : nullptr;
     a.K = min(a.k_each, span.len - span.at * a.k_each);
@@ -104,7 +157,7 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void grouped_dw_kernel(GroupedArgs
 template <class T, bool BX, bool FAST>
 void launch_grouped_rows_t(const GroupedArgs &g, int tile, hipStream_t s)
 {
-    const dim3 grid(static_cast<unsigned>(grouped_numbers(g.a.M, g.groups, grouped_rows(tile)) * ceil_div(g.a.N, grouped_columns(tile))), g.a.splits);
+    const dim3 grid(static_cast<unsigned>(grouped_most(g.a.M, g.groups, grouped_rows(tile)) * ceil_div(g.a.N, grouped_columns(tile))), g.a.splits);
     if (tile == DENSE_64) {
         hipLaunchKernelGGL((grouped_rows_kernel<T, BX, FAST, 2, 2, 1, 1>), grid, dim3(256), 0, s, g);
     } else if (tile == DENSE_128) {

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void grouped_dw_join_kernel(GroupedArgs g)
     }
 }
 
-// dP = dZ act'(P) (dP NULL: not written) and, for the rows of a workgroup, which are of one group, its column sums (sums NULL: none), by the group's numbers
+// dP = dZ act'(P) (dP NULL: not written) and, for the rows of a workgroup, which are of one group, its column sums (sums NULL: none), by the tile's number
 // (grouped_plan.hpp).  2^log_lanes threads have the 16 bytes of VEC columns each of a row; a thread has DP_ROWS rows, all of them on their way at once.
 constexpr int DP_ROWS = 4;
 static int dp_lanes(int width, int vec)
@@ -92,8 +92,8 @@ __global__ __launch_bounds__(256) void grouped_dp_kernel(int n, const int *__res
     constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16, V = T::VEC;
     __shared__ float part[256 * V];
     const int lanes = 1 << log_lanes, subs = 256 >> log_lanes, side = subs * DP_ROWS;
-    const GroupSpan span = group_span(ptr, groups, n, side, blockIdx.x);
-    if (span.group < 0 || static_cast<int64_t>(span.at) * side >= span.len) return;
+    const GroupSpan span = group_span<false>(ptr, groups, n, side, [&](int) { return static_cast<int>(blockIdx.x); });
+    if (span.group < 0) return;
     const int lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> log_lanes, col = (blockIdx.y * lanes + lane) * V, left = width - col;
     const int64_t row0 = span.start + static_cast<int64_t>(span.at) * side + sub, end = span.start + span.len;
     ftc_u32x4 w[DP_ROWS], u[DP_ROWS];
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void grouped_dp_kernel(int n, const int *__res
         __syncthreads();
     }
     for (int i = threadIdx.x; i < columns; i += 256)
-        if (blockIdx.y * columns + i < static_cast<unsigned>(width)) sums[static_cast<int64_t>(blockIdx.x) * width + blockIdx.y * columns + i] = part[i];
+        if (blockIdx.y * columns + i < static_cast<unsigned>(width)) sums[static_cast<int64_t>(span.start / side + span.group + span.at) * width + blockIdx.y * columns + i] = part[i];
 }
 
 // db_g = sum of the sums of the group's rows: 16 columns a workgroup, 16 threads a column.
@@ -185,11 +185,11 @@ static size_t rows_ws(int n, int groups, int N, int K)
     }
     return most > 1 ? align_up(static_cast<size_t>(most) * n * N * sizeof(float), 256) : 0;
 }
-static size_t dw_ws(int n, int M, int N)
+static size_t dw_ws(int n, int groups, int M, int N)
 {
     int64_t most = 0;
     for (int v = 0; v < 4; ++v) {
-        const int64_t parts = grouped_dw_parts(n, grouped_dw_plan(n, M, N, v & 1, v & 2));
+        const int64_t parts = grouped_dw_parts(n, grouped_dw_plan(n, groups, M, N, v & 1, v & 2));
         if (parts > most) most = parts;
     }
     return align_up(static_cast<size_t>(most) * M * N * sizeof(float), 256);
@@ -215,7 +215,7 @@ static void add_rows_size(LaunchSize &z, int n, int groups, int N, int K)
 {
     for (int v = 0; v < 4; ++v) {
         const DensePlan p = grouped_plan(n, groups, N, K, v & 1, v & 2);
-        z.add(grouped_numbers(n, groups, grouped_rows(p.tile)) * dense_parts(N, grouped_columns(p.tile)) * grouped_threads(p.tile), p.splits);
+        z.add(grouped_most(n, groups, grouped_rows(p.tile)) * dense_parts(N, grouped_columns(p.tile)) * grouped_threads(p.tile), p.splits);
     }
     z.add(static_cast<int64_t>(n) * ceil_div(N, 8), 1);
 }
@@ -230,13 +230,13 @@ LaunchSize grouped_linear_backward_size(int n, int groups, int d_in, int d_out)
     LaunchSize z;
     add_rows_size(z, n, groups, d_in, d_out);
     for (int v = 0; v < 4; ++v) {
-        const DensePlan p = grouped_dw_plan(n, d_in, d_out, v & 1, v & 2);
-        z.add((grouped_numbers(n, groups, p.k_each) + 7) * dense_tiles(d_in, d_out, p.tile) * grouped_threads(p.tile), n / p.k_each);
+        const DensePlan p = grouped_dw_plan(n, groups, d_in, d_out, v & 1, v & 2);
+        z.add(grouped_dw_groups(n, groups, p.k_each, dense_tiles(d_in, d_out, p.tile)) * grouped_threads(p.tile), n / p.k_each);
     }
     z.add(static_cast<int64_t>(d_in) * d_out / 4, 1);
     for (int vec = 4; vec <= 8; vec *= 2) {
         const int lanes = dp_lanes(d_out, vec);
-        z.add(256ll * grouped_numbers(n, groups, dp_rows(lanes)), ceil_div(d_out, vec << lanes));
+        z.add(256ll * grouped_most(n, groups, dp_rows(lanes)), ceil_div(d_out, vec << lanes));
     }
     z.add(static_cast<int64_t>(DB_THREADS) * groups, ceil_div(d_out, 16));
     return z;
@@ -247,12 +247,12 @@ size_t grouped_linear_ws(int n, int groups, int d_in, int d_out) { return rows_w
 static size_t sums_bytes(int n, int groups, int d_out)
 {
     const int rows = dp_rows(dp_lanes(d_out, 4));  // those of fp32 are at most as many as those of 16 bits
-    return align_up(static_cast<size_t>(grouped_numbers(n, groups, rows)) * d_out * sizeof(float), 256);
+    return align_up(static_cast<size_t>(grouped_most(n, groups, rows)) * d_out * sizeof(float), 256);
 }
 
 size_t grouped_linear_backward_ws(int n, int groups, int d_in, int d_out)
 {
-    const size_t x = rows_ws(n, groups, d_in, d_out), w = dw_ws(n, d_in, d_out);
+    const size_t x = rows_ws(n, groups, d_in, d_out), w = dw_ws(n, groups, d_in, d_out);
     return align_up(static_cast<size_t>(n) * d_out * sizeof(float), 256) + sums_bytes(n, groups, d_out) + (x > w ? x : w);
 }
 
@@ -280,7 +280,7 @@ static void grouped_backward_t(const LinearShape &p, const LinearGrads &k, const
     const void *G = p.slope ? dP : k.dZ;
     const int64_t ldg = p.slope ? p.d_out : k.lddz;
     if ((p.slope || k.db) && p.n > 0) {
-        const dim3 grid(static_cast<unsigned>(grouped_numbers(p.n, groups, side)), ceil_div(p.d_out, T::VEC << lanes));
+        const dim3 grid(static_cast<unsigned>(grouped_most(p.n, groups, side)), ceil_div(p.d_out, T::VEC << lanes));
         hipLaunchKernelGGL(grouped_dp_kernel<T>, grid, dim3(256), 0, s, p.n, group_ptr, groups, p.d_out, k.dZ, static_cast<int64_t>(k.lddz), p.slope,
                            static_cast<int64_t>(p.lds), p.slope ? dP : nullptr, k.db ? sums : nullptr, lanes);
     }
@@ -301,7 +301,7 @@ static void grouped_backward_t(const LinearShape &p, const LinearGrads &k, const
         a.A = p.X; a.lda = p.ldx; a.B = G; a.ldb = ldg;
         a.M = p.d_in; a.N = p.d_out; a.K = p.n;
         a.out = k.dW; a.ldo = p.d_out; a.out_dtype = k.dw_dtype;
-        const DensePlan plan = grouped_dw_plan(p.n, p.d_in, p.d_out, p.dtype == FTC_F32, grouped_dw_fast(a, p.dtype));
+        const DensePlan plan = grouped_dw_plan(p.n, groups, p.d_in, p.d_out, p.dtype == FTC_F32, grouped_dw_fast(a, p.dtype));
         a.k_each = plan.k_each;
         a.part = reinterpret_cast<float *>(q);
         launch_grouped_dw(g, p.dtype, plan.tile, s);

@@ -11,10 +11,11 @@ constexpr int grouped_rows(int tile) { return tile == GROUPED_THIN ? 32 : dense_
 constexpr int grouped_columns(int tile) { return tile == GROUPED_THIN ? 128 : dense_side(tile); }
 constexpr int grouped_threads(int tile) { return tile == DENSE_256 ? 512 : 256; }
 
-// Groups begin anywhere, and tiles (or chunks, in the weight gradient) of `side` rows begin anew with each.  Group g, rows s .. e - 1, has the numbers from
-// s / side + g on: ceil((e - s) / side) <= e / side - s / side + 1, so the next one's are behind them, whatever the groups are, and n / side + groups numbers do for
-// all of them; some stand for nothing.
-inline int64_t grouped_numbers(int n, int groups, int side) { return static_cast<int64_t>(n / side) + groups; }
+// Groups begin anywhere, and tiles (or chunks, in the weight gradient) of `side` rows begin anew with each, so n rows in groups have at most this many, those of groups
+// without rows, one each in the weight gradient, included.
+inline int64_t grouped_most(int n, int groups, int side) { return static_cast<int64_t>(n / side) + groups; }
+// What a tile of a group leaves for a later kernel has a place by its number: group g, rows s .. e - 1, has the numbers from s / side + g on.  ceil((e - s) / side) <= e / side - s / side + 1,
+// so the next group's are behind them, whatever the groups are, and all are below grouped_most().
 
 // Z and dX: n rows in groups.
 inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fast)
@@ -50,9 +51,35 @@ inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fa
     return best;
 }
 
-// dW: a group's contraction is over its rows, in chunks of at most k_each of them.  As the dense layer has it for all the rows in one group, which no
-// group has more of; where there are groups enough these have their chunks to themselves.
-inline DensePlan grouped_dw_plan(int n, int M, int N, bool f32, bool fast) { return dense_plan(M, N, n, f32, fast); }
+// dW: a group's contraction is over its rows, in chunks of at most k_each of them, each for a workgroup a tile.  Time by the work of a compute unit, with half a chunk more a
+// group, or by that of the longest chunk, whichever is more; parts are written and read once, those of groups of several chunks.
+inline DensePlan grouped_dw_plan(int n, int groups, int M, int N, bool f32, bool fast)
+{
+    static constexpr DenseCost cost[2][3] = {{{0.45f, 0.22f, 5}, {0.79f, 0.53f, 2}, {1.74f, 1.74f, 1}}, {{0.75f, 0.49f, 4}, {1.55f, 1.46f, 2}, {0.f, 0.f, 0}}};
+    constexpr float JOIN_US = 5.f, PART_BYTES_US = 4e6f;
+    DensePlan best = {DENSE_64, 1, 64};
+    if (n < 1 || groups < 1 || M < 1 || N < 1) return best;
+    float least = INFINITY;
+    const int step = f32 ? 32 : 64, used = groups < n ? groups : n;
+    for (int tile = DENSE_64; tile <= (fast && !f32 ? DENSE_256 : DENSE_128); ++tile) {
+        const DenseCost &c = cost[f32][tile];
+        const float alone = fast ? c.alone : 1.5f * c.alone;
+        const float tiles = static_cast<float>(dense_tiles(M, N, tile));
+        for (int64_t want = 1; want <= 256; want = want < 8 ? want + 1 : want + want / 4) {
+            DensePlan p = {tile, 1, static_cast<int>(dense_parts(dense_parts(n, want), 64) * 64)};
+            p.splits = static_cast<int>(dense_parts(n, p.k_each));
+            if (p.splits > 1 && 8.f * p.splits * M * N > 2e9f) break;  // parts of 2 GB
+            const float rows = n + 0.5f * step * used, work = tiles * rows / step * c.shared / 256, longest = static_cast<float>(p.k_each) / step * alone;
+            float us = work > longest ? work + 0.5f * longest : longest + 0.5f * work;
+            if (p.splits > 1) us += JOIN_US + 8.f * p.splits * M * N / PART_BYTES_US;
+            if (us < least) {
+                least = us;
+                best = p;
+            }
+        }
+    }
+    return best;
+}
 // Parts of a weight gradient: a group of several chunks, so of more than k_each rows, has those from 2 (s / k_each) on.  With q = e / k_each - s / k_each >= 1 it has at
 // most q + 1 <= 2 q chunks, so the next group's are behind them.
 inline int64_t grouped_dw_parts(int n, const DensePlan &p) { return p.k_each < n ? 2ll * (n / p.k_each) : 0; }

@@ -105,6 +105,27 @@ def test_larger(dtype, lens, d_in, d_out):
     assert torch.equal(inplace, narrow) and torch.equal(narrow, wide.to(dtype))
 
 
+@pytest.mark.parametrize("groups", [63, 64, 65, 200, 512, 513, 3000])
+def test_many_groups(groups):
+    """Of no row, of one, and of several tiles, in front of which and behind which there are rows of no group."""
+    lens = [(0, 1, 3, 0, 130)[(i * i + i // 7) % 5] if i % 50 else 300 for i in range(groups)]
+    lens = [x if sum(lens) < 40_000 else min(x, 9) for x in lens]
+    ptr = (np.cumsum([0] + lens) + 3).tolist()
+    n, rows = ptr[-1] + 5, slice(3, ptr[-1])
+    for dtype, d_in, d_out in ((torch.float16, 16, 24), (torch.float32, 9, 8)):
+        X, W, b, _ = layer(n, groups, d_in, d_out, dtype, residual=False)
+        slope = B.slope_like(X.new_empty((n, d_out))).zero_()
+        out = B.ftc_grouped_linear(X, W, offsets(ptr), bias=b, act=B.FTC_ACT_SILU, slope=slope)
+        (z, dz), _, _ = grouped(X, W, ptr, b, "silu", None, dtype)
+        check(f"Z {groups} {dtype}", out[rows], z[rows], dz[rows])
+        dZ = matrix(n, d_out, dtype, 5)
+        dX, dW, db = B.ftc_grouped_linear_backward(X, W, offsets(ptr), dZ, slope=slope)
+        want = grouped_backward(X, W, ptr, dZ, slope, dtype, torch.float32)
+        check(f"dX {groups} {dtype}", dX[rows], want[0][0][rows], want[0][1][rows])
+        check(f"dW {groups} {dtype}", dW, *want[1])
+        check(f"db {groups} {dtype}", db, *want[2])
+
+
 def test_one_group_is_the_dense_layer():
     """The same sums, perhaps in other parts: each is within the bound of the formula, so they are within twice that of each other."""
     for dtype in DTYPES:

@@ -65,8 +65,9 @@ def test_binding_refuses(monkeypatch):
 
 
 def test_numbers_of_groups():
-    """Tiles: those of a group from s // side + g on are as many as it needs before the next group's, and all of them are below n // side + groups.  Parts of a weight
-    gradient: from 2 (s // side) on for groups of more than `side` rows, below 2 (n // side); and each such group has one first multiple of side behind its start."""
+    """Tiles: those of a group from s // side + g on are as many as it needs before the next group's, and all of them are below n // side + groups, which is also what all
+    groups need together.  Parts of a weight gradient: from 2 (s // side) on for groups of more than `side` rows, below 2 (n // side); and each such group has one first
+    multiple of side behind its start."""
     rng = random.Random(5)
     for _ in range(3000):
         side, groups = rng.choice([1, 4, 32, 64, 100]), rng.randrange(1, 30)
@@ -79,19 +80,22 @@ def test_numbers_of_groups():
             if e - s > side:
                 parts += range(2 * (s // side), 2 * (s // side) + need)
             joined += [g for j in range(n // side) for row in [(j + 1) * side] if row < n and s <= row < e and e - s > side and s != row and row - s <= side]
-        assert numbers == sorted(set(numbers)) and numbers[-1] < n // side + groups
+        assert numbers == sorted(set(numbers)) and numbers[-1] < n // side + groups and len(numbers) <= n // side + groups
         assert parts == sorted(set(parts)) and (not parts or parts[-1] < 2 * (n // side))
         assert joined == [g for g, (s, e) in enumerate(zip(ptr, ptr[1:])) if e - s > side]
 
 
-def test_plan(tmp_path):
-    """Every tile and parts of the contraction are taken somewhere, and parts cover the contraction."""
-    code = """#include "grouped_plan.hpp"
+PLAN = """#include "grouped_plan.hpp"
 #include <stdio.h>
 int main(void) { int n, g, N, K, f32, fast; while (scanf("%d %d %d %d %d %d", &n, &g, &N, &K, &f32, &fast) == 6) {
-  ftc::DensePlan p = ftc::grouped_plan(n, g, N, K, f32, fast); printf("%d %d %d\\n", p.tile, p.splits, p.k_each); } }"""
+  ftc::DensePlan p = ftc::grouped_plan(n, g, N, K, f32, fast), w = ftc::grouped_dw_plan(n, g, K, N, f32, fast);
+  printf("%d %d %d %d %d %d %lld\\n", p.tile, p.splits, p.k_each, w.tile, w.splits, w.k_each, (long long)ftc::grouped_dw_parts(n, w)); } }"""
+
+
+def test_plan(tmp_path):
+    """Every tile and parts of the contraction are taken somewhere, and parts cover the contraction."""
     src, exe = tmp_path / "plan.cpp", tmp_path / "plan"
-    src.write_text(code)
+    src.write_text(PLAN)
     subprocess.run(["g++", "-std=c++17", "-O1", "-I" + os.path.join(ROOT, "paper_2412_12218_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     rng = random.Random(3)
     asked = [(rng.choice([1, 7, 24, 300, 5000, 60000]), rng.choice([1, 3, 20, 200]), rng.choice([1, 64, 500, 4096]), rng.choice([1, 64, 100, 777, 4096]), rng.randrange(2),
@@ -99,7 +103,10 @@ int main(void) { int n, g, N, K, f32, fast; while (scanf("%d %d %d %d %d %d", &n
     out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, a)) for a in asked), text=True, capture_output=True, check=True).stdout
     plans = [tuple(map(int, line.split())) for line in out.splitlines()]
     assert len(plans) == len(asked)
-    for (n, g, N, K, f32, fast), (tile, splits, each) in zip(asked, plans):
+    for (n, g, N, K, f32, fast), (tile, splits, each, w_tile, w_splits, w_each, parts) in zip(asked, plans):
         assert 0 <= tile <= 3 and splits >= 1 and each % 64 == 0 and (splits - 1) * each < K <= splits * each
-        assert tile != 2 or (fast and not f32)
+        assert 0 <= w_tile <= 2 and w_each % 64 == 0 and (w_splits - 1) * w_each < n <= w_splits * w_each
+        assert all(t != 2 or (fast and not f32) for t in (tile, w_tile))
+        assert parts == (2 * (n // w_each) if w_each < n else 0) and parts * N * K * 4 <= 2.1e9   # a plan of one part has none
     assert {p[0] for p in plans} == {0, 1, 2, 3} and any(p[1] > 1 for p in plans)
+    assert {p[3] for p in plans} == {0, 1, 2} and any(p[4] > 1 for p in plans) and any(p[4] == 1 for p in plans)
