@@ -285,9 +285,9 @@ __device__ __forceinline__ void dense_tile(int id, int tiles_m, int tiles_n, int
     dense_band(id, tiles_m, tiles_n, m, n);
 }
 
-// The tile (tm, tn) of a product over the indices k_begin .. k_end - 1, with the epilogue, or without it to `part` (M x N).
+// The tile (tm, tn) of a product over the indices k_begin .. k_end - 1, with the epilogue, or without it to `part` (rows part_ld apart, the first that of the product).
 template <class T, bool AX, bool BX, bool FAST, int RW, int CW, int WM, int WN>
-__device__ __forceinline__ void dense_product(const DenseArgs &a, int tm, int tn, int k_begin, int k_end, float *part)
+__device__ __forceinline__ void dense_product(const DenseArgs &a, int tm, int tn, int k_begin, int k_end, float *part, int64_t part_ld)
 {
     constexpr int WAVES = RW * CW, TM = 32 * WM * RW, TN = 32 * WN * CW, STEP = 128 / T::BYTES, KS = STEP / 16;
     typedef Operand<T, TM, STEP, AX, WAVES> OA;
@@ -447,7 +447,7 @@ __device__ __forceinline__ void dense_product(const DenseArgs &a, int tm, int tn
             const ftc_f32x4 u = *reinterpret_cast<const ftc_f32x4 *>(at), v = *reinterpret_cast<const ftc_f32x4 *>(at + 4);
             float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
             if (part) {
-                store_eight_numbers(part, static_cast<int64_t>(row) * a.N + col, FTC_F32, left, x);
+                store_eight_numbers(part, row * part_ld + col, FTC_F32, left, x);
                 continue;
             }
             activate<T>(a, row, col, left, bias, x);
@@ -482,7 +482,7 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void dense_kernel(DenseArgs a)
     dense_tile(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
     const int k_begin = static_cast<int>(blockIdx.y) * a.k_each, k_end = min(a.K, k_begin + a.k_each);
     float *part = a.splits > 1 ? a.part + static_cast<int64_t>(blockIdx.y) * a.M * a.N : nullptr;
-    dense_product<T, AX, BX, FAST, RW, CW, WM, WN>(a, tm, tn, k_begin, k_end, part);
+    dense_product<T, AX, BX, FAST, RW, CW, WM, WN>(a, tm, tn, k_begin, k_end, part, a.N);
 }
 
 template <class T, bool AX, bool BX, bool FAST>

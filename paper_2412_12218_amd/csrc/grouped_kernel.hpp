@@ -98,28 +98,29 @@ __device__ __forceinline__ const void *moved(const void *p, int64_t bytes) { ret
 __device__ __forceinline__ void *moved(void *p, int64_t bytes) { return p ? static_cast<char *>(p) + bytes : nullptr; }
 __device__ __forceinline__ int out_bytes(int dtype) { return dtype == FTC_F32 ? 4 : 2; }
 
-template <class T, bool BX, bool FAST, int RW, int CW, int WM, int WN>
-__global__ __launch_bounds__(64 * RW * CW, 2) void grouped_rows_kernel(GroupedArgs g)
+// Tiles of 256 have a compute unit each, so those behind the last 256 of a launch would take as long as 256 do.  Where these are at most half of 256 their contraction is taken
+// in parts, for as many workgroups as there are units: each writes its part of a tile, and grouped_tail_kernel adds them up.  us of 48 000 rows in 16 groups, 4096 -> 1024 in fp16, 776 tiles:
+// 482 without, 440.
+struct GroupedTail {
+    int full, rest, parts;  // tiles in front, tiles in parts, parts of each
+};
+constexpr int TAIL_PARTS = 8, TAIL_LEAST = 256;  // parts at most, indices of a part at least
+inline __host__ __device__ GroupedTail grouped_tail(int64_t tiles, int K)
 {
-    constexpr int TM = 32 * WM * RW, TN = 32 * WN * CW;
-    DenseArgs a = g.a;
-    const int tiles_n = (a.N + TN - 1) / TN;
-    int tn = 0;
-    // groups of few rows are bound by reading their weights, which no two tiles share: those of a group go round the XCDs
-    const GroupSpan span = group_span<false>(g.group_ptr, g.groups, a.M, TM, [&](int tiles) {
-        int tm = -1;
-        if (TM == 32) {
-            tm = blockIdx.x / tiles_n;
-            tn = blockIdx.x % tiles_n;
-        } else if (blockIdx.x < static_cast<unsigned>(tiles * tiles_n)) {
-            dense_tile(blockIdx.x, tiles, tiles_n, tm, tn);
-        }
-        return tm;
-    });
-    if (span.group < 0) return;
+    const int rest = static_cast<int>(tiles % 256), full = static_cast<int>(tiles - rest);
+    if (full == 0 || rest == 0 || rest > 128) return {static_cast<int>(tiles), 0, 1};
+    const int fill = 256 / rest, most = K / TAIL_LEAST, parts = fill < TAIL_PARTS ? fill : TAIL_PARTS, take = parts < most ? parts : most;
+    if (take < 2) return {static_cast<int>(tiles), 0, 1};
+    return {full, rest, take};
+}
+__device__ __forceinline__ int tail_each(int K, int parts) { return ((K + parts - 1) / parts + 63) / 64 * 64; }
+
+// The product of a group, out of that of all rows.
+template <class T>
+__device__ __forceinline__ DenseArgs of_group(const DenseArgs &all, const GroupSpan &span)
+{
     const int64_t first = span.start;
-    const int k_begin = static_cast<int>(blockIdx.y) * a.k_each, k_end = min(a.K, k_begin + a.k_each);
-    float *part = a.splits > 1 ? a.part + (static_cast<int64_t>(blockIdx.y) * a.M + first) * a.N : nullptr;
+    DenseArgs a = all;
     a.M = span.len;
     a.A = moved(a.A, first * a.lda * T::BYTES);
     a.B = moved(a.B, static_cast<int64_t>(span.group) * a.N * a.K * T::BYTES);
@@ -127,7 +128,81 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void grouped_rows_kernel(GroupedAr
     a.residual = moved(a.residual, first * a.ldr * T::BYTES);
     a.slope = moved(a.slope, first * a.lds * T::BYTES);
     a.out = moved(a.out, first * a.ldo * out_bytes(a.out_dtype));
-    dense_product<T, false, BX, FAST, RW, CW, WM, WN>(a, span.at, tn, k_begin, k_end, part);
+    return a;
+}
+
+template <class T, bool BX, bool FAST, int RW, int CW, int WM, int WN>
+__global__ __launch_bounds__(64 * RW * CW, 2) void grouped_rows_kernel(GroupedArgs g)
+{
+    constexpr int TM = 32 * WM * RW, TN = 32 * WN * CW;
+    const int tiles_n = (g.a.N + TN - 1) / TN;
+    int tn = 0, part_of = -1;  // which of the parts of a tile of the tail
+    GroupedTail tail = {0, 0, 1};
+    // groups of few rows are bound by reading their weights, which no two tiles share: those of a group go round the XCDs
+    const GroupSpan span = group_span<false>(g.group_ptr, g.groups, g.a.M, TM, [&](int tiles) {
+        int tm = -1, id = blockIdx.x;
+        if (TM == 32) {
+            tm = id / tiles_n;
+            tn = id % tiles_n;
+            return tm;
+        }
+        if (TM == 256) {
+            tail = grouped_tail(static_cast<int64_t>(tiles) * tiles_n, g.a.splits > 1 ? 0 : g.a.K);
+            if (id >= tail.full && tail.rest) {
+                part_of = (id - tail.full) % tail.parts;
+                id = tail.full + (id - tail.full) / tail.parts;
+            }
+        }
+        if (id < tiles * tiles_n) dense_tile(id, tiles, tiles_n, tm, tn);
+        return tm;
+    });
+    if (span.group < 0) return;
+    const DenseArgs a = of_group<T>(g.a, span);
+    int k_begin = static_cast<int>(blockIdx.y) * a.k_each, k_end = min(a.K, k_begin + a.k_each);
+    float *part = a.splits > 1 ? a.part + (static_cast<int64_t>(blockIdx.y) * g.a.M + span.start) * a.N : nullptr;
+    int64_t part_ld = a.N;
+    if (TM == 256 && part_of >= 0) {
+        const int each = tail_each(a.K, tail.parts);
+        k_begin = min(part_of * each, a.K);
+        k_end = min(k_begin + each, a.K);
+        // the workgroup's place, as one tile
+        part_ld = TN;
+        part = a.part + static_cast<int64_t>(blockIdx.x - tail.full) * TM * TN - (static_cast<int64_t>(span.at) * TM * TN + static_cast<int64_t>(tn) * TN);
+    }
+    dense_product<T, false, BX, FAST, RW, CW, WM, WN>(a, span.at, tn, k_begin, k_end, part, part_ld);
+}
+
+// The sums of the tail's parts: 32 workgroups a tile, eight columns of a row a thread.
+template <class T>
+__global__ __launch_bounds__(256) void grouped_tail_kernel(GroupedArgs g)
+{
+    constexpr int TM = 256, TN = 256;
+    const int tiles_n = (g.a.N + TN - 1) / TN, which = blockIdx.x / 32;
+    int tn = 0;
+    GroupedTail tail = {0, 0, 1};
+    const GroupSpan span = group_span<false>(g.group_ptr, g.groups, g.a.M, TM, [&](int tiles) {
+        int tm = -1;
+        tail = grouped_tail(static_cast<int64_t>(tiles) * tiles_n, g.a.K);
+        if (which < tail.rest) dense_tile(tail.full + which, tiles, tiles_n, tm, tn);
+        return tm;
+    });
+    if (span.group < 0) return;
+    const DenseArgs a = of_group<T>(g.a, span);
+    const int id = blockIdx.x % 32 * 256 + threadIdx.x, r = id / (TN / 8), c = id % (TN / 8) * 8, row = span.at * TM + r, col = tn * TN + c, left = a.N - col;
+    if (row >= a.M || left <= 0) return;
+    float x[8], bias[8];
+    load_eight_numbers<T>(a.bias, col, a.bias ? left : 0, bias);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = 0.f;
+#pragma unroll
+    for (int p = 0; p < TAIL_PARTS; ++p) {
+        if (p >= tail.parts) break;
+        float v[8];
+        load_eight_numbers<F32>(a.part, (static_cast<int64_t>(which * tail.parts + p) * TM + r) * TN + c, left, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] += v[j];
+    }
+    epilogue<T>(a, row, col, left, bias, x);
 }
 
 // Eight tiles of a chunk (a band's column, dense_band: they share the rows of both operands) are of one XCD, the eights go round the XCDs.
@@ -151,13 +226,14 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void grouped_dw_kernel(GroupedArgs
     a.A = moved(a.A, first * a.lda * T::BYTES);
     a.B = moved(a.B, first * a.ldb * T::BYTES);
     a.out = moved(a.out, static_cast<int64_t>(span.group) * a.M * a.N * out_bytes(a.out_dtype));
-    dense_product<T, true, true, FAST, RW, CW, WM, WN>(a, tm, tn, 0, a.K, part);
+    dense_product<T, true, true, FAST, RW, CW, WM, WN>(a, tm, tn, 0, a.K, part, a.N);
 }
 
 template <class T, bool BX, bool FAST>
 void launch_grouped_rows_t(const GroupedArgs &g, int tile, hipStream_t s)
 {
-    const dim3 grid(static_cast<unsigned>(grouped_most(g.a.M, g.groups, grouped_rows(tile)) * ceil_div(g.a.N, grouped_columns(tile))), g.a.splits);
+    const int64_t most = grouped_most(g.a.M, g.groups, grouped_rows(tile)) * ceil_div(g.a.N, grouped_columns(tile));
+    const dim3 grid(static_cast<unsigned>(most + (tile == DENSE_256 ? 256 : 0)), g.a.splits);  // 256: the tail's parts
     if (tile == DENSE_64) {
         hipLaunchKernelGGL((grouped_rows_kernel<T, BX, FAST, 2, 2, 1, 1>), grid, dim3(256), 0, s, g);
     } else if (tile == DENSE_128) {
@@ -166,6 +242,7 @@ void launch_grouped_rows_t(const GroupedArgs &g, int tile, hipStream_t s)
         hipLaunchKernelGGL((grouped_rows_kernel<T, BX, FAST, 1, 4, 1, 1>), grid, dim3(256), 0, s, g);
     } else if constexpr (FAST && T::BYTES == 2) {
         hipLaunchKernelGGL((grouped_rows_kernel<T, BX, FAST, 2, 4, 4, 2>), grid, dim3(512), 0, s, g);
+        if (g.a.splits == 1 && most > 256 && g.a.K >= 2 * TAIL_LEAST) hipLaunchKernelGGL(grouped_tail_kernel<T>, dim3(128 * 32), dim3(256), 0, s, g);
     }
 }
 

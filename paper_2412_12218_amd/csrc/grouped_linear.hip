@@ -178,12 +178,13 @@ __global__ __launch_bounds__(DB_THREADS) void grouped_db_kernel(int n, const int
 // ---- launches --------------------------------------------------------------------------------------------------
 static size_t rows_ws(int n, int groups, int N, int K)
 {
-    int most = 1;
+    size_t most = 0;
     for (int v = 0; v < 4; ++v) {
         const DensePlan p = grouped_plan(n, groups, N, K, v & 1, v & 2);
-        if (p.splits > most) most = p.splits;
+        const size_t tail = p.tile == DENSE_256 ? 256ull * 256 * 256 : 0, own = p.splits > 1 ? static_cast<size_t>(p.splits) * n * N : tail;
+        if (own > most) most = own;
     }
-    return most > 1 ? align_up(static_cast<size_t>(most) * n * N * sizeof(float), 256) : 0;
+    return align_up(most * sizeof(float), 256);
 }
 static size_t dw_ws(int n, int groups, int M, int N)
 {
@@ -215,7 +216,7 @@ static void add_rows_size(LaunchSize &z, int n, int groups, int N, int K)
 {
     for (int v = 0; v < 4; ++v) {
         const DensePlan p = grouped_plan(n, groups, N, K, v & 1, v & 2);
-        z.add(grouped_most(n, groups, grouped_rows(p.tile)) * dense_parts(N, grouped_columns(p.tile)) * grouped_threads(p.tile), p.splits);
+        z.add(grouped_most(n, groups, grouped_rows(p.tile)) * dense_parts(N, grouped_columns(p.tile)) * grouped_threads(p.tile) + 256 * 512, p.splits);
     }
     z.add(static_cast<int64_t>(n) * ceil_div(N, 8), 1);
 }

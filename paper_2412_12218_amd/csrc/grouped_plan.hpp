@@ -22,7 +22,7 @@ inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fa
 {
     static constexpr DenseCost cost[2][4] = {{{0.45f, 0.22f, 5}, {0.79f, 0.53f, 2}, {1.74f, 1.74f, 1}, {0.45f, 0.22f, 4}},
                                              {{0.75f, 0.49f, 4}, {1.55f, 1.46f, 2}, {0.f, 0.f, 0}, {0.75f, 0.49f, 4}}};
-    constexpr float JOIN_US = 5.f, PART_BYTES_US = 4e6f;
+    constexpr float JOIN_US = 5.f, PART_BYTES_US = 4e6f, TAIL_US = 25.f;  // TAIL_US: the tiles of a last turn in parts (grouped_kernel.hpp)
     DensePlan best = {DENSE_64, 1, 64};
     if (n < 1 || groups < 1 || N < 1 || K < 1) return best;
     float least = INFINITY;
@@ -31,15 +31,17 @@ inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fa
         if (tile == DENSE_256 && (!fast || f32)) continue;
         const DenseCost &c = cost[f32][tile];
         const float alone = fast ? c.alone : 1.5f * c.alone;
-        const int used = groups < n ? groups : n;  // a group's last tile is half full
-        const int64_t tiles = (n / grouped_rows(tile) + (used + 1) / 2) * dense_parts(N, grouped_columns(tile));
+        const int used = groups < n ? groups : n;  // a group's last tile is half full, or less: that of many groups of few rows
+        const int64_t tiles = (n / grouped_rows(tile) + (3 * used + 4) / 5) * dense_parts(N, grouped_columns(tile));
         for (int want = 1; want <= 64; want = want < 8 ? want + 1 : want + want / 4) {
             DensePlan p = {tile, 1, static_cast<int>(dense_parts(dense_parts(K, want), 64) * 64)};
             p.splits = static_cast<int>(dense_parts(K, p.k_each));
             if (p.splits != want) continue;
-            const int64_t blocks = tiles * p.splits, room = 256ll * c.most, full = blocks / room, rest = blocks % room;
-            const auto each = [&](int64_t k) { return k * c.shared > alone ? k * c.shared : alone; };
-            float us = dense_parts(p.k_each, step) * (full * each(c.most) + (rest ? each((rest + 255) / 256) : 0.f));
+            // how many tiles there are is known so well only, so nothing is made of how the last turn is filled
+            const int64_t blocks = tiles * p.splits, share = (blocks + 255) / 256;
+            const float steps = static_cast<float>(dense_parts(p.k_each, step));
+            float us = steps * (share * c.shared > alone ? share * c.shared : alone);
+            if (blocks > 256ll * c.most) us = tile == DENSE_256 && p.splits == 1 ? steps * alone * blocks / 256 + TAIL_US : steps * (c.shared * blocks / 256 + 0.5f * alone);
             if (p.splits > 1) us += JOIN_US + 8.f * p.splits * n * N / PART_BYTES_US;
             if (us < least) {
                 least = us;

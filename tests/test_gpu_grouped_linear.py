@@ -231,3 +231,28 @@ def test_captured_and_on_another_stream():
     graph.replay()
     want = B.ftc_grouped_linear(X, W, offsets(other), bias=b, act=B.FTC_ACT_GELU, slope=B.slope_like(out))
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("lens", [[2600, 0, 1100, 700, 1], [8000, 3], [300] * 16], ids=str)
+def test_last_turn_in_parts(dtype, lens):
+    """More tiles of 256 than compute units, the last ones in parts of the contraction; in both directions, with bias, activation, residual and slopes."""
+    d_in, d_out = 4096, 4104   # 340, 561 and 544 tiles of Z
+    ptr = np.cumsum([0] + lens).tolist()
+    n = ptr[-1]
+    X, W, b, R = layer(n, len(lens), d_in, d_out, dtype)
+    slope = B.slope_like(R[:, :d_out].contiguous())
+    out = B.ftc_grouped_linear(X, W, offsets(ptr), bias=b, act=B.FTC_ACT_SILU, residual=R, slope=slope)
+    dZ = matrix(n, d_out, dtype, 5)
+    dX = B.ftc_grouped_linear_backward(X, W, offsets(ptr), dZ, slope=slope, want_dW=False, want_db=False)[0]
+    again = B.ftc_grouped_linear(X, W, offsets(ptr), bias=b, act=B.FTC_ACT_SILU, residual=R)
+    assert torch.equal(out, again)
+    rows = torch.cat([torch.arange(max(0, p - 5), min(n, p + 5)) for p in ptr] + [torch.arange(n - 40, n), torch.arange(0, n, 97)]).unique()
+    for g, (a, e) in enumerate(zip(ptr, ptr[1:])):
+        at = rows[(rows >= a) & (rows < e)].cuda()
+        if len(at):
+            (z, dz), (s, ds), _ = grouped(X[at], W[g:g + 1], [0, len(at)], b[g:g + 1], "silu", R[at], dtype)
+            check(f"Z {g}", out[at], z, dz)
+            assert np.all(np.abs(slope_values(slope[at]) - s) <= ds)
+            want, bound = grouped_backward(X[at], W[g:g + 1], [0, len(at)], dZ[at], slope[at], dtype, dtype)[0]
+            check(f"dX {g}", dX[at], want, bound)

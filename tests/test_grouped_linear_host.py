@@ -109,4 +109,8 @@ def test_plan(tmp_path):
         assert all(t != 2 or (fast and not f32) for t in (tile, w_tile))
         assert parts == (2 * (n // w_each) if w_each < n else 0) and parts * N * K * 4 <= 2.1e9   # a plan of one part has none
     assert {p[0] for p in plans} == {0, 1, 2, 3} and any(p[1] > 1 for p in plans)
+    # layers whose last tiles come in parts (test_gpu_grouped_linear.py): tiles of 256, between one and 128 more of them than a multiple of 256
+    for n, g, N, K, tiles in ((4401, 5, 4104, 4096, 340), (4401, 5, 4096, 4104, 320), (8003, 2, 4104, 4096, 561), (4800, 16, 4096, 4104, 512)):
+        out = subprocess.run([str(exe)], input=f"{n} {g} {N} {K} 0 1", text=True, capture_output=True, check=True).stdout
+        assert out.split()[:2] == ["2", "1"] and tiles >= 256
     assert {p[3] for p in plans} == {0, 1, 2} and any(p[4] > 1 for p in plans) and any(p[4] == 1 for p in plans)
