@@ -478,7 +478,7 @@ def _here(*tensors):
 
 def _ld(t, rows, cols, dtype=None):
     """Leading dimension of a rows x cols matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (dtype is not None and t.dtype != dtype):
+    if t.shape != (rows, cols) or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"expected {rows} x {cols}" + (f" of {dtype}" if dtype is not None else "") + f", got {tuple(t.shape)} of {t.dtype}")
     st, sc = t.stride()
     if cols > 1 and sc != 1:

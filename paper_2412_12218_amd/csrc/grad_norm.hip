@@ -54,17 +54,17 @@ bool grad_whole(const ftc_grad &g, bool clip) { return g.rows == 1 || (g.ld == g
 
 #if defined(__HIPCC__)
 
-// Which gradient a chunk is of, the last one that begins at or before it (uniform).
+// Which gradient a chunk is of, the last one that begins at or before it (uniform): 64 of them are looked at at once.
 template <class E>
 __device__ __forceinline__ int entry_of(const GradArgs<E> &a, uint32_t c)
 {
-    int lo = 0, hi = a.entries;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.e.first[mid] <= c) lo = mid;
-        else hi = mid;
+    int count = 0;
+#pragma unroll
+    for (int b = 0; b < E::ENTRIES; b += 64) {
+        const int i = b + (threadIdx.x & 63);
+        count += __popcll(__builtin_amdgcn_ballot_w64(i < a.entries && a.e.first[i] <= c));
     }
-    return lo;
+    return count - 1;
 }
 template <class E>
 __device__ __forceinline__ int type_of(const GradArgs<E> &a, int e) { return static_cast<int>(a.e.cols[e] >> GRAD_TYPE_SHIFT); }
@@ -174,19 +174,26 @@ template <class E>
 __global__ __launch_bounds__(GRAD_THREADS) void grad_clip_kernel(GradArgs<E> a, const double *sums, int count, float scale, float max_norm, float *norm)
 {
     __shared__ double area[GRAD_THREADS / 64];
-    const double v = grad_norm_of(sums, count, fabsf(scale), area);
-    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(v);
-    double factor = scale;
-    if (!(v <= max_norm)) factor *= max_norm / v;  // NaN: NaN, for all to see
+    double factor = 0;
+    bool known = false;  // the factor is computed while the first chunk is on its way
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const uint32_t chunk = a.chunks - 1 - c;
         const int e = entry_of(a, chunk);
-        if (factor == 1 && a.e.out[e] == a.e.grad[e]) continue;
+        const bool in_place = a.e.out[e] == a.e.grad[e];
+        if (known && factor == 1 && in_place) continue;
         by_type(type_of(a, e), [&](auto type) {
             typedef decltype(type) T;
             constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
             GradPieces<T> p;
             p.load(a, e, chunk);
+            if (!known) {
+                const double v = grad_norm_of(sums, count, fabsf(scale), area);
+                if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(v);
+                factor = scale;
+                if (!(v <= max_norm)) factor *= max_norm / v;  // NaN: NaN, for all to see
+                known = true;
+                if (factor == 1 && in_place) return;
+            }
 #pragma unroll
             for (int i = 0; i < p.COUNT; ++i) {
                 float x[T::VEC];
