@@ -1,6 +1,8 @@
 // The norms around a block, with its gate and its residual connection, in one pass over the rows:
 //   p = Npost(F),  h = x_scale X + gate p,  u = Npre(h),  N(t) = (t - mean) / sqrt(mean((t - mean)^2) + eps) w + b   (RMS: without the mean).
 // All of a row is in registers (block_norm.hpp); h is normalised before it is rounded.
+#include <algorithm>
+
 #include "block_norm.hpp"
 
 namespace ftc {
@@ -51,14 +53,10 @@ __global__ __launch_bounds__(row_threads(L)) void block_norm_kernel(BlockArgs a,
     for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * GROUPS; row0 < a.n; row0 += step) {
         const bool there = row0 + r.sub < a.n;
         float h[C][8], p[C][8], gate[C][8], m[4] = {0.f, 1.f, 0.f, 1.f};
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            frag_numbers<T>(next_x[c], h[c]);
-            frag_numbers<T>(next_f[c], p[c]);
-        }
+        r.numbers(next_x, h);
+        r.numbers(next_f, p);
         if (BLOCK && a.ldg) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) frag_numbers<T>(next_gate[c], gate[c]);
+            r.numbers(next_gate, gate);
         } else {
 #pragma unroll
             for (int c = 0; c < C; ++c)
@@ -100,36 +98,44 @@ template <class T, int L, int C, bool BLOCK>
 static void forward_t(const BlockArgs &a, void *H, int ldh, void *U, int ldu, float *stats, hipStream_t s)
 {
     const dim3 grid(row_groups(a.n, L, BLOCK ? 1024 : 2048)), threads(row_threads(L));
-    const bool whole = whole_rows<T>(a.d, a.ldx) && whole_rows<T>(a.d, a.ldf) && whole_rows<T>(a.d, a.ldg) && whole_rows<T>(a.d, ldh) && whole_rows<T>(a.d, ldu);
-    const int arrays = 1 + (a.F != nullptr) + (a.ldg != 0) + (H != nullptr) + (U != nullptr);
-    if (whole && row_stream(static_cast<int64_t>(a.n) * a.d * T::BYTES * arrays))
-        hipLaunchKernelGGL((block_norm_kernel<T, L, C, BLOCK, true, true>), grid, threads, 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
-    else if (whole)
-        hipLaunchKernelGGL((block_norm_kernel<T, L, C, BLOCK, true, false>), grid, threads, 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
-    else
-        hipLaunchKernelGGL((block_norm_kernel<T, L, C, BLOCK, false, false>), grid, threads, 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats);
+    const bool whole = a.d % T::VEC == 0, nt = row_stream(a.n, a.d, T::BYTES, {a.X, a.F, a.ldg ? a.gate : nullptr, H, U});
+#define FTC_GO(WHOLE, NT) \
+    hipLaunchKernelGGL((block_norm_kernel<T, L, C, BLOCK, WHOLE, NT>), grid, threads, 0, s, a, H, static_cast<int64_t>(ldh), U, static_cast<int64_t>(ldu), stats)
+    if (whole && nt) FTC_GO(true, true);
+    else if (whole) FTC_GO(true, false);
+    else if (nt) FTC_GO(false, true);
+    else FTC_GO(false, false);
+#undef FTC_GO
 }
 
 int32_t launch_block_norm(const ftc_block &b, void *H, int ldh, void *U, int ldu, float *stats, hipStream_t s)
 {
     const BlockArgs a = {b.n, b.d, b.F ? b.post : FTC_NORM_NONE, b.pre, b.eps, b.x_scale, b.X, b.F, b.gate, b.post_w, b.post_b, b.pre_w, b.pre_b, b.ldx, b.ldf, b.ldg};
+    const int64_t lds[5] = {b.ldx, b.ldf, b.ldg, ldh, ldu};
+    const int lanes = row_lanes(b.d, *std::max_element(lds, lds + 5), elem_size(b.dtype));
 #define FTC_ROWS(T, L, C)                                                     \
     do {                                                                      \
         if (a.F) forward_t<T, L, C, true>(a, H, ldh, U, ldu, stats, s);       \
         else forward_t<T, L, C, false>(a, H, ldh, U, ldu, stats, s);          \
     } while (0)
-#define FTC_WIDTHS(T)                                \
-    do {                                             \
-        if (b.d <= 32) FTC_ROWS(T, 4, 1);            \
-        else if (b.d <= 64) FTC_ROWS(T, 8, 1);       \
-        else if (b.d <= 128) FTC_ROWS(T, 16, 1);     \
-        else if (b.d <= 256) FTC_ROWS(T, 32, 1);     \
-        else if (b.d <= 512) FTC_ROWS(T, 64, 1);     \
-        else if (b.d <= 1024) FTC_ROWS(T, 128, 1);   \
-        else if (b.d <= 2048) FTC_ROWS(T, 256, 1);   \
-        else if (b.d <= 4096) FTC_ROWS(T, 512, 1);   \
-        else if (b.d <= 8192) FTC_ROWS(T, 512, 2);   \
-        else FTC_ROWS(T, 1024, 2);                   \
+#define FTC_WIDTHS(T)                                                     \
+    do {                                                                  \
+        switch (lanes) {                                                  \
+        case 4: FTC_ROWS(T, 4, 1); break;                                 \
+        case 8: FTC_ROWS(T, 8, 1); break;                                 \
+        case 16: FTC_ROWS(T, 16, 1); break;                               \
+        case 32: FTC_ROWS(T, 32, 1); break;                               \
+        case 64: FTC_ROWS(T, 64, 1); break;                               \
+        case 128: FTC_ROWS(T, 128, 1); break;                             \
+        case 192: FTC_ROWS(T, 192, 1); break;                             \
+        case 256: FTC_ROWS(T, 256, 1); break;                             \
+        case 384: FTC_ROWS(T, 384, 1); break;                             \
+        case 512:                                                         \
+            if (b.d <= 4096) FTC_ROWS(T, 512, 1);                         \
+            else FTC_ROWS(T, 512, 2);                                     \
+            break;                                                        \
+        default: FTC_ROWS(T, 1024, 2);                                    \
+        }                                                                 \
     } while (0)
     if (b.dtype == FTC_F32) FTC_WIDTHS(F32);
     else if (b.dtype == FTC_F16) FTC_WIDTHS(F16);

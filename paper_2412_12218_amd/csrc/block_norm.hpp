@@ -3,10 +3,21 @@
 // A row is in the registers of L lanes, C pieces of eight numbers each, lane l having the pieces l, l + L, ...; it is read once whatever is computed
 // of it.  Up to 64 lanes are lanes of one wave and their sums stay in registers; more are waves of one workgroup, whose sums meet in LDS.
 #pragma once
+#include <initializer_list>
+
 #include "stream_piece.hpp"
 
 namespace ftc {
 
+// Lanes of a row: as many as make it one piece each, up to 512, and two from there on.  Rows of a workgroup that are 2^31 bytes apart have 64 lanes at least.
+constexpr int ROW_LANES[] = {4, 8, 16, 32, 64, 128, 192, 256, 384, 512};
+inline int row_lanes(int d, int64_t widest_ld, int bytes)
+{
+    const int least = 64 * widest_ld * bytes < (1ll << 31) ? 4 : 64;
+    for (int lanes : ROW_LANES)
+        if (lanes >= least && d <= (lanes == 512 ? 16 : 8) * lanes) return lanes;
+    return 1024;
+}
 constexpr int row_threads(int lanes) { return lanes > 64 ? lanes : 256; }  // of a workgroup
 
 // Workgroups of a launch: at most as many as the compute units hold at once, and as many turns for each of them.
@@ -15,10 +26,15 @@ inline int row_groups(int n, int lanes, int threads_a_unit)
     const int threads = row_threads(lanes), groups = ceil_div(n, threads / lanes), most = 256 * (threads_a_unit / threads > 0 ? threads_a_unit / threads : 1);
     return groups <= most ? groups : ceil_div(groups, ceil_div(groups, most));
 }
-// Whether a pass over so many bytes takes the non-temporal hint (stream_piece.hpp): more than a third of the last-level cache of 256 MB, of which the kernels before and behind have
-// theirs.  us with / without: 74 MB (46 000 x 200 in fp32, normed) 14.9 / 13.1; 123 MB (20 000 x 768 in bf16, a block's join) 32 / 42, its gradients (184 MB) 46 / 54; 256 MB (200 000 x 128) 47 / 50;
-// 410 MB (50 000 x 1024) 75 / 80.
-inline bool row_stream(int64_t bytes) { return bytes > 85ll << 20; }
+// Whether a pass over these matrices (NULL: not there) takes the non-temporal hint (stream_piece.hpp): more than a third of the last-level cache of 256 MB, of which the kernels
+// before and behind have theirs.  us with / without: 74 MB (46 000 x 200 in fp32, normed) 14.9 / 13.1; 123 MB (20 000 x 768 in bf16, a block's join) 32 / 42, its gradients (184 MB) 46 / 54;
+// 256 MB (200 000 x 128) 47 / 50; 410 MB (50 000 x 1024) 75 / 80.
+inline bool row_stream(int n, int d, int bytes, std::initializer_list<const void *> matrices)
+{
+    int64_t all = 0;
+    for (const void *p : matrices) all += p ? static_cast<int64_t>(n) * d * bytes : 0;
+    return all > 85ll << 20;
+}
 
 struct BlockArgs {
     int n, d, post, pre;
@@ -59,18 +75,19 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float *area, int &turn)
 }
 
 // A lane's C pieces of rows of d numbers.  Loads and stores are of 16 bytes, those of neighbouring lanes beside each other: in fp32 a piece is two of
-// them, 4 L numbers apart.  WHOLE: rows are whole 16 bytes, which are there or not, and the rows of a workgroup lie within 2^31 bytes, so that what a lane adds to the
-// address of the workgroup's first row is 32 bits and the same for every turn.
+// them, 4 L numbers apart.  What a lane adds to the address of the workgroup's first row (of its own row, from 64 lanes on) is 32 bits and the same for every turn.
+// WHOLE: rows are whole 16 bytes, which are there or not; else the last ones of a row are loaded as the row's last 16 bytes, and moved.
 template <class T, int L, int C, bool WHOLE, bool NT>
 struct RowPieces {
     static constexpr int V = T::VEC, UNITS = 8 / V, DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
-    int d, lane, sub;  // sub: which of the workgroup's rows
+    int d, lane, sub;  // sub: which of the workgroup's rows (uniform from 64 lanes on)
     __device__ __forceinline__ int col(int c, int u) const { return V * ((c * UNITS + u) * L + lane); }
     __device__ __forceinline__ bool has(int c, int j) const { return WHOLE ? col(c, j / V) < d : col(c, j / V) + j % V < d; }
-    __device__ __forceinline__ int64_t at(int64_t row0, int64_t ld, int c, int u) const { return (row0 + sub) * ld + col(c, u); }
-    __device__ __forceinline__ int64_t byte(int64_t row0, int64_t ld, int c, int u) const
+    // of the number `col` of this lane's row
+    __device__ __forceinline__ int64_t byte(int64_t row0, int64_t ld, int col) const
     {
-        return row0 * ld * T::BYTES + (static_cast<uint32_t>(sub) * static_cast<uint32_t>(ld) + static_cast<uint32_t>(col(c, u))) * static_cast<uint32_t>(T::BYTES);
+        if constexpr (L >= 64) return (row0 + sub) * ld * T::BYTES + static_cast<uint32_t>(col * T::BYTES);
+        else return row0 * ld * T::BYTES + (static_cast<uint32_t>(sub) * static_cast<uint32_t>(ld) + static_cast<uint32_t>(col)) * static_cast<uint32_t>(T::BYTES);
     }
     static __device__ __forceinline__ ftc_u32x4 whole_piece(const void *base, int64_t at) { return NT ? load_piece_nt<T>(base, at) : load_piece<T>(base, at, V); }
     static __device__ __forceinline__ void store_whole(void *base, int64_t at, const float (&y)[V])
@@ -97,34 +114,59 @@ struct RowPieces {
     // What this lane has of a row of the workgroup's, row0 the first of them; there: whether there is this lane's.  What is not there keeps what it was.
     __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row0, bool there, Frag<T> (&f)[C]) const
     {
+        const char *p = static_cast<const char *>(base);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                const int left = there ? d - col(c, u) : 0;
-                if (WHOLE ? left > 0 : left >= V) put(f[c], u, whole_piece(WHOLE ? static_cast<const char *>(base) + byte(row0, ld, c, u) : base, WHOLE ? 0 : at(row0, ld, c, u)));
-                else if (!WHOLE && left > 0) put(f[c], u, load_piece<T>(base, at(row0, ld, c, u), left));
+                const int at = col(c, u);
+                if (!there || at >= d) continue;
+                ftc_u32x4 w;
+                if (WHOLE || d >= V) w = whole_piece(p + byte(row0, ld, WHOLE ? at : min(at, d - V)), 0);
+                else w = load_piece<T>(p + byte(row0, ld, at), 0, d);
+                put(f[c], u, w);
             }
+    }
+    // The numbers of what load() brought; the last ones of a row go to their places here, not where the load would have to be waited for.
+    __device__ __forceinline__ void numbers(const Frag<T> (&f)[C], float (&x)[C][8]) const
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            Frag<T> v = f[c];
+            if constexpr (!WHOLE) {
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) {
+                    const int at = col(c, u);
+                    if (d < V || at >= d || at + V <= d) continue;
+                    ftc_u32x4 w;
+                    if constexpr (T::BYTES == 4) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(v.f[4 * u + j]);
+                    } else {
+                        w = v.w;
+                    }
+                    move_down<T>(w, at + V - d);
+                    put(v, u, w);
+                }
+            }
+            frag_numbers<T>(v, x[c]);
+        }
     }
     __device__ __forceinline__ void store(void *base, int64_t ld, int64_t row0, bool there, const float (&x)[C][8]) const
     {
+        char *p = static_cast<char *>(base);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                const int left = there ? d - col(c, u) : 0;
+                const int at = col(c, u), left = d - at;
+                if (!there || left <= 0) continue;
+                char *to = p + byte(row0, ld, at);
                 float y[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) y[j] = x[c][u * V + j];
-                if constexpr (WHOLE) {
-                    if (left > 0) store_whole(static_cast<char *>(base) + byte(row0, ld, c, u), 0, y);
-                } else if (left >= V) {
-                    store_whole(base, at(row0, ld, c, u), y);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V - 1; ++j)
-                        if (j < left) store_elem(base, at(row0, ld, c, u) + j, DT, y[j]);
-                }
+                if (WHOLE || left >= V) store_whole(to, 0, y);
+                else store_first<T>(to, left, y);
             }
     }
     // A vector of d numbers; all vectors are loaded before the first is looked at.  NULL: `none` each
@@ -146,9 +188,6 @@ struct RowPieces {
     }
 };
 
-// Whether rows at `ld` can be taken as WHOLE.
-template <class T>
-inline bool whole_rows(int d, int64_t ld) { return d % T::VEC == 0 && 64 * ld * T::BYTES < (1ll << 31); }
 
 // Mean (0 for FTC_NORM_RMS) of a row and what its distance from there is multiplied by.  The squares are those of the distances, from registers, so
 // a mean that is large beside the spread costs nothing.  Distances from 1e19 on, whose squares are infinite in fp32, once more times 2^-96.

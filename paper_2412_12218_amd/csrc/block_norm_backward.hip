@@ -4,6 +4,8 @@
 //   N'(g) = rstd (g w - mean(g w xh) xh - mean(g w)),  dw = sum over the rows of g xh,  db = sum of g   (RMS: without the mean of g w).
 // A workgroup keeps the sums over its rows in registers, adds them up over its row groups and writes one row of each; a second kernel adds
 // these in order.
+#include <algorithm>
+
 #include "block_norm.hpp"
 
 namespace ftc {
@@ -20,9 +22,10 @@ struct BlockGradArgs {
 
 // BLOCK: with F
 template <class T, int L, int C, bool BLOCK, bool WHOLE, bool NT>
-__global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(BlockArgs a, BlockGradArgs g)
+__global__ __launch_bounds__(row_threads(L), 2) void block_norm_backward_kernel(BlockArgs a, BlockGradArgs g)
 {
     constexpr int THREADS = row_threads(L), GROUPS = THREADS / L;
+    constexpr bool LEAN = C > 1;  // registers: no rows ahead, weights out of the caches for every row
     __shared__ float area[64];
     __shared__ __align__(16) float joined[GROUPS > 1 ? THREADS * C * 8 : 1];
     int turn = 0;
@@ -82,39 +85,52 @@ __global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(Blo
         if (BLOCK && a.ldg) r.load(a.gate, a.ldg, row0, there, next_gate);
         if (there && g.stats) next_m = *reinterpret_cast<const ftc_f32x4 *>(g.stats + 4 * (row0 + sub));
     };
-    fetch(static_cast<int64_t>(blockIdx.x) * GROUPS);
-    Frag<T> raw_post_w[C], raw_post_b[C], raw_pre_w[C], raw_gate[C];
-    r.fetch(a.post_w, raw_post_w);
-    r.fetch(a.post_b, raw_post_b);
-    r.fetch(a.pre_w, raw_pre_w);
-    r.fetch(a.ldg ? nullptr : a.gate, raw_gate);
-    r.vector(a.post_w, raw_post_w, 1.f, post_w);
-    r.vector(a.post_b, raw_post_b, 0.f, post_b);
-    r.vector(a.pre_w, raw_pre_w, 1.f, pre_w);
-    r.vector(a.ldg ? nullptr : a.gate, raw_gate, 1.f, one_gate);
+    if constexpr (!LEAN) fetch(static_cast<int64_t>(blockIdx.x) * GROUPS);
+    auto weights = [&] {
+        Frag<T> raw_post_w[C], raw_post_b[C], raw_pre_w[C], raw_gate[C];
+        r.fetch(a.post_w, raw_post_w);
+        r.fetch(a.post_b, raw_post_b);
+        r.fetch(a.pre_w, raw_pre_w);
+        r.fetch(a.ldg ? nullptr : a.gate, raw_gate);
+        r.vector(a.post_w, raw_post_w, 1.f, post_w);
+        r.vector(a.post_b, raw_post_b, 0.f, post_b);
+        r.vector(a.pre_w, raw_pre_w, 1.f, pre_w);
+        r.vector(a.ldg ? nullptr : a.gate, raw_gate, 1.f, one_gate);
+    };
+    if constexpr (!LEAN) weights();
+    // LEAN: one of them, where it is used
+    auto weight = [&](const void *base, float none, float (&x)[C][8]) {
+        if constexpr (LEAN) {
+            asm volatile("" ::: "memory");  // not before the loop
+            Frag<T> raw[C];
+            r.fetch(base, raw);
+            r.vector(base, raw, none, x);
+        }
+    };
     for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * GROUPS; row0 < a.n; row0 += step) {
         const bool there = row0 + sub < a.n;
+        if constexpr (LEAN) fetch(row0);
         const ftc_f32x4 m = next_m;
         float fh[C][8], p[C][8], hh[C][8], gr[C][8], gate[C][8];
         Frag<T> dh[C];
+        r.numbers(next_x, hh);
+        r.numbers(next_f, fh);
+        r.numbers(next_du, gr);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            frag_numbers<T>(next_x[c], hh[c]);
-            frag_numbers<T>(next_f[c], fh[c]);
-            frag_numbers<T>(next_du[c], gr[c]);
-            dh[c] = next_dh[c];
-        }
+        for (int c = 0; c < C; ++c) dh[c] = next_dh[c];
         if (BLOCK && a.ldg) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) frag_numbers<T>(next_gate[c], gate[c]);
+            r.numbers(next_gate, gate);
         } else {
+            weight(a.gate, 1.f, one_gate);
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) gate[c][j] = one_gate[c][j];
         }
-        if (row0 + step < a.n) fetch(row0 + step);
+        if (!LEAN && row0 + step < a.n) fetch(row0 + step);
         if (BLOCK && a.post != FTC_NORM_NONE) {
+            weight(a.post_w, 1.f, post_w);
+            weight(a.post_b, 0.f, post_b);
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -145,14 +161,16 @@ __global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(Blo
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) hh[c][j] = (hh[c][j] - m[2]) * (r.has(c, j) ? m[3] : 0.f);
+            weight(a.pre_w, 1.f, pre_w);
             back(a.pre, hh, m[3], pre_w, sum[SUM_PRE_W], sum[SUM_PRE_B], gr);
         }
+        {
+            float v[C][8];
+            r.numbers(dh, v);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            float v[8];
-            frag_numbers<T>(dh[c], v);
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) gr[c][j] += v[j];  // dh now
+                for (int j = 0; j < 8; ++j) gr[c][j] += v[c][j];  // dh now
         }
         if (g.dX) {
             float v[C][8];
@@ -174,7 +192,10 @@ __global__ __launch_bounds__(row_threads(L)) void block_norm_backward_kernel(Blo
                 }
             if (g.dgate) r.store(g.dgate, g.lddg, row0, there, p);
         }
-        if (a.post != FTC_NORM_NONE) back(a.post, fh, m[1], post_w, sum[SUM_POST_W], sum[SUM_POST_B], gr);
+        if (a.post != FTC_NORM_NONE) {
+            weight(a.post_w, 1.f, post_w);
+            back(a.post, fh, m[1], post_w, sum[SUM_POST_W], sum[SUM_POST_B], gr);
+        }
         if (g.dF) r.store(g.dF, g.lddf, row0, there, gr);
     }
 #pragma unroll
@@ -242,33 +263,26 @@ __global__ __launch_bounds__(SUM_THREADS) void block_norm_sums_kernel(int parts,
     }
 }
 
-static int lanes_of(int d)
-{
-    int lanes = 4;
-    while (lanes < 512 && lanes * 8 < d) lanes *= 2;
-    return d > 8192 ? 1024 : lanes;
-}
-
 // Workgroups of a launch, which are the rows of the sums' parts.
-static int backward_groups(int n, int d) { return row_groups(n, lanes_of(d), 512); }
+static int backward_groups(int n, int lanes) { return row_groups(n, lanes, 512); }
 
 size_t block_norm_backward_ws(int n, int d)
 {
-    return align_up(static_cast<size_t>(SUMS) * backward_groups(n, d) * d * sizeof(float), 256);
+    // narrow rows far apart have 64 lanes
+    const int near = backward_groups(n, row_lanes(d, d, 4)), far = backward_groups(n, row_lanes(d, INT32_MAX, 4));
+    return align_up(static_cast<size_t>(SUMS) * (near > far ? near : far) * d * sizeof(float), 256);
 }
 
 template <class T, int L, int C, bool BLOCK>
 static void backward_t(const BlockArgs &a, const BlockGradArgs &g, int groups, hipStream_t s)
 {
-    const int64_t lds[8] = {a.ldx, a.ldf, a.ldg, g.lddh, g.lddu, g.lddx, g.lddf, g.lddg};
-    const void *const arrays[8] = {a.X, a.F, a.ldg ? a.gate : nullptr, g.dH, g.dU, g.dX, g.dF, g.dgate};
-    bool whole = true;
-    int64_t bytes = 0;
-    for (int64_t ld : lds) whole = whole && whole_rows<T>(a.d, ld);
-    for (const void *p : arrays) bytes += p ? static_cast<int64_t>(a.n) * a.d * T::BYTES : 0;
-    if (whole && row_stream(bytes)) hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, BLOCK, true, true>), dim3(groups), dim3(row_threads(L)), 0, s, a, g);
-    else if (whole) hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, BLOCK, true, false>), dim3(groups), dim3(row_threads(L)), 0, s, a, g);
-    else hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, BLOCK, false, false>), dim3(groups), dim3(row_threads(L)), 0, s, a, g);
+    const bool whole = a.d % T::VEC == 0, nt = row_stream(a.n, a.d, T::BYTES, {a.X, a.F, a.ldg ? a.gate : nullptr, g.dH, g.dU, g.dX, g.dF, g.dgate});
+#define FTC_GO(WHOLE, NT) hipLaunchKernelGGL((block_norm_backward_kernel<T, L, C, BLOCK, WHOLE, NT>), dim3(groups), dim3(row_threads(L)), 0, s, a, g)
+    if (whole && nt) FTC_GO(true, true);
+    else if (whole) FTC_GO(true, false);
+    else if (nt) FTC_GO(false, true);
+    else FTC_GO(false, false);
+#undef FTC_GO
 }
 
 int32_t launch_block_norm_backward(const ftc_block &b, const float *stats, const void *dH, int lddh, const void *dU, int lddu,
@@ -276,7 +290,8 @@ int32_t launch_block_norm_backward(const ftc_block &b, const float *stats, const
 {
     const BlockArgs a = {b.n, b.d, b.F ? b.post : FTC_NORM_NONE, b.pre, b.eps, b.x_scale, b.X, b.F, b.gate, b.post_w, b.post_b, b.pre_w, b.pre_b, b.ldx, b.ldf, b.ldg};
     const bool rows = b.gate && b.ldg != 0;
-    const int groups = backward_groups(b.n, b.d);
+    const int64_t lds[8] = {b.ldx, b.ldf, b.ldg, lddh, lddu, g.lddx, g.lddf, g.lddg};
+    const int lanes = row_lanes(b.d, *std::max_element(lds, lds + 8), elem_size(b.dtype)), groups = backward_groups(b.n, lanes);
     BlockGradArgs k = {stats, dH, dU, g.dX, g.dF, rows ? g.dgate : nullptr, lddh, lddu, g.lddx, g.lddf, g.lddg, {}};
     BlockSums sums = {};
     void *const outs[SUMS] = {rows ? nullptr : g.dgate, g.dpost_w, g.dpost_b, g.dpre_w, g.dpre_b};
@@ -293,18 +308,24 @@ int32_t launch_block_norm_backward(const ftc_block &b, const float *stats, const
         if (a.F) backward_t<T, L, C, true>(a, k, groups, s);    \
         else backward_t<T, L, C, false>(a, k, groups, s);       \
     } while (0)
-#define FTC_WIDTHS(T)                                \
-    do {                                             \
-        if (b.d <= 32) FTC_ROWS(T, 4, 1);            \
-        else if (b.d <= 64) FTC_ROWS(T, 8, 1);       \
-        else if (b.d <= 128) FTC_ROWS(T, 16, 1);     \
-        else if (b.d <= 256) FTC_ROWS(T, 32, 1);     \
-        else if (b.d <= 512) FTC_ROWS(T, 64, 1);     \
-        else if (b.d <= 1024) FTC_ROWS(T, 128, 1);   \
-        else if (b.d <= 2048) FTC_ROWS(T, 256, 1);   \
-        else if (b.d <= 4096) FTC_ROWS(T, 512, 1);   \
-        else if (b.d <= 8192) FTC_ROWS(T, 512, 2);   \
-        else FTC_ROWS(T, 1024, 2);                   \
+#define FTC_WIDTHS(T)                                                     \
+    do {                                                                  \
+        switch (lanes) {                                                  \
+        case 4: FTC_ROWS(T, 4, 1); break;                                 \
+        case 8: FTC_ROWS(T, 8, 1); break;                                 \
+        case 16: FTC_ROWS(T, 16, 1); break;                               \
+        case 32: FTC_ROWS(T, 32, 1); break;                               \
+        case 64: FTC_ROWS(T, 64, 1); break;                               \
+        case 128: FTC_ROWS(T, 128, 1); break;                             \
+        case 192: FTC_ROWS(T, 192, 1); break;                             \
+        case 256: FTC_ROWS(T, 256, 1); break;                             \
+        case 384: FTC_ROWS(T, 384, 1); break;                             \
+        case 512:                                                         \
+            if (b.d <= 4096) FTC_ROWS(T, 512, 1);                         \
+            else FTC_ROWS(T, 512, 2);                                     \
+            break;                                                        \
+        default: FTC_ROWS(T, 1024, 2);                                    \
+        }                                                                 \
     } while (0)
         if (b.dtype == FTC_F32) FTC_WIDTHS(F32);
         else if (b.dtype == FTC_F16) FTC_WIDTHS(F16);

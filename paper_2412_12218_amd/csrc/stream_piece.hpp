@@ -29,5 +29,39 @@ __device__ __forceinline__ void store_piece_nt(void *base, int64_t idx, const fl
     }
 }
 
+// The first `left` numbers of a piece, fewer than it has, in at most three stores.
+template <class T>
+__device__ __forceinline__ void store_first(void *base, int left, const float (&x)[T::VEC])
+{
+    if constexpr (T::BYTES == 4) {
+        float *p = static_cast<float *>(base);
+        typedef float f2 __attribute__((ext_vector_type(2), aligned(4)));
+        float last = x[0];
+        if (left & 2) {
+            *reinterpret_cast<f2 *>(p) = f2{x[0], x[1]};
+            last = x[2];
+            p += 2;
+        }
+        if (left & 1) *p = last;
+    } else {
+        typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+        typedef uint32_t u1 __attribute__((aligned(2)));
+        uint16_t *p = static_cast<uint16_t *>(base);
+        ftc_u32x4 w = frag_of<T>(x).w;
+        if (left & 4) {
+            *reinterpret_cast<u2 *>(p) = u2{w[0], w[1]};
+            w[0] = w[2];
+            w[1] = w[3];
+            p += 4;
+        }
+        if (left & 2) {
+            *reinterpret_cast<u1 *>(p) = w[0];
+            w[0] = w[1];
+            p += 2;
+        }
+        if (left & 1) *p = static_cast<uint16_t>(w[0]);
+    }
+}
+
 #endif  // __HIPCC__
 }  // namespace ftc
