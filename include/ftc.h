@@ -521,9 +521,9 @@ typedef struct {
 } ftc_grad;
 
 size_t ftc_grad_norm_workspace_bytes(int32_t count);
-int32_t ftc_grad_norm(const ftc_grad *grads, int32_t count, float scale, float *norm, void *ws, size_t ws_bytes,
+int32_t ftc_grad_norm(const ftc_grad *grads, int32_t count, double scale, float *norm, void *ws, size_t ws_bytes,
                       void *stream);
-int32_t ftc_clip_grad_norm(const ftc_grad *grads, int32_t count, float max_norm, float scale, float *norm, void *ws,
+int32_t ftc_clip_grad_norm(const ftc_grad *grads, int32_t count, double max_norm, double scale, float *norm, void *ws,
                            size_t ws_bytes, void *stream);
 
 /*

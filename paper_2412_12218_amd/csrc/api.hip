@@ -1009,7 +1009,7 @@ int32_t ftc_grouped_linear_backward(int32_t n, const int32_t *group_ptr, int32_t
 
 // ---- the norm over all gradients
 static constexpr int32_t GRAD_MOST = 1 << 20;  // gradients of a call
-static int32_t check_grads(const char *who, const ftc_grad *grads, int32_t count, float scale, const float *norm, bool out)
+static int32_t check_grads(const char *who, const ftc_grad *grads, int32_t count, double scale, const float *norm, bool out)
 {
     if (count < 0) return fail(FTC_EINVAL, "%s: negative count", who);
     if (count > 0 && !grads) return fail(FTC_EINVAL, "%s: grads is NULL", who);
@@ -1038,7 +1038,7 @@ static int32_t check_grads(const char *who, const ftc_grad *grads, int32_t count
 
 size_t ftc_grad_norm_workspace_bytes(int32_t count) { return count < 0 || count > GRAD_MOST ? 0 : grad_norm_ws(count); }
 
-int32_t ftc_grad_norm(const ftc_grad *grads, int32_t count, float scale, float *norm, void *ws, size_t ws_bytes, void *stream)
+int32_t ftc_grad_norm(const ftc_grad *grads, int32_t count, double scale, float *norm, void *ws, size_t ws_bytes, void *stream)
 {
     const char *who = "ftc_grad_norm";
     FTC_TRY(check_grads(who, grads, count, scale, norm, false));
@@ -1046,11 +1046,11 @@ int32_t ftc_grad_norm(const ftc_grad *grads, int32_t count, float scale, float *
     return launch_grad_norm(grads, count, scale, norm, ws, static_cast<hipStream_t>(stream));
 }
 
-int32_t ftc_clip_grad_norm(const ftc_grad *grads, int32_t count, float max_norm, float scale, float *norm, void *ws, size_t ws_bytes, void *stream)
+int32_t ftc_clip_grad_norm(const ftc_grad *grads, int32_t count, double max_norm, double scale, float *norm, void *ws, size_t ws_bytes, void *stream)
 {
     const char *who = "ftc_clip_grad_norm";
     FTC_TRY(check_grads(who, grads, count, scale, norm, true));
-    if (!(max_norm >= 0.f)) return fail(FTC_EINVAL, "%s: max_norm is negative or NaN", who);
+    if (!(max_norm >= 0)) return fail(FTC_EINVAL, "%s: max_norm is negative or NaN", who);
     FTC_TRY(check_ws(who, grad_norm_ws(count), ws, ws_bytes));
     return launch_clip_grad_norm(grads, count, max_norm, scale, norm, ws, static_cast<hipStream_t>(stream));
 }

@@ -220,8 +220,8 @@ int32_t launch_linear_backward(const LinearShape &p, const LinearGrads &g, void 
 // grad_norm.hip
 bool grad_whole(const ftc_grad &g, bool clip);
 size_t grad_norm_ws(int count);
-int32_t launch_grad_norm(const ftc_grad *grads, int count, float scale, float *norm, void *ws, hipStream_t s);
-int32_t launch_clip_grad_norm(const ftc_grad *grads, int count, float max_norm, float scale, float *norm, void *ws, hipStream_t s);
+int32_t launch_grad_norm(const ftc_grad *grads, int count, double scale, float *norm, void *ws, hipStream_t s);
+int32_t launch_clip_grad_norm(const ftc_grad *grads, int count, double max_norm, double scale, float *norm, void *ws, hipStream_t s);
 // grouped_linear.hip
 LaunchSize grouped_linear_size(int n, int groups, int d_in, int d_out);
 LaunchSize grouped_linear_backward_size(int n, int groups, int d_in, int d_out);

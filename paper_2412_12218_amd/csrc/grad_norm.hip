@@ -162,16 +162,16 @@ __device__ __forceinline__ double grad_norm_of(const double *sums, int count, do
     return sqrt(group_total(s, area)) * scale;
 }
 
-__global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(const double *sums, int count, float scale, float *norm)
+__global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(const double *sums, int count, double scale, float *norm)
 {
     __shared__ double area[GRAD_THREADS / 64];
-    const double v = grad_norm_of(sums, count, fabsf(scale), area);
+    const double v = grad_norm_of(sums, count, fabs(scale), area);
     if (threadIdx.x == 0) *norm = static_cast<float>(v);
 }
 
 // From the last chunk to the first: what was read last for the norm is in cache still.
 template <class E>
-__global__ __launch_bounds__(GRAD_THREADS) void grad_clip_kernel(GradArgs<E> a, const double *sums, int count, float scale, float max_norm, float *norm)
+__global__ __launch_bounds__(GRAD_THREADS) void grad_clip_kernel(GradArgs<E> a, const double *sums, int count, double scale, double max_norm, float *norm)
 {
     __shared__ double area[GRAD_THREADS / 64];
     double factor = 0;
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_clip_kernel(GradArgs<E> a, 
             GradPieces<T> p;
             p.load(a, e, chunk);
             if (!known) {
-                const double v = grad_norm_of(sums, count, fabsf(scale), area);
+                const double v = grad_norm_of(sums, count, fabs(scale), area);
                 if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(v);
                 factor = scale;
                 if (!(v <= max_norm)) factor *= max_norm / v;  // NaN: NaN, for all to see
@@ -272,14 +272,14 @@ static int launch_squares(const ftc_grad *grads, int count, void *ws, hipStream_
     });
 }
 
-int32_t launch_grad_norm(const ftc_grad *grads, int count, float scale, float *norm, void *ws, hipStream_t s)
+int32_t launch_grad_norm(const ftc_grad *grads, int count, double scale, float *norm, void *ws, hipStream_t s)
 {
     const int parts = count > 0 ? launch_squares(grads, count, ws, s) : 0;
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(GRAD_THREADS), 0, s, static_cast<const double *>(ws), parts, scale, norm);
     return launch_status("gradient norm");
 }
 
-int32_t launch_clip_grad_norm(const ftc_grad *grads, int count, float max_norm, float scale, float *norm, void *ws, hipStream_t s)
+int32_t launch_clip_grad_norm(const ftc_grad *grads, int count, double max_norm, double scale, float *norm, void *ws, hipStream_t s)
 {
     const int parts = count > 0 ? launch_squares(grads, count, ws, s) : 0;
     if (parts == 0) {  // nothing to clip: the norm of nothing

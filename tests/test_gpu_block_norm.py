@@ -109,7 +109,7 @@ def test_only_what_is_wanted():
     stream = torch.cuda.current_stream().cuda_stream
     only = torch.empty_like(U)
     b = B._block(s["X"], s["F"], 0.875, B.FTC_NORM_LAYER, s["post_w"], s["post_b"], s["gate"], B.FTC_NORM_LAYER, s["pre_w"], s["pre_b"], 1e-5)
-    B._check(B.lib().ftc_block_norm(B.C.byref(b), None, 0, only.data_ptr(), 72, None, stream))
+    B._check(B.lib().ftc_block_norm(b, None, 0, only.data_ptr(), 72, None, stream))
     assert torch.equal(only, U)
 
 

@@ -26,7 +26,7 @@ def check_norm(got, want):
 
 
 def check_clipped(got, grads, scale, max_norm):
-    norm, max_norm = norm_of(grads, scale), float(np.float32(max_norm))   # the limit is an argument in fp32: rounding it is the caller's
+    norm = norm_of(grads, scale)
     factor = scale * min(1.0, max_norm / norm) if norm else scale
     for i, (o, g) in enumerate(zip(got, grads)):
         # the factor in 64 bits, the product rounded to fp32 and from there to the type
@@ -99,9 +99,8 @@ def test_large_and_small_numbers():
             assert B.ftc_grad_norm([t]).item() == math.inf    # the number is not one of fp32; clipping has it in 64 bits
         out = torch.empty_like(t)
         B.ftc_clip_grad_norm(B.GradList([t], out=[out]), 1e-3 * value)
-        limit = float(np.float32(1e-3 * value))
-        if limit:
-            check("clipped", out, f64(t) * (limit / want), np.abs(f64(t) * (limit / want)) * 2.0 ** -23 + 2 * TINY[F32])
+        clipped = f64(t) * (1e-3 * value / want)
+        check("clipped", out, clipped, np.abs(clipped) * 2.0 ** -23 + 2 * TINY[F32])
     mixed = [torch.full((3,), 1e25, device="cuda"), torch.full((10**6,), 1.0, device="cuda")]
     check_norm(B.ftc_grad_norm(mixed), norm_of(mixed))
 
