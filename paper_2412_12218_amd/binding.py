@@ -758,6 +758,8 @@ def _block(X, F, x_scale, post, post_w, post_b, gate, pre, pre_w, pre_b, eps):
             _vector(gate, d, (dt,))
         else:
             ldg = _ld(gate, n, d, dt)
+            if ldg < d:
+                raise ValueError("the rows of gate overlap (one gate for all rows is a vector)")
     at = lambda t: 0 if t is None else t.data_ptr()
     return _BLOCK.pack(n, d, _DTYPES[dt], post, pre, eps, x_scale, X.data_ptr(), at(F), at(gate), at(post_w), at(post_b), at(pre_w), at(pre_b),
                        _ld(X, n, d), 0 if F is None else _ld(F, n, d, dt), ldg)

@@ -76,6 +76,7 @@ __global__ __launch_bounds__(row_threads(L), 2) void block_norm_backward_kernel(
             r.clear(next_f);
             r.clear(next_dh);
             r.clear(next_du);
+            r.clear(next_gate);
             next_m = ftc_f32x4{0.f, 0.f, 0.f, 0.f};
         }
         r.load(a.X, a.ldx, row0, there, next_x);

@@ -72,7 +72,7 @@ def test_nothing_to_do():
 def test_binding_refuses(monkeypatch):
     X, w = torch.zeros(4, 8), torch.zeros(8)
     monkeypatch.setattr(B, "_here", lambda *t: 0)
-    for k in (dict(pre_w=torch.zeros(7)), dict(pre_w=w.double()), dict(F=torch.zeros(4, 7)), dict(F=torch.zeros(4, 8).half()), dict(gate=torch.zeros(3, 8)),
+    for k in (dict(pre_w=torch.zeros(7)), dict(pre_w=w.double()), dict(F=torch.zeros(4, 7)), dict(F=torch.zeros(4, 8).half()), dict(gate=torch.zeros(3, 8)), dict(F=X, gate=torch.zeros(8).expand(4, 8)),
               dict(gate=torch.zeros(7)), dict(stats=torch.zeros(4, 3)), dict(stats=torch.zeros(4, 4).double()), dict(H=torch.zeros(4, 9)),
               dict(U=torch.zeros(4, 8).half()), dict(F=torch.zeros(8, 4).t())):
         with pytest.raises(ValueError):

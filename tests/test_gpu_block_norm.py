@@ -236,3 +236,44 @@ def test_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, [H, U, *grads])), turn
+
+
+@pytest.mark.parametrize("d", [20, 64, 250])
+def test_rows_far_apart(d):
+    """Rows of a workgroup beyond 2^31 bytes of each other, and a matrix beyond 2^32."""
+    ld = 9_000_000
+    whole = torch.zeros(130 * ld, dtype=torch.float16, device="cuda")
+    X = whole.view(130, ld)[:, 5:5 + d]
+    X.copy_(matrix(130, d, torch.float16, 1))
+    near = X.contiguous()
+    w, dU = vector(d, torch.float16, 2, 1.0), matrix(130, d, torch.float16, 3)
+    stats, far_stats = torch.empty((130, 4), device="cuda"), torch.empty((130, 4), device="cuda")
+    _, want = B.ftc_block_norm(near, pre=B.FTC_NORM_LAYER, pre_w=w, stats=stats)
+    _, got = B.ftc_block_norm(X, pre=B.FTC_NORM_LAYER, pre_w=w, stats=far_stats)
+    # other lanes have a row: sums of d numbers in another order
+    ref = block(near, None, 1.0, "none", None, None, None, "layer", w, None, dU=dU)
+    check("U", got, *ref["U"])
+    check("U of near rows", want, *ref["U"])
+    g = B.ftc_block_norm_backward(X, far_stats, dU=dU, pre=B.FTC_NORM_LAYER, pre_w=w)
+    check("dX", g.dX, *ref["dX"])
+    check("dpre_w", g.dpre_w, *ref["dpre_w"])
+
+
+def test_two_streams_at_once():
+    form = FORMS[4]
+    n, d, dtype = 3000, 264, torch.bfloat16
+    s = given(n, d, dtype, form)
+    dH, dU = matrix(n, d, dtype, 9), matrix(n, d, dtype, 10)
+    stats = torch.empty((n, 4), device="cuda")
+    H, U = run(s, form, stats=stats)
+    want = [H, U, *run_back(s, form, stats, dH=dH, dU=dU)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [None, None]
+    for turn in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                own = torch.empty((n, 4), device="cuda")
+                h, u = run(s, form, stats=own)
+                got[i] = [h, u, *run_back(s, form, own, dH=dH, dU=dU)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
