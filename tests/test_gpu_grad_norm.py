@@ -153,3 +153,19 @@ def test_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(norm, want_norm) and all(torch.equal(a, b) for a, b in zip(grads, want)), turn
+
+
+def test_gradients_beyond_32_bits():
+    """A tensor of more than 2^31 numbers and 2^32 bytes; equal numbers, so the sums are known."""
+    n = 2 ** 31 + 12_345
+    t = torch.full((n,), 0.5, dtype=F16, device="cuda")
+    t[-1] = 2.0
+    want = math.sqrt((n - 1) * 0.25 + 4.0)
+    check_norm(B.ftc_grad_norm([t]), want)
+    B.ftc_clip_grad_norm([t], want / 2)      # halves
+    assert bool((t[:-1] == 0.25).all()) and t[-1].item() == 1.0
+    wide = torch.zeros((70_000, 33_000), dtype=F16, device="cuda")[:, :3]   # rows 66 kB apart, the last beyond 2^32 bytes
+    wide.fill_(0.5)
+    check_norm(B.ftc_grad_norm([wide]), math.sqrt(210_000 * 0.25))
+    B.ftc_clip_grad_norm([wide], math.sqrt(210_000 * 0.25) / 2)
+    assert bool((wide == 0.25).all())

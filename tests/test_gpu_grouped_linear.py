@@ -256,3 +256,44 @@ def test_last_turn_in_parts(dtype, lens):
             assert np.all(np.abs(slope_values(slope[at]) - s) <= ds)
             want, bound = grouped_backward(X[at], W[g:g + 1], [0, len(at)], dZ[at], slope[at], dtype, dtype)[0]
             check(f"dX {g}", dX[at], want, bound)
+
+
+def test_weights_beyond_32_bits():
+    """More than 2^32 bytes of weights, the last group's behind all of them."""
+    groups, d_in, d_out = 600, 2048, 2048
+    W = torch.zeros((groups, d_in, d_out), dtype=torch.float16, device="cuda")
+    W[-1] = matrix(d_in, d_out, torch.float16, 1, scale=d_in ** -0.5)
+    X, dZ = matrix(70, d_in, torch.float16, 2), matrix(70, d_out, torch.float16, 3)
+    for first in (0, 64):   # rows in front of it: of the group before
+        ptr = [0] * (groups - 1) + [first, 70]
+        out = B.ftc_grouped_linear(X, W, offsets(ptr))
+        at = slice(first, 70)
+        (z, dz), _, _ = grouped(X[at], W[-1:], [0, 70 - first], None, "none", None, torch.float16)
+        check("Z", out[at], z, dz)
+        assert bool((out[:first] == 0).all())
+        dX, dW, db = B.ftc_grouped_linear_backward(X, W, offsets(ptr), dZ, dw_dtype=torch.float16)
+        want = grouped_backward(X[at], W[-1:], [0, 70 - first], dZ[at], None, torch.float16, torch.float16)
+        check("dX", dX[at], *want[0])
+        check("dW", dW[-1:], *want[1])
+        check("db", db[-1:], *want[2])
+        assert bool((dW[:groups - 2] == 0).all()) and bool((db[:groups - 2] == 0).all())
+
+
+def test_two_streams_at_once():
+    lens = [900, 0, 77, 2000, 3]
+    ptr = np.cumsum([0] + lens).tolist()
+    X, W, b, _ = layer(ptr[-1], 5, 256, 320, torch.bfloat16, residual=False)
+    dZ, at = matrix(ptr[-1], 320, torch.bfloat16, 4), offsets(ptr)
+
+    def step():
+        slope = B.slope_like(dZ)
+        return [B.ftc_grouped_linear(X, W, at, bias=b, act=B.FTC_ACT_GELU, slope=slope), *B.ftc_grouped_linear_backward(X, W, at, dZ, slope=slope)]
+    want = step()
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [None, None]
+    for turn in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i] = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
