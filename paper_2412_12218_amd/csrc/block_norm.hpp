@@ -93,7 +93,7 @@ struct RowPieces {
     static __device__ __forceinline__ void store_whole(void *base, int64_t at, const float (&y)[V])
     {
         if constexpr (NT) store_piece_nt<T>(base, at, y);
-        else store_vec_any<V>(base, at, DT, y);
+        else store_piece<T>(base, at, y);
     }
     static __device__ __forceinline__ void put(Frag<T> &f, int u, ftc_u32x4 w)
     {
@@ -172,22 +172,32 @@ struct RowPieces {
     // A vector of d numbers; all vectors are loaded before the first is looked at.  NULL: `none` each
     __device__ __forceinline__ void fetch(const void *base, Frag<T> (&f)[C]) const
     {
+        clear(f);
+        if (!base) return;  // uniform
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int u = 0; u < UNITS; ++u) put(f[c], u, load_piece<T>(base, col(c, u), base ? d - col(c, u) : 0));
+            for (int u = 0; u < UNITS; ++u) {
+                const int at = col(c, u);
+                if (at >= d) continue;
+                ftc_u32x4 w;
+                if (WHOLE || d >= V) w = load_piece<T>(base, WHOLE ? at : min(at, d - V), V);
+                else w = load_piece<T>(base, at, d);
+                put(f[c], u, w);
+            }
     }
     __device__ __forceinline__ void vector(const void *base, const Frag<T> (&f)[C], float none, float (&x)[C][8]) const
     {
+        if (base) {
+            numbers(f, x);
+        } else {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            frag_numbers<T>(f[c], x[c]);
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[c][j] = base ? x[c][j] : none;
+                for (int j = 0; j < 8; ++j) x[c][j] = none;
         }
     }
 };
-
 
 // Mean (0 for FTC_NORM_RMS) of a row and what its distance from there is multiplied by.  The squares are those of the distances, from registers, so
 // a mean that is large beside the spread costs nothing.  Distances from 1e19 on, whose squares are infinite in fp32, once more times 2^-96.

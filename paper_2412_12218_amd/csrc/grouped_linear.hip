@@ -4,6 +4,7 @@
 // The products are the dense layer's tiles, each of one group (grouped_kernel.hpp), all groups in one launch.  What is kept of the activation, and the
 // roundings, are the dense layer's (linear.hip).
 #include "grouped_kernel.hpp"
+#include "stream_piece.hpp"
 
 namespace ftc {
 
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(256) void grouped_dp_kernel(int n, const int *__res
         if (dP && left > 0) {
             const int64_t at = row * width + col;
             if (left >= V) {
-                store_vec_any<V>(dP, at, DT, g);
+                store_piece<T>(dP, at, g);
             } else {
 #pragma unroll
                 for (int j = 0; j < V - 1; ++j)

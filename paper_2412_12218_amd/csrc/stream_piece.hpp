@@ -14,6 +14,18 @@ __device__ __forceinline__ ftc_u32x4 load_piece_nt(const void *base, int64_t idx
     const u4 v = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(static_cast<const char *>(base) + idx * T::BYTES));
     return ftc_u32x4{v.x, v.y, v.z, v.w};
 }
+template <class T>  // without the hint
+__device__ __forceinline__ void store_piece(void *base, int64_t idx, const float (&x)[T::VEC])
+{
+    if constexpr (T::BYTES == 4) {
+        typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+        *reinterpret_cast<f4 *>(static_cast<float *>(base) + idx) = f4{x[0], x[1], x[2], x[3]};
+    } else {
+        typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+        const ftc_u32x4 w = frag_of<T>(x).w;
+        *reinterpret_cast<u4 *>(static_cast<uint16_t *>(base) + idx) = u4{w[0], w[1], w[2], w[3]};
+    }
+}
 template <class T>
 __device__ __forceinline__ void store_piece_nt(void *base, int64_t idx, const float (&x)[T::VEC])
 {
