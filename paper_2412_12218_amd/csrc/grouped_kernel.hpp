@@ -11,7 +11,7 @@ namespace ftc {
 struct GroupedArgs {
     DenseArgs a;  // M: all rows (Z, dX); K: all rows (dW)
     const int *group_ptr;
-    int groups;
+    int groups, tail;  // tail: whether there may be one (grouped_tail_on)
 };
 
 // Z: A along the contraction, W across it.  dX: both along it.  dW: both across it, k_each rows a chunk, a.splits > 1 where groups may have several.
@@ -104,7 +104,7 @@ __device__ __forceinline__ int out_bytes(int dtype) { return dtype == FTC_F32 ? 
 struct GroupedTail {
     int full, rest, parts;  // tiles in front, tiles in parts, parts of each
 };
-constexpr int TAIL_PARTS = 8, TAIL_LEAST = 256;  // parts at most, indices of a part at least
+constexpr int TAIL_PARTS = 8;  // at most
 inline __host__ __device__ GroupedTail grouped_tail(int64_t tiles, int K)
 {
     const int rest = static_cast<int>(tiles % 256), full = static_cast<int>(tiles - rest);
@@ -146,8 +146,8 @@ __global__ __launch_bounds__(64 * RW * CW, 2) void grouped_rows_kernel(GroupedAr
             tn = id % tiles_n;
             return tm;
         }
-        if (TM == 256) {
-            tail = grouped_tail(static_cast<int64_t>(tiles) * tiles_n, g.a.splits > 1 ? 0 : g.a.K);
+        if (TM == 256 && g.tail) {
+            tail = grouped_tail(static_cast<int64_t>(tiles) * tiles_n, g.a.K);
             if (id >= tail.full && tail.rest) {
                 part_of = (id - tail.full) % tail.parts;
                 id = tail.full + (id - tail.full) / tail.parts;
@@ -233,7 +233,7 @@ template <class T, bool BX, bool FAST>
 void launch_grouped_rows_t(const GroupedArgs &g, int tile, hipStream_t s)
 {
     const int64_t most = grouped_most(g.a.M, g.groups, grouped_rows(tile)) * ceil_div(g.a.N, grouped_columns(tile));
-    const dim3 grid(static_cast<unsigned>(most + (tile == DENSE_256 ? 256 : 0)), g.a.splits);  // 256: the tail's parts
+    const dim3 grid(static_cast<unsigned>(most + (g.tail ? 256 : 0)), g.a.splits);  // 256: the tail's parts
     if (tile == DENSE_64) {
         hipLaunchKernelGGL((grouped_rows_kernel<T, BX, FAST, 2, 2, 1, 1>), grid, dim3(256), 0, s, g);
     } else if (tile == DENSE_128) {
@@ -242,7 +242,7 @@ void launch_grouped_rows_t(const GroupedArgs &g, int tile, hipStream_t s)
         hipLaunchKernelGGL((grouped_rows_kernel<T, BX, FAST, 1, 4, 1, 1>), grid, dim3(256), 0, s, g);
     } else if constexpr (FAST && T::BYTES == 2) {
         hipLaunchKernelGGL((grouped_rows_kernel<T, BX, FAST, 2, 4, 4, 2>), grid, dim3(512), 0, s, g);
-        if (g.a.splits == 1 && most > 256 && g.a.K >= 2 * TAIL_LEAST) hipLaunchKernelGGL(grouped_tail_kernel<T>, dim3(128 * 32), dim3(256), 0, s, g);
+        if (g.tail) hipLaunchKernelGGL(grouped_tail_kernel<T>, dim3(128 * 32), dim3(256), 0, s, g);
     }
 }
 

@@ -101,8 +101,10 @@ __global__ __launch_bounds__(256) void grouped_dp_kernel(int n, const int *__res
 #pragma unroll
     for (int i = 0; i < DP_ROWS; ++i) {
         const int64_t row = row0 + i * subs;
-        w[i] = load_piece<T>(dZ, row * ldz + col, row < end ? left : 0);
-        if (slope) u[i] = load_piece<T>(slope, row * lds + col, row < end ? left : 0);
+        // read for the last time
+        const bool all = row < end && left >= V;
+        w[i] = all ? load_piece_nt<T>(dZ, row * ldz + col) : load_piece<T>(dZ, row * ldz + col, row < end && left < V ? left : 0);
+        if (slope) u[i] = all ? load_piece_nt<T>(slope, row * lds + col) : load_piece<T>(slope, row * lds + col, row < end && left < V ? left : 0);
     }
     float sum[V];
 #pragma unroll
@@ -182,7 +184,7 @@ static size_t rows_ws(int n, int groups, int N, int K)
     size_t most = 0;
     for (int v = 0; v < 4; ++v) {
         const DensePlan p = grouped_plan(n, groups, N, K, v & 1, v & 2);
-        const size_t tail = p.tile == DENSE_256 ? 256ull * 256 * 256 : 0, own = p.splits > 1 ? static_cast<size_t>(p.splits) * n * N : tail;
+        const size_t tail = p.tile == DENSE_256 && grouped_tail_on(n, groups, N, K) ? 256ull * 256 * 256 : 0, own = p.splits > 1 ? static_cast<size_t>(p.splits) * n * N : tail;
         if (own > most) most = own;
     }
     return align_up(most * sizeof(float), 256);
@@ -204,6 +206,7 @@ static void grouped(GroupedArgs g, int dtype, void *ws, hipStream_t s)
     g.a.splits = p.splits;
     g.a.k_each = p.k_each;
     g.a.part = static_cast<float *>(ws);
+    g.tail = p.tile == DENSE_256 && p.splits == 1 && grouped_tail_on(g.a.M, g.groups, g.a.N, g.a.K);
     launch_grouped_rows<BX>(g, dtype, p.tile, s);
     if (p.splits > 1) {
         const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(g.a.M) * ceil_div(g.a.N, 8) + 255) / 256));

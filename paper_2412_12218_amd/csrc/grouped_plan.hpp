@@ -17,6 +17,17 @@ inline int64_t grouped_most(int n, int groups, int side) { return static_cast<in
 // What a tile of a group leaves for a later kernel has a place by its number: group g, rows s .. e - 1, has the numbers from s / side + g on.  ceil((e - s) / side) <= e / side - s / side + 1,
 // so the next group's are behind them, whatever the groups are, and all are below grouped_most().
 
+// Tiles that n rows in groups come to, as far as the host can tell: a group's last one is half full, or less, where there are many groups of few rows.
+inline int64_t grouped_tiles(int n, int groups, int N, int tile)
+{
+    const int used = groups < n ? groups : n;
+    return (n / grouped_rows(tile) + (3ll * used + 4) / 5) * dense_parts(N, grouped_columns(tile));
+}
+// Whether tiles of 256 behind the last full turn of the compute units are taken in parts (grouped_kernel.hpp): where a second kernel for them is no waste, as it is launched
+// before it is known how many tiles there are (5 us of 170 in a training step of 20 000 x 768 -> 768, whose 249 tiles are less than one turn).
+constexpr int TAIL_LEAST = 256;  // indices of a part at least
+inline bool grouped_tail_on(int n, int groups, int N, int K) { return K >= 2 * TAIL_LEAST && grouped_tiles(n, groups, N, DENSE_256) > 264; }
+
 // Z and dX: n rows in groups.
 inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fast)
 {
@@ -31,8 +42,8 @@ inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fa
         if (tile == DENSE_256 && (!fast || f32)) continue;
         const DenseCost &c = cost[f32][tile];
         const float alone = fast ? c.alone : 1.5f * c.alone;
-        const int used = groups < n ? groups : n;  // a group's last tile is half full, or less: that of many groups of few rows
-        const int64_t tiles = (n / grouped_rows(tile) + (3 * used + 4) / 5) * dense_parts(N, grouped_columns(tile));
+        const int64_t tiles = grouped_tiles(n, groups, N, tile);
+        const bool tail = tile == DENSE_256 && grouped_tail_on(n, groups, N, K);
         for (int want = 1; want <= 64; want = want < 8 ? want + 1 : want + want / 4) {
             DensePlan p = {tile, 1, static_cast<int>(dense_parts(dense_parts(K, want), 64) * 64)};
             p.splits = static_cast<int>(dense_parts(K, p.k_each));
@@ -41,7 +52,7 @@ inline DensePlan grouped_plan(int n, int groups, int N, int K, bool f32, bool fa
             const int64_t blocks = tiles * p.splits, share = (blocks + 255) / 256;
             const float steps = static_cast<float>(dense_parts(p.k_each, step));
             float us = steps * (share * c.shared > alone ? share * c.shared : alone);
-            if (blocks > 256ll * c.most) us = tile == DENSE_256 && p.splits == 1 ? steps * alone * blocks / 256 + TAIL_US : steps * (c.shared * blocks / 256 + 0.5f * alone);
+            if (blocks > 256ll * c.most) us = tail && p.splits == 1 ? steps * alone * blocks / 256 + TAIL_US : steps * (c.shared * blocks / 256 + 0.5f * alone);
             if (p.splits > 1) us += JOIN_US + 8.f * p.splits * n * N / PART_BYTES_US;
             if (us < least) {
                 least = us;
