@@ -98,13 +98,21 @@ __global__ __launch_bounds__(256) void grouped_dp_kernel(int n, const int *__res
     const int lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> log_lanes, col = (blockIdx.y * lanes + lane) * V, left = width - col;
     const int64_t row0 = span.start + static_cast<int64_t>(span.at) * side + sub, end = span.start + span.len;
     ftc_u32x4 w[DP_ROWS], u[DP_ROWS];
+    // both are read for the last time
+    if ((span.at + 1) * side <= span.len && static_cast<int>((blockIdx.y + 1) * lanes * V) <= width) {  // uniform: all of the rows and columns are there
 #pragma unroll
-    for (int i = 0; i < DP_ROWS; ++i) {
-        const int64_t row = row0 + i * subs;
-        // read for the last time
-        const bool all = row < end && left >= V;
-        w[i] = all ? load_piece_nt<T>(dZ, row * ldz + col) : load_piece<T>(dZ, row * ldz + col, row < end && left < V ? left : 0);
-        if (slope) u[i] = all ? load_piece_nt<T>(slope, row * lds + col) : load_piece<T>(slope, row * lds + col, row < end && left < V ? left : 0);
+        for (int i = 0; i < DP_ROWS; ++i) {
+            const int64_t row = row0 + i * subs;
+            w[i] = load_piece_nt<T>(dZ, row * ldz + col);
+            if (slope) u[i] = load_piece_nt<T>(slope, row * lds + col);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < DP_ROWS; ++i) {
+            const int64_t row = row0 + i * subs;
+            w[i] = load_piece<T>(dZ, row * ldz + col, row < end ? left : 0);
+            if (slope) u[i] = load_piece<T>(slope, row * lds + col, row < end ? left : 0);
+        }
     }
     float sum[V];
 #pragma unroll
