@@ -1,6 +1,10 @@
 // The norms around a block, with its gate and its residual connection, in one pass over the rows:
 //   p = Npost(F),  h = x_scale X + gate p,  u = Npre(h),  N(t) = (t - mean) / sqrt(mean((t - mean)^2) + eps) w + b   (RMS: without the mean).
 // All of a row is in registers (block_norm.hpp); h is normalised before it is rounded.
+//
+// Bound by memory: 50 000 x 1024 in fp16 with both norms and a gate 75 us (410 MB at 5.4 TB/s; a copy with the same hint reaches 6.3, without 5.6), 46 000 x 200 in fp32, one
+// norm, 13 us (74 MB, in cache in part).  A row is a lane's eight numbers wide, not more: two pieces a lane (one wave a row of 1024) take as long, with three waves a SIMD instead of
+// four.  What is not kept: registers for F in a norm without a block (66 instead of 131 in fp32, 13 us for 19).
 #include <algorithm>
 
 #include "block_norm.hpp"
