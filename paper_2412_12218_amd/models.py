@@ -309,25 +309,25 @@ class GraphTransformerPath:
 
     def _join(self, weights, at):
         """The arguments of the norms and the residual connection behind block `at` (0: in front of the first; 2 i + 1, 2 i + 2: behind attention and
-        feed-forward block of layer i) and the names and owners of their weights."""
-        layers, args, names = weights["layers"], dict(x_scale=self.residual_scale if at else 1.0, post=B.FTC_NORM_NONE, pre=self.norm), {}
+        feed-forward block of layer i) and, by the name of its gradient, where each of their weights is: in which layer (-1: the whole's) and its key."""
+        args, names = dict(x_scale=self.residual_scale if at else 1.0, post=B.FTC_NORM_NONE, pre=self.norm), {}
 
-        def take(owner, name, arg):
-            args[arg], names["d" + arg] = owner[name], (owner, name)
+        def take(layer, name, arg):
+            args[arg], names["d" + arg] = (weights["layers"][layer] if layer >= 0 else weights)[name], (layer, name)
 
-        def take_norm(owner, name, arg, kind):
-            take(owner, name, arg + "_w")
+        def take_norm(layer, name, arg, kind):
+            take(layer, name, arg + "_w")
             if kind == B.FTC_NORM_LAYER:
-                take(owner, name + "_bias", arg + "_b")
+                take(layer, name + "_bias", arg + "_b")
         if at:
-            owner, block = layers[(at - 1) // 2], ("attention", "feed")[(at - 1) % 2]
+            layer, block = (at - 1) // 2, ("attention", "feed")[(at - 1) % 2]
             args["F"], args["post"] = self.given[at - 1], self.post_norm
             if self.post_norm:
-                take_norm(owner, block + "_post", "post", self.post_norm)
+                take_norm(layer, block + "_post", "post", self.post_norm)
             if self.gates:
-                take(owner, block + "_gate", "gate")
+                take(layer, block + "_gate", "gate")
         if self.norm:
-            take_norm(*((weights, "head_norm") if at == 2 * self.layers else (layers[at // 2], ("attention_norm", "feed_norm")[at % 2])), "pre", self.norm)
+            take_norm(*((-1, "head_norm") if at == 2 * self.layers else (at // 2, ("attention_norm", "feed_norm")[at % 2])), "pre", self.norm)
         return args, names
 
     def _streams(self):
@@ -367,7 +367,6 @@ class GraphTransformerPath:
 
     def _backward_blocks(self, weights, grads, d_out, mask):
         between, ws, back = self._streams(), self.ws, B.ftc_linear_backward
-        into = {id(o): g for o, g in [(weights, grads), *zip(weights["layers"], grads["layers"])]}
 
         def join(at):
             """Through the join: d_h is the gradient of the stream in front of it then, d_given that of the block's result.  What reaches the stream behind it on the
@@ -378,8 +377,8 @@ class GraphTransformerPath:
             last = at == 2 * self.layers       # nothing goes on behind the head's norm
             got = B.ftc_block_norm_backward(between[max(at - 1, 0)], self.stats[at], dH=None if last and self.norm else self.d_h, dU=self.d_normed if self.norm else None,
                                             dX=self.d_h, dF=self.d_given if at else None, ws=ws, **args)
-            for name, (owner, key) in names.items():
-                into[id(owner)][key] = getattr(got, name)
+            for name, (layer, key) in names.items():
+                (grads["layers"][layer] if layer >= 0 else grads)[key] = getattr(got, name)
 
         def block_input(at, **k):
             """Where the gradient of what a block (or the head) got goes."""

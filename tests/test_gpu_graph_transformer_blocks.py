@@ -122,7 +122,7 @@ def test_training_step(dtype, form):
     errors = [off(logits, want)] + [off(a, b) for a, b in zip(flat(grads), want_grads)]
     print(dtype, form, [f"{e:.1e}" for e in errors], flush=True)
     assert all(g.dtype == torch.float32 and g.shape == b.shape for g, b in zip(flat(grads), want_grads)) and max(errors) < TOL[dtype]
-    # all of them clipped by their one norm: the product of a gradient and a factor in 64 bits, the limit an argument in fp32
+    # all of them clipped by their one norm: the product of a gradient and a factor in 64 bits, rounded once
     kept = [g.clone() for g in flat(grads)]
     total = math.sqrt(sum(float((g.double() ** 2).sum()) for g in kept))
     norm = path.clip(grads, 0.25 * total, scale=0.5)
@@ -157,6 +157,44 @@ def test_captured_training_step():
         eager = other.backward(ids, w, d_out, mask=mask)
         eager_norm = other.clip(eager, 1.0)
         assert torch.equal(path.logits, logits) and torch.equal(norm, eager_norm) and all(torch.equal(a, b) for a, b in zip(flat(grads), flat(eager)))
+
+
+def test_layers_that_share_weights():
+    """One dict for all layers: each has gradients of its own, those of layers with equal weights."""
+    dtype, form = torch.float16, FORMS[1]
+    lens, n, ptr, ids, mask, d_out, types = batch(dtype)
+    w = weights(dtype, form)
+    one = w | dict(layers=[w["layers"][0]] * LAYERS)
+    equal = w | dict(layers=[dict(w["layers"][0]) for _ in range(LAYERS)])
+    grads = []
+    for v in (one, equal):
+        path = path_of(form, n, ptr, types, dtype)
+        path.forward(ids, v, mask=mask)
+        grads.append(path.backward(ids, v, d_out, mask=mask))
+    assert all(sorted(g) == sorted(w["layers"][0]) for g in grads[0]["layers"])
+    assert all(torch.equal(a, b) for a, b in zip(flat(grads[0]), flat(grads[1])))
+
+
+@pytest.mark.parametrize("lens", [(), (0, 0), (1,)])
+def test_smallest_batches(lens):
+    """No graph, graphs without a node, one node."""
+    dtype, form = torch.float16, FORMS[1]
+    gen = torch.Generator().manual_seed(2)
+    n, w = sum(lens), weights(dtype, form)
+    ptr = torch.tensor([0] + list(torch.cumsum(torch.tensor(lens, dtype=torch.int64), 0)), dtype=torch.int32).cuda()
+    ids, types = (torch.randint(0, TYPES, (n,), generator=gen, dtype=torch.int32).cuda() for _ in range(2))
+    d_out, mask = torch.randn((n, OUT), generator=gen).to(dtype).cuda(), torch.ones(n, dtype=torch.uint8).cuda()
+    path = path_of(form, n, ptr, types, dtype)
+    logits = path.forward(ids, w)
+    grads = path.backward(ids, w, d_out)
+    norm = path.clip(grads, 1.0)
+    if n:
+        want, want_grads = reference(form, lens, ids, w, mask, d_out, types)
+        assert float((logits.cpu().double() - want).norm() / want.norm()) < TOL[dtype]
+        total = math.sqrt(sum(float((g ** 2).sum()) for g in want_grads))
+        assert abs(norm.item() - total) < TOL[dtype] * total
+    else:
+        assert logits.shape == (0, OUT) and norm.item() == 0 and not any(bool(g.any()) for g in flat(grads))
 
 
 def test_types_are_checked():
