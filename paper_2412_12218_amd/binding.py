@@ -576,28 +576,27 @@ def ftc_linear_backward(X, W, dZ, slope=None, want_dX=True, want_dW=True, want_d
 
 
 def _contiguous(t, shape, dtype):
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"expected a contiguous {shape} tensor of {dtype}, got {tuple(t.shape)} of {t.dtype}")
 
 
 def ftc_grouped_linear(X, W, group_ptr, bias=None, act=FTC_ACT_NONE, residual=None, out=None, out_dtype=None, slope=None, ws=None):
     """act(X W[g] + bias[g]) + residual for the rows group_ptr[g] .. group_ptr[g+1] of every group g; W groups x d_in x d_out, bias groups x d_out, group_ptr
     int32.  out in X's type unless given; rows of no group keep what out has there.  slope: see slope_like."""
-    (n, d_in), (groups, _, d_out) = X.shape, W.shape
+    (n, d_in), (groups, _, d_out), dt, L = X.shape, W.shape, X.dtype, lib()
     if out is None:
-        out = torch.empty((n, d_out), dtype=out_dtype or X.dtype, device=X.device)
+        out = torch.empty((n, d_out), dtype=out_dtype or dt, device=X.device)
     if ws is None:
-        ws = _workspace(lib().ftc_grouped_linear_workspace_bytes(n, groups, d_in, d_out), X.device)
+        ws = _workspace(L.ftc_grouped_linear_workspace_bytes(n, groups, d_in, d_out), X.device)
     stream = _here(X, W, group_ptr, bias, residual, out, slope, ws)
     _vector(group_ptr, groups + 1, (torch.int32,))
-    _contiguous(W, (groups, d_in, d_out), X.dtype)
+    _contiguous(W, (groups, d_in, d_out), dt)
     if bias is not None:
-        _contiguous(bias, (groups, d_out), X.dtype)
-    sdt = torch.float32 if X.dtype == torch.float32 else torch.int16
-    _check(lib().ftc_grouped_linear(n, _ptr(group_ptr), groups, _ptr(X), _ld(X, n, d_in), _dt(X), d_in, _ptr(W), d_out, _ptr(bias), act, _ptr(residual),
-                                    _ld(residual, n, d_out, X.dtype) if residual is not None else 0, _ptr(slope),
-                                    _ld(slope, n, d_out, sdt) if slope is not None else 0, _ptr(out), _ld(out, n, d_out), _dt(out), _ptr(ws),
-                                    ws.numel(), stream))
+        _contiguous(bias, (groups, d_out), dt)
+    ldr = _ld(residual, n, d_out, dt) if residual is not None else 0
+    lds = _ld(slope, n, d_out, torch.float32 if dt == torch.float32 else torch.int16) if slope is not None else 0
+    _check(L.ftc_grouped_linear(n, group_ptr.data_ptr(), groups, X.data_ptr(), _ld(X, n, d_in), _dt(X), d_in, W.data_ptr(), d_out, _ptr(bias), act,
+                                _ptr(residual), ldr, _ptr(slope), lds, out.data_ptr(), _ld(out, n, d_out), _dt(out), ws.data_ptr(), ws.numel(), stream))
     return out
 
 
