@@ -1,25 +1,28 @@
 // The norm over many gradients, norm = |scale| sqrt(sum of all g^2), and their clipping, out = scale min(1, max_norm / norm) g.
 //
-// A launch has as many gradients as fit its arguments, so there is nothing to copy to the device, and all of them in chunks of GRAD_CHUNK numbers
+// A launch has as many gradients as fit its arguments, so there is nothing to copy to the device, and all of them in chunks of up to GRAD_CHUNK numbers
 // that its workgroups take in turn.  Squares are added in 64 bits: no gradient that is finite overflows, and a sum over 10^8 numbers is as exact as one over ten.
 // Each workgroup leaves one sum; whoever needs the norm adds these up in order, the workgroups that clip for themselves, which saves a launch between.
 //
 // Bound by memory, which the gradients cross twice: 63 M in fp32, 133 tensors, squares 45 us (254 MB at 5.6 TB/s), clipping 78 (507 MB at 6.5, some of it from cache); small lists by
-// two launches, 4 and 6 us.
+// two launches, 3 and 4 us.
 #include "stream_piece.hpp"
 
 namespace ftc {
 
 constexpr int GRAD_THREADS = 256, GRAD_CHUNK = 8192;  // numbers of a chunk
+// Up to FEW_NUMBERS of all gradients in shorter ones, for more workgroups: clipping of 100 000 in 20 tensors 5.9 us in a graph, 8.3 in chunks of GRAD_CHUNK, a million 8.4 and 9.2, level at
+// 1.5 million, three 15.7 and 15.1.
+constexpr int FEW_CHUNK = 2048, FEW_NUMBERS = 1 << 20;
 constexpr int GRAD_GROUPS = 2048;                       // workgroups of a launch at most
 // 16 bytes each: neighbouring lanes have neighbouring ones
 constexpr int grad_vec(int dtype) { return dtype == FTC_F32 ? 4 : 8; }
 
 // The gradients of a launch: where each begins, how many numbers it has (a row of it) with its type in the two highest bits, and its first chunk.  What is contiguous, almost
 // everything, is one row; matrices of rows that are not have launches of their own.
-template <int MOST>
+template <int MOST, int NUMBERS = GRAD_CHUNK>
 struct GradWhole {
-    static constexpr int ENTRIES = MOST;
+    static constexpr int ENTRIES = MOST, CHUNK = NUMBERS;
     static constexpr bool ONE_ROW = true;
     const void *grad[MOST];
     void *out[MOST];
@@ -49,6 +52,8 @@ struct GradArgs {
     double *sums;  // one a workgroup
 };
 typedef GradArgs<GradWhole<140>> GradArgsWhole;
+typedef GradArgs<GradWhole<140, FEW_CHUNK>> GradArgsSmall;
+typedef GradArgs<GradWhole<32, FEW_CHUNK>> GradArgsFew;  // a launch with 4 kB of arguments takes the host 0.4 us more
 typedef GradArgs<GradRows<64>> GradArgsRows;
 static_assert(sizeof(GradArgsWhole) <= 4000 && sizeof(GradArgsRows) <= 4000, "within the arguments of a launch");
 
@@ -73,18 +78,18 @@ template <class E>
 __device__ __forceinline__ int type_of(const GradArgs<E> &a, int e) { return static_cast<int>(a.e.cols[e] >> GRAD_TYPE_SHIFT); }
 
 // This thread's pieces of chunk c, all on their way at once; and where they go.
-template <class T>
+template <class T, int CHUNK>
 struct GradPieces {
-    static constexpr int COUNT = GRAD_CHUNK / (GRAD_THREADS * T::VEC);
+    static constexpr int COUNT = CHUNK / (GRAD_THREADS * T::VEC);
     ftc_u32x4 w[COUNT];
     int left[COUNT];
     int64_t to[COUNT];
     template <class E>
     __device__ __forceinline__ void load(const GradArgs<E> &a, int e, uint32_t c)
     {
-        const int64_t cols = static_cast<int64_t>(a.e.cols[e] & ((1ull << GRAD_TYPE_SHIFT) - 1)), first = static_cast<int64_t>(c - a.e.first[e]) * (GRAD_CHUNK / T::VEC) + threadIdx.x;
+        const int64_t cols = static_cast<int64_t>(a.e.cols[e] & ((1ull << GRAD_TYPE_SHIFT) - 1)), first = static_cast<int64_t>(c - a.e.first[e]) * (CHUNK / T::VEC) + threadIdx.x;
         if constexpr (E::ONE_ROW) {
-            if (static_cast<int64_t>(c - a.e.first[e] + 1) * GRAD_CHUNK <= cols) {  // uniform: all of the chunk is there
+            if (static_cast<int64_t>(c - a.e.first[e] + 1) * CHUNK <= cols) {  // uniform: all of the chunk is there
 #pragma unroll
                 for (int i = 0; i < COUNT; ++i) {
                     to[i] = (first + i * GRAD_THREADS) * T::VEC;
@@ -143,7 +148,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_squares_kernel(GradArgs<E> 
         const int e = entry_of(a, c);
         by_type(type_of(a, e), [&](auto type) {
             typedef decltype(type) T;
-            GradPieces<T> p;
+            GradPieces<T, E::CHUNK> p;
             p.load(a, e, c);
 #pragma unroll
             for (int i = 0; i < p.COUNT; ++i) {
@@ -187,7 +192,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_clip_kernel(GradArgs<E> a, 
         by_type(type_of(a, e), [&](auto type) {
             typedef decltype(type) T;
             constexpr int DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
-            GradPieces<T> p;
+            GradPieces<T, E::CHUNK> p;
             p.load(a, e, chunk);
             if (!known) {
                 const double v = grad_norm_of(sums, count, fabs(scale), area);
@@ -229,7 +234,7 @@ size_t grad_norm_ws(int count)
 template <class Args, class F>
 static int each_launch_of(bool whole, const ftc_grad *grads, int count, double *sums, const F &f)
 {
-    constexpr int MOST = decltype(Args::e)::ENTRIES;
+    constexpr int MOST = decltype(Args::e)::ENTRIES, CHUNK = decltype(Args::e)::CHUNK;
     const bool clip = !sums;
     int all = 0;
     for (int i = 0; i < count;) {
@@ -239,7 +244,7 @@ static int each_launch_of(bool whole, const ftc_grad *grads, int count, double *
         for (; i < count && a.entries < MOST; ++i) {
             const ftc_grad &g = grads[i];
             if (g.rows == 0 || g.cols == 0 || grad_whole(g, clip) != whole) continue;
-            const int64_t rows = whole ? 1 : g.rows, cols = whole ? g.rows * g.cols : g.cols, vec = grad_vec(g.dtype), pieces = (cols + vec - 1) / vec, each = GRAD_CHUNK / vec;
+            const int64_t rows = whole ? 1 : g.rows, cols = whole ? g.rows * g.cols : g.cols, vec = grad_vec(g.dtype), pieces = (cols + vec - 1) / vec, each = CHUNK / vec;
             const int e = a.entries++;
             a.e.grad[e] = g.grad;
             a.e.out[e] = g.out;
@@ -264,7 +269,11 @@ static int each_launch_of(bool whole, const ftc_grad *grads, int count, double *
 template <class F>
 static int each_launch(const ftc_grad *grads, int count, double *sums, const F &f)
 {
-    const int whole = each_launch_of<GradArgsWhole>(true, grads, count, sums, f);
+    int64_t numbers = 0;
+    for (int i = 0; i < count && numbers <= FEW_NUMBERS; ++i) numbers += grads[i].rows * grads[i].cols;
+    const int whole = numbers > FEW_NUMBERS ? each_launch_of<GradArgsWhole>(true, grads, count, sums, f)
+                      : count > decltype(GradArgsFew::e)::ENTRIES ? each_launch_of<GradArgsSmall>(true, grads, count, sums, f)
+                                                                  : each_launch_of<GradArgsFew>(true, grads, count, sums, f);
     return whole + each_launch_of<GradArgsRows>(false, grads, count, sums ? sums + whole : nullptr, f);
 }
 

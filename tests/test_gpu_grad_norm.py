@@ -56,6 +56,22 @@ def test_norm_and_clipping(shapes):
         assert all(torch.equal(a, b) for a, b in zip(grads, kept))
 
 
+# on both sides of the number of tensors, and of numbers, from which on a program asks for other chunks, and of those
+@pytest.mark.parametrize("shapes", [[(2048,), (2047,), (2049,), (4096,)], [(40, 77)] * 32, [(40, 77)] * 33, [(2 ** 20 - 9,), (9,)], [(2 ** 20 - 9,), (10,)],
+                                    [(7,)] * 139 + [(2 ** 20 - 7 * 139,)], [(7,)] * 140 + [(2 ** 20,)], [(1, 3000)] * 300], ids=lambda s: f"{len(s)} {s[0]} {s[-1]}")
+def test_chunks(shapes):
+    for dtype in (F32, BF16):
+        grads = [numbers(s, dtype, i) for i, s in enumerate(shapes)]
+        norm = norm_of(grads)
+        out = [torch.full_like(g, 7) for g in grads]
+        got = B.ftc_clip_grad_norm(B.GradList(grads, out=out), 0.3 * norm)
+        check_norm(got, norm)
+        check_clipped(out, grads, 1.0, 0.3 * norm)
+        assert torch.equal(B.ftc_grad_norm(grads), got)
+        B.ftc_clip_grad_norm(grads, 0.3 * norm)
+        assert all(torch.equal(a, b) for a, b in zip(grads, out))
+
+
 def test_below_the_limit_everything_stays():
     grads = [numbers((50, 30), t, i) for i, t in enumerate((F32, F16, BF16))]
     kept = [g.clone() for g in grads]
