@@ -660,7 +660,8 @@ class GradList:
     gradients stay where they are.  The tensors share no memory, but that a gradient may be its own `out`."""
 
     def __init__(self, grads, out=None):
-        self.grads, self.out = list(grads), list(grads if out is None else out)
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
         if len(self.out) != len(self.grads):
             raise ValueError(f"{len(self.out)} outputs for {len(self.grads)} gradients")
         devices = {t.device for t in self.grads + self.out}
