@@ -252,8 +252,8 @@ class GraphTransformerPath:
       post_norm  a norm of what a block gives: "attention_post" and "feed_post" of a layer; layer norms have biases ("feed_norm_bias", ...)
       gates      learned factors of what a block adds, d of them: "attention_gate" and "feed_gate" of a layer
       residual_scale  what the residual connections multiply their input by
-      types      the type of every node (device int32, from 0 on below n_types): "up" and "down" are of each type, n_types x d x hidden and
-                 n_types x hidden x d, their biases n_types x hidden and n_types x d
+      types      the type of every node (contiguous int32 on graph_ptr's device, from 0 on below n_types): "up" and "down" are of each type, n_types x d x hidden and
+                 n_types x hidden x d, their biases n_types x hidden and n_types x d.  Read when the path is made: nodes of other types are another path
     clip() is the clipping of all gradients by their norm."""
 
     LINEAR = ("qkv", "out", "up", "down")
@@ -290,8 +290,11 @@ class GraphTransformerPath:
             return
         self.group_ptr = None
         if types is not None:
+            B._vector(types, n, (torch.int32,))     # what orders them reads n whole numbers of 32 bits on the device
+            if types.device != dev:
+                raise ValueError(f"types are on {types.device}, graph_ptr on {dev}")
             low, high = (int(x.item()) for x in types.aminmax()) if n else (0, -1)
-            if types.shape != (n,) or low < 0 or high >= n_types:
+            if low < 0 or high >= n_types:
                 raise ValueError(f"types of {n} nodes, from 0 on below n_types")
             self.perm, self.inv, _ = B.ftc_order_by_key(types)
             self.group_ptr = torch.zeros(n_types + 1, dtype=torch.int32, device=dev)
