@@ -16,7 +16,7 @@ template <class T, int L, int C, bool BLOCK, bool WHOLE, bool NT>
 __global__ __launch_bounds__(row_threads(L)) void block_norm_kernel(BlockArgs a, void *H, int64_t ldh, void *U, int64_t ldu, float *stats)
 {
     constexpr int GROUPS = row_threads(L) / L;
-    __shared__ float area[32];
+    __shared__ float area[64];
     int turn = 0;
     const RowPieces<T, L, C, WHOLE, NT> r = {a.d, static_cast<int>(threadIdx.x) % L, L < 64 ? static_cast<int>(threadIdx.x) / L : __builtin_amdgcn_readfirstlane(threadIdx.x / L)};
     auto scaled = [&](float (&x)[C][8], float mean, float rstd, const float (&w)[C][8], const float (&b)[C][8]) {

@@ -45,7 +45,7 @@ struct BlockArgs {
 
 #if defined(__HIPCC__)
 
-// Totals of K sums over the L lanes of a row, in each of them.  `area`: 2 x K x 16 floats of LDS, `turn`: which half, the other one at the next call
+// Totals of K sums, one or two, over the L lanes of a row, in each of them.  `area`: 2 x 32 floats of LDS, `turn`: which half, the other one at the next call, whatever its K
 // (a wave that writes a half again has passed the barrier of the call between, and so have all that read it).
 template <int L, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float *area, int &turn)
@@ -58,7 +58,8 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float *area, int &turn)
     if constexpr (L > 64) {
         constexpr int WAVES = L / 64;
         const int wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;  // of the row
-        float *half = area + turn * K * 16;
+        static_assert(K <= 2, "within a half");
+        float *half = area + turn * 32;
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
             for (int k = 0; k < K; ++k) half[k * 16 + wave] = v[k];
@@ -199,13 +200,15 @@ struct RowPieces {
     }
 };
 
-// Mean (0 for FTC_NORM_RMS) of a row and what its distance from there is multiplied by.  The squares are those of the distances, from registers, so
-// a mean that is large beside the spread costs nothing.  Distances from 1e19 on, whose squares are infinite in fp32, once more times 2^-96.
+// Mean (0 for FTC_NORM_RMS) of a row and what its distance from there is multiplied by.  A sum of d numbers is off by some roundings of the numbers
+// themselves, which is much beside a small spread, so the mean is taken in two steps: the distances from the first one, m, are exact but for a rounding of their own,
+// and their mean, which the sum of their squares brings along, is what m is off by.  sum (x - m)^2 / d is more than the variance by the square of that; where this is not
+// little (equal numbers), the squares are summed again.  So are, times 2^-96, distances from 1e19 on, whose squares are infinite in fp32.
 template <class T, int L, int C, bool WHOLE, bool NT>
 __device__ __forceinline__ void row_statistics(const RowPieces<T, L, C, WHOLE, NT> &r, int kind, float eps, const float (&x)[C][8], float *area, int &turn, float &mean, float &rstd)
 {
     const float each = 1.f / static_cast<float>(r.d);
-    float s[1] = {0.f};
+    float s[1] = {0.f}, moved = 0.f;
     mean = 0.f;
     if (kind == FTC_NORM_LAYER) {  // uniform
 #pragma unroll
@@ -214,35 +217,42 @@ __device__ __forceinline__ void row_statistics(const RowPieces<T, L, C, WHOLE, N
             for (int j = 0; j < 8; ++j) s[0] = fmaf(x[c][j], each, s[0]);  // zeros behind the row; no sum beyond the largest number
         row_sums<L, 1>(s, area, turn);
         mean = s[0];
-        s[0] = 0.f;
+        float two[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float v = r.has(c, j) ? x[c][j] - mean : 0.f;
-                s[0] = fmaf(v, v, s[0]);
+                two[0] = fmaf(v, v, two[0]);
+                two[1] = fmaf(v, each, two[1]);
             }
+        row_sums<L, 2>(two, area, turn);
+        s[0] = two[0];
+        mean += two[1];
+        moved = two[1] * two[1];
     } else {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[0] = fmaf(x[c][j], x[c][j], s[0]);
+        row_sums<L, 1>(s, area, turn);
     }
-    row_sums<L, 1>(s, area, turn);
-    rstd = 1.f / sqrtf(fmaf(s[0], each, eps));
+    const float square = fmaf(s[0], each, eps - moved);
+    rstd = 1.f / sqrtf(square);
     // lanes that meet in row_sums go the same way: those of a wave, or of a workgroup, which has one row then
-    const bool wide = s[0] == INFINITY;
-    if (L > 64 ? wide : __builtin_amdgcn_ballot_w64(wide) != 0) {
+    const bool wide = !(s[0] < INFINITY), again = wide || 64.f * moved > s[0] * each;
+    if (L > 64 ? again : __builtin_amdgcn_ballot_w64(again) != 0) {
+        const float scale = wide ? 0x1p-96f : 1.f;
         s[0] = 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float v = r.has(c, j) ? (x[c][j] - mean) * 0x1p-96f : 0.f;
+                const float v = r.has(c, j) ? (x[c][j] - mean) * scale : 0.f;
                 s[0] = fmaf(v, v, s[0]);
             }
         row_sums<L, 1>(s, area, turn);
-        if (wide) rstd = 0x1p-96f / sqrtf(s[0] * each);
+        if (again) rstd = scale / sqrtf(fmaf(s[0], each, wide ? 0.f : eps));
     }
 }
 
