@@ -203,7 +203,8 @@ struct RowPieces {
 // Mean (0 for FTC_NORM_RMS) of a row and what its distance from there is multiplied by.  A sum of d numbers is off by some roundings of the numbers
 // themselves, which is much beside a small spread, so the mean is taken in two steps: the distances from the first one, m, are exact but for a rounding of their own,
 // and their mean, which the sum of their squares brings along, is what m is off by.  sum (x - m)^2 / d is more than the variance by the square of that; where this is not
-// little (equal numbers), the squares are summed again.  So are, times 2^-96, distances from 1e19 on, whose squares are infinite in fp32.
+// little (equal numbers), the squares are summed again.  So are, times 2^-96, distances from 1e19 on, whose squares are infinite in fp32,
+// also where only eps makes them so.
 template <class T, int L, int C, bool WHOLE, bool NT>
 __device__ __forceinline__ void row_statistics(const RowPieces<T, L, C, WHOLE, NT> &r, int kind, float eps, const float (&x)[C][8], float *area, int &turn, float &mean, float &rstd)
 {
@@ -240,7 +241,7 @@ __device__ __forceinline__ void row_statistics(const RowPieces<T, L, C, WHOLE, N
     const float square = fmaf(s[0], each, eps - moved);
     rstd = 1.f / sqrtf(square);
     // lanes that meet in row_sums go the same way: those of a wave, or of a workgroup, which has one row then
-    const bool wide = !(s[0] < INFINITY), again = wide || 64.f * moved > s[0] * each;
+    const bool wide = !(square < INFINITY), again = wide || 64.f * moved > s[0] * each;
     if (L > 64 ? again : __builtin_amdgcn_ballot_w64(again) != 0) {
         const float scale = wide ? 0x1p-96f : 1.f;
         s[0] = 0.f;
@@ -252,7 +253,7 @@ __device__ __forceinline__ void row_statistics(const RowPieces<T, L, C, WHOLE, N
                 s[0] = fmaf(v, v, s[0]);
             }
         row_sums<L, 1>(s, area, turn);
-        if (again) rstd = scale / sqrtf(fmaf(s[0], each, wide ? 0.f : eps));
+        if (again) rstd = scale / sqrtf(fmaf(s[0], each, eps * scale * scale));
     }
 }
 

@@ -5,7 +5,7 @@ import torch
 
 from block_rows import block, tight
 from paper_2412_12218_amd import binding as B
-from test_gpu_block_norm import DTYPES, matrix, vector
+from test_gpu_block_norm import DTYPES, KINDS, matrix, vector
 from transformer_reference import check
 
 pytestmark = pytest.mark.gpu
@@ -80,3 +80,17 @@ def test_the_row_beside_it_does_not_matter():
         U, _ = layer_norm(X)
         keep = [i for i in range(39) if i not in (3, 12, 21, 30)]
         assert torch.equal(U[keep], alone[keep]) and bool((U[[3, 12]] == 0).all()) and bool(U[[21, 30]].isnan().all())
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_large_eps(kind):
+    """Squares beyond fp32 beside an eps that counts: 1 / sqrt(v + eps) is as the formula has it."""
+    X = torch.tensor([[1.5e19, -1.5e19, 1e19, -1e19], [3e19, -3e19, 2e19, -2e19], [1.0, 2.0, 3.0, 4.0], [1e19, -1e19, 0.0, 0.0]], device="cuda")
+    for eps in (3e38, 1e38, 1e36):
+        x, e = X.double().cpu().numpy(), float(np.float32(eps))
+        mean = x.mean(1, keepdims=True) if kind == "layer" else 0.0
+        r = 1 / np.sqrt(((x - mean) ** 2).mean(1) + e)
+        stats = torch.empty((4, 4), device="cuda")
+        _, U = B.ftc_block_norm(X, pre=KINDS[kind], eps=eps, stats=stats)
+        check(f"factor {kind} {eps}", stats[:, 3], r, r * 2.0 ** -20)     # 1 / sqrt of a sum of five: ten roundings at most
+        check(f"U {kind} {eps}", U, (x - mean) * r[:, None], np.abs((x - mean) * r[:, None]) * 2.0 ** -19 + 2.0 ** -40)
