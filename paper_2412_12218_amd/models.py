@@ -401,12 +401,14 @@ class GraphTransformerPath:
                 grouped = B.ftc_grouped_linear_backward
                 B.ftc_permute_rows(self.d_given, self.perm, out=self.unsorted)
                 _, g["down"], g["down_bias"] = grouped(self.up[i], w["down"], self.group_ptr, self.unsorted, dX=self.d_up, ws=ws)
-                _, g["up"], g["up_bias"] = grouped(self.by_type[i], w["up"], self.group_ptr, self.d_up, slope=self.slope[i], dX=self.d_by_type, ws=ws)
+                up = lambda **k: grouped(self.by_type[i], w["up"], self.group_ptr, self.d_up, slope=self.slope[i], dX=self.d_by_type, ws=ws, **k)
                 if self.norm:
+                    _, g["up"], g["up_bias"] = up()
                     B.ftc_permute_rows(self.d_by_type, self.inv, out=self.d_normed)
-                else:
-                    B.ftc_permute_rows(self.d_by_type, self.inv, out=self.unsorted)
-                    B.ftc_block_norm(self.d_h, F=self.unsorted, pre=B.FTC_NORM_NONE, H=self.d_h)
+                else:       # d_h in the order of the types and back: the product is added to it before their one rounding
+                    B.ftc_permute_rows(self.d_h, self.perm, out=self.unsorted)
+                    _, g["up"], g["up_bias"] = up(dX_add=self.unsorted)
+                    B.ftc_permute_rows(self.d_by_type, self.inv, out=self.d_h)
             join(at + 1)
             _, g["out"], g["out_bias"] = back(self.attended[i], w["out"], self.d_given, dX=self.d_attended, ws=ws)
             args, kw = self._attention_args(i, mask)
