@@ -101,23 +101,6 @@ __device__ __forceinline__ const void *moved(const void *p, int64_t bytes) { ret
 __device__ __forceinline__ void *moved(void *p, int64_t bytes) { return p ? static_cast<char *>(p) + bytes : nullptr; }
 __device__ __forceinline__ int out_bytes(int dtype) { return dtype == FTC_F32 ? 4 : 2; }
 
-// Tiles of 256 have a compute unit each, so those behind the last 256 of a launch would take as long as 256 do.  Where these are at most half of 256 their contraction is taken
-// in parts, for as many workgroups as there are units: each writes its part of a tile, and grouped_tail_kernel adds them up.  us of 48 000 rows in 16 groups, 4096 -> 1024 in fp16, 776 tiles:
-// 482 without, 440.
-struct GroupedTail {
-    int full, rest, parts;  // tiles in front, tiles in parts, parts of each
-};
-constexpr int TAIL_PARTS = 8;  // at most
-inline __host__ __device__ GroupedTail grouped_tail(int64_t tiles, int K)
-{
-    const int rest = static_cast<int>(tiles % 256), full = static_cast<int>(tiles - rest);
-    if (full == 0 || rest == 0 || rest > 128) return {static_cast<int>(tiles), 0, 1};
-    const int fill = 256 / rest, most = K / TAIL_LEAST, parts = fill < TAIL_PARTS ? fill : TAIL_PARTS, take = parts < most ? parts : most;
-    if (take < 2) return {static_cast<int>(tiles), 0, 1};
-    return {full, rest, take};
-}
-__device__ __forceinline__ int tail_each(int K, int parts) { return ((K + parts - 1) / parts + 63) / 64 * 64; }
-
 // The product of a group, out of that of all rows.
 template <class T>
 __device__ __forceinline__ DenseArgs of_group(const DenseArgs &all, const GroupSpan &span)

@@ -28,6 +28,24 @@ inline int64_t grouped_tiles(int n, int groups, int N, int tile)
 constexpr int TAIL_LEAST = 256;  // indices of a part at least
 inline bool grouped_tail_on(int n, int groups, int N, int K) { return K >= 2 * TAIL_LEAST && grouped_tiles(n, groups, N, DENSE_256) > 264; }
 
+// Tiles of 256 have a compute unit each, so those behind the last 256 of a launch would take as long as 256 do.  Where these are at most half of 256 their contraction is taken
+// in parts, for as many workgroups as there are units: each writes its part of a tile, and grouped_tail_kernel (grouped_kernel.hpp) adds them up.  us of 48 000 rows in 16 groups, 4096 -> 1024 in fp16, 776 tiles:
+// 482 without, 440.
+struct GroupedTail {
+    int full, rest, parts;  // tiles in front, tiles in parts, parts of each
+};
+constexpr int TAIL_PARTS = 8;  // at most
+constexpr GroupedTail grouped_tail(int64_t tiles, int K)
+{
+    const int rest = static_cast<int>(tiles % 256), full = static_cast<int>(tiles - rest);
+    if (full == 0 || rest == 0 || rest > 128) return {static_cast<int>(tiles), 0, 1};
+    const int fill = 256 / rest, most = K / TAIL_LEAST, parts = fill < TAIL_PARTS ? fill : TAIL_PARTS, take = parts < most ? parts : most;
+    if (take < 2) return {static_cast<int>(tiles), 0, 1};
+    return {full, rest, take};
+}
+// Indices of a part, whole steps; the last parts can be without any.
+constexpr int tail_each(int K, int parts) { return ((K + parts - 1) / parts + 63) / 64 * 64; }
+
 // Z and dX: n rows in groups.  As dense_plan() has it, with the tile of 32 rows at the cost of one of 64: it is as fast at reading weights and has half as many rows to be without.
 // us of tiles of 64 / of 32 rows, 64 groups, 1024 -> 4096: 24 rows bf16 25 / 24, fp32 81 / 50; 200 rows 77 / 75, 207 / 135; 1000 rows 97 / 91, 248 / 172; larger tiles, other sizes: 8 rows in 8 groups,
 // 4096 -> 512 in bf16 31 (64), 14 (64, in parts, as taken), 48 000 in 16, 4096 -> 1024 in fp16 706 (64), 482 (128), 440 (256); 20 000 in 8, 768 -> 768 50, 44 to 46, 49.
