@@ -67,13 +67,18 @@ __global__ __launch_bounds__(256) void grouped_dp_kernel(int n, const int *__res
     const int lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> log_lanes, col = (blockIdx.y * lanes + lane) * V, left = width - col;
     const int64_t row0 = span.start + static_cast<int64_t>(span.at) * side + sub, end = span.start + span.len;
     ftc_u32x4 w[DP_ROWS], u[DP_ROWS];
-    // both are read for the last time
+    // with a slope both are read for the last time, as dP takes their place; without one dZ itself is what dX and dW read next
+    // (backward pass of 48 000 x 1024 -> 1024 in 16 groups in fp16 without a slope 322 us with the hint on dZ, 306 without; 46 000 x 100 -> 128 in 118 groups in fp32 65, 62)
     if ((span.at + 1) * side <= span.len && static_cast<int>((blockIdx.y + 1) * lanes * V) <= width) {  // uniform: all of the rows and columns are there
 #pragma unroll
         for (int i = 0; i < DP_ROWS; ++i) {
             const int64_t row = row0 + i * subs;
-            w[i] = load_piece_nt<T>(dZ, row * ldz + col);
-            if (slope) u[i] = load_piece_nt<T>(slope, row * lds + col);
+            if (slope) {
+                w[i] = load_piece_nt<T>(dZ, row * ldz + col);
+                u[i] = load_piece_nt<T>(slope, row * lds + col);
+            } else {
+                w[i] = load_piece<T>(dZ, row * ldz + col, V);
+            }
         }
     } else {
 #pragma unroll
