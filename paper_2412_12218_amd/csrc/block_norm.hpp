@@ -9,7 +9,7 @@
 
 namespace ftc {
 
-// Lanes of a row: as many as make it one piece each, up to 512, and two from there on.  Rows of a workgroup that are 2^31 bytes apart have 64 lanes at least.
+// Lanes of a row: as many as make it one piece each, up to 512, and two from there on, 1024 lanes above 8192 numbers.  Rows of a workgroup that are 2^31 bytes apart have 64 lanes at least.
 constexpr int ROW_LANES[] = {4, 8, 16, 32, 64, 128, 192, 256, 384, 512};
 inline int row_lanes(int d, int64_t widest_ld, int bytes)
 {
@@ -80,7 +80,7 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float *area, int &turn)
 // WHOLE: rows are whole 16 bytes, which are there or not; else the last ones of a row are loaded as the row's last 16 bytes, and moved.
 template <class T, int L, int C, bool WHOLE, bool NT>
 struct RowPieces {
-    static constexpr int V = T::VEC, UNITS = 8 / V, DT = T::BYTES == 4 ? FTC_F32 : std::is_same<T, F16>::value ? FTC_F16 : FTC_BF16;
+    static constexpr int V = T::VEC, UNITS = 8 / V;
     int d, lane, sub;  // sub: which of the workgroup's rows (uniform from 64 lanes on)
     __device__ __forceinline__ int col(int c, int u) const { return V * ((c * UNITS + u) * L + lane); }
     __device__ __forceinline__ bool has(int c, int j) const { return WHOLE ? col(c, j / V) < d : col(c, j / V) + j % V < d; }

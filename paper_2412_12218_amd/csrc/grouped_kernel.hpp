@@ -17,7 +17,7 @@ struct GroupedArgs {
     int groups, tail;  // tail: whether there may be one (grouped_tail_on)
 };
 
-// Z: A along the contraction, W across it.  dX: both along it.  dW: both across it, k_each rows a chunk, a.splits > 1 where groups may have several.
+// Z: A along the contraction, W across it.  dX: both along it.  dW: both across it, in chunks of at most k_each rows.
 template <bool BX>
 void launch_grouped_rows(const GroupedArgs &g, int dtype, int tile, hipStream_t s);
 void launch_grouped_dw(const GroupedArgs &g, int dtype, int tile, hipStream_t s);
@@ -37,9 +37,9 @@ int64_t grouped_dw_groups(int n, int groups, int k_each, int64_t tiles);
 
 #if defined(__HIPCC__)
 
-// What a workgroup is for: tile (chunk) `at` of the rows start .. start + len - 1 of a group, of the tiles of all groups; group -1: nothing.
+// What a workgroup is for: tile (chunk) `at` of the rows start .. start + len - 1 of a group; group -1: nothing.
 struct GroupSpan {
-    int group, start, len, at, tiles;
+    int group, start, len, at;
 };
 __device__ __forceinline__ int group_offset(const int *ptr, int i, int n) { return min(max(ptr[i], 0), n); }
 // Tiles of a group; EMPTY: one of a group without rows, too.
@@ -60,18 +60,18 @@ __device__ __forceinline__ GroupSpan group_span(const int *ptr, int groups, int 
     const int lane = threadIdx.x & 63;
     if (groups > GROUPS_COUNTED) {
         const int tiles = n / side + groups, wanted = number(tiles);
-        if (wanted < 0 || wanted >= tiles) return {-1, 0, 0, 0, tiles};
+        if (wanted < 0 || wanted >= tiles) return {-1, 0, 0, 0};
         int lo = 0, hi = groups;  // the last group whose numbers begin at or before it is in lo .. hi - 1
         do {
             const int stride = (hi - lo + 63) / 64, i = lo + lane * stride;
             const bool before = i < hi && group_offset(ptr, i, n) / side + i <= wanted;
             const int count = __popcll(__builtin_amdgcn_ballot_w64(before));
-            if (count == 0) return {-1, 0, 0, 0, tiles};  // in front of the first group
+            if (count == 0) return {-1, 0, 0, 0};  // in front of the first group
             lo += (count - 1) * stride;
             hi = min(lo + stride, hi);
         } while (hi - lo > 1);
         const int s = __builtin_amdgcn_readfirstlane(group_offset(ptr, lo, n)), e = __builtin_amdgcn_readfirstlane(group_offset(ptr, lo + 1, n)), at = wanted - s / side - lo;
-        return {at >= 0 && at < group_tiles<EMPTY>(s, e, side) ? lo : -1, s, max(e - s, 0), at, tiles};
+        return {at >= 0 && at < group_tiles<EMPTY>(s, e, side) ? lo : -1, s, max(e - s, 0), at};
     }
     const int each = (groups + 63) / 64, from = min(lane * each, groups), to = min(from + each, groups);
     int own = 0, start = group_offset(ptr, from, n), last = start;
@@ -82,7 +82,7 @@ __device__ __forceinline__ GroupSpan group_span(const int *ptr, int groups, int 
         last = end;
     }
     const int upto = wave_inclusive_scan(own), tiles = __builtin_amdgcn_readlane(upto, 63), wanted = number(tiles);
-    if (wanted < 0 || wanted >= tiles) return {-1, 0, 0, 0, tiles};
+    if (wanted < 0 || wanted >= tiles) return {-1, 0, 0, 0};
     const int at_lane = __popcll(__builtin_amdgcn_ballot_w64(upto <= wanted));  // the first lane that has more
     int g = min(at_lane * each, groups - 1), at = wanted - __builtin_amdgcn_readlane(upto - own, at_lane);
     int s = __builtin_amdgcn_readlane(start, at_lane), e = each == 1 ? __builtin_amdgcn_readlane(last, at_lane) : group_offset(ptr, g + 1, n);
@@ -94,7 +94,7 @@ __device__ __forceinline__ GroupSpan group_span(const int *ptr, int groups, int 
         g = min(g + 1, groups - 1);
         e = group_offset(ptr, g + 1, n);
     }
-    return {at >= 0 && at < group_tiles<EMPTY>(s, e, side) ? g : -1, s, max(e - s, 0), at, tiles};  // else: offsets that decrease
+    return {at >= 0 && at < group_tiles<EMPTY>(s, e, side) ? g : -1, s, max(e - s, 0), at};  // else: offsets that decrease
 }
 
 __device__ __forceinline__ const void *moved(const void *p, int64_t bytes) { return p ? static_cast<const char *>(p) + bytes : nullptr; }
