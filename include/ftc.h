@@ -464,7 +464,8 @@ int32_t ftc_grouped_linear_backward(int32_t n, const int32_t *group_ptr, int32_t
  * F may be NULL: h = x_scale X.  Weights and biases (d numbers each) may be NULL: ones and zeros.  gate may be NULL (ones), d numbers (ldg 0) or
  * n x d (ldg >= d); gate, post_w and post_b are of F, post_w and post_b of a norm, and refused without.  All matrices and vectors are of `dtype`;
  * everything in between is fp32, and u is that of the unrounded h.  1 <= d <= 16384, eps > 0.  With distances from the mean above 1e19, whose squares fp32 does not
- * hold, rows are normalised as in exact arithmetic all the same.
+ * hold, rows are normalised as in exact arithmetic all the same, as long as the distances themselves are numbers of fp32.  A layer norm's mean is right to a rounding of it and some of
+ * the distances: equal numbers give the bias.
  */
 typedef enum {
     FTC_NORM_NONE = 0,

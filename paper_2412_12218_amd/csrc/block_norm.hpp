@@ -27,8 +27,8 @@ inline int row_groups(int n, int lanes, int threads_a_unit)
     return groups <= most ? groups : ceil_div(groups, ceil_div(groups, most));
 }
 // Whether a pass over these matrices (NULL: not there) takes the non-temporal hint (stream_piece.hpp): more than a third of the last-level cache of 256 MB, of which the kernels
-// before and behind have theirs.  us with / without: 74 MB (46 000 x 200 in fp32, normed) 14.9 / 13.1; 123 MB (20 000 x 768 in bf16, a block's join) 32 / 42, its gradients (184 MB) 46 / 54;
-// 256 MB (200 000 x 128) 47 / 50; 410 MB (50 000 x 1024) 75 / 80.
+// before and behind have theirs.  us with / without, over three sets of inputs in turn: 74 MB (46 000 x 200 in fp32, normed) 16.6 / 13.5; 123 MB (20 000 x 768 in bf16, a block's join with two layer norms) 35.0 / 36.6, its gradients
+// (184 MB) with their sums 52.4 / 53.3; 256 MB (200 000 x 128) 46 / 50; 410 MB (50 000 x 1024) 76 / 82.
 inline bool row_stream(int n, int d, int bytes, std::initializer_list<const void *> matrices)
 {
     int64_t all = 0;

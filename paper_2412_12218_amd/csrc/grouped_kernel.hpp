@@ -3,7 +3,7 @@
 // The groups' rows are known on the device only, so a launch has as many workgroups as groups could ever need (grouped_plan.hpp), and each of them looks up which tile of
 // which group it is for, or that it is not needed.
 //
-// As fast as the dense layer's tiles: 48 000 rows in 16 groups, 4096 -> 1024 in fp16 430 us (937 TFLOP/s; a library product of 8192^3 1086), 20 000 in 8 groups, 768 -> 768 in bf16 Z 48,
+// As fast as the dense layer's tiles: 48 000 rows in 16 groups, 4096 -> 1024 in fp16 430 to 453 us from card to card (937 to 889 TFLOP/s; a library product of 8192^3 1086), 20 000 in 8 groups, 768 -> 768 in bf16 Z 48,
 // dX 38, dW 48 us.  24 rows of 64 groups, 1024 -> 4096 in bf16: 24 us, 135 MB of weights at 5.6 TB/s.
 #pragma once
 #include "dense_kernel.hpp"

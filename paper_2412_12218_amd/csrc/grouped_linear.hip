@@ -2,7 +2,8 @@
 //   dP = dZ act'(P),  dX_g = dP_g W_g^T,  dW_g = X_g^T dP_g,  db_g = column sums of dP_g.
 //
 // The products are the dense layer's tiles, each of one group (grouped_kernel.hpp), all groups in one launch.  What is kept of the activation, and the
-// roundings, are the dense layer's (linear.hip).
+// roundings, are the dense layer's (linear.hip): act' is 16 bits of fixed point for 16-bit types (db 2e-4 to 3e-4 of its norm from one of unrounded slopes), dP is rounded to X's type, once, for both
+// of its products, which the matrix instructions have in that type: 2.3e-3 of their norms in bf16, 1.7e-3 without, which are the results' own roundings.
 #include "grouped_kernel.hpp"
 #include "stream_piece.hpp"
 
